@@ -34,6 +34,10 @@ EXPORTED = (
     "comem_decode_attn_noalloc", "comem_prefill_attn_workspace", "comem_prefill_attn_split",
     "comem_prefill_attn_split_paged",
 )
+ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
+PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_fork", "comem_kv_compact",
+                  "comem_kv_release")
+ROPE_INTERLEAVED = 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # COMEM_NOALLOC_SCRATCH_BYTES
 FLAG_DEBUG_CHECKS = 1
 DEVICE_ERR_CTX_LEN, DEVICE_ERR_BLOCK_TABLE = 1, 2
@@ -69,6 +73,42 @@ class CostInputs(ctypes.Structure):
         ("hbm_bytes_per_s", ctypes.c_double),
         ("prefill_tokens_per_s", ctypes.c_double),
         ("generated_tokens", ctypes.c_double),
+    ]
+
+
+class RopeConfig(ctypes.Structure):
+    """comem_rope_config: the norms' weights, the table of angles and the kind of rotation."""
+
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("cos_sin", ctypes.c_void_p),
+        ("num_positions", ctypes.c_int64),
+        ("rot_dim", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class PagesState(ctypes.Structure):
+    """comem_kv_pages: the pools, the block table and the reference counts."""
+
+    _fields_ = [
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("stride_layer", ctypes.c_int64),
+        ("stride_page", ctypes.c_int64),
+        ("stride_token", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("num_layers", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64),
+        ("refcounts", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p),
+        ("ctx_lens", ctypes.c_void_p),
+        ("num_rows", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32),
+        ("max_ctx_len", ctypes.c_int64),
     ]
 
 
@@ -154,6 +194,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comem_prefill_attn_split_paged.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, i64, i64, i32, i64, vp, i32, vp,
                                                    i32, i64, vp, vp, vp, sz, vp]
     lib.comem_prefill_attn_split_paged.restype = ctypes.c_int
+    rp, pp = ctypes.POINTER(RopeConfig), ctypes.POINTER(PagesState)
+    lib.comem_rope_append.argtypes = [vp, rp, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, i64, vp, vp,
+                                      i32, i64, vp]
+    lib.comem_rope_append_paged.argtypes = [vp, rp, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, i64,
+                                            i64, i32, i64, vp, i32, vp, i32, i64, vp]
+    lib.comem_kv_pages_workspace.argtypes = [vp, pp, ctypes.POINTER(sz)]
+    lib.comem_kv_reserve.argtypes = [vp, pp, vp, vp, vp, sz, vp]
+    lib.comem_kv_fork.argtypes = [vp, pp, vp, vp, i32, vp, vp, sz, vp]
+    lib.comem_kv_compact.argtypes = [vp, pp, vp, vp, i64, vp, vp, i32, vp, vp, sz, vp]
+    lib.comem_kv_release.argtypes = [vp, pp, vp, i32, vp]
+    for name in ROPE_EXPORTED + PAGES_EXPORTED:
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -339,6 +391,53 @@ def comem_prefill_attn_split_paged(plan, q, q_start, q_lens, max_q_len, k_pages,
            "comem_prefill_attn_split_paged")
 
 
+def comem_rope_append(plan, rope: RopeConfig, q, q_stride, new_k, k_stride, new_v, v_stride, q_start, q_lens, max_q_len,
+                      positions, q_out, k, v, stride_token, stride_head, seq_start, ctx_lens, batch, max_ctx_len,
+                      stream) -> None:
+    _check(load_library().comem_rope_append(plan, ctypes.byref(rope), q, q_stride, new_k, k_stride, new_v, v_stride,
+                                            q_start, q_lens, max_q_len, positions, q_out, k, v, stride_token,
+                                            stride_head, seq_start, ctx_lens, batch, max_ctx_len, stream),
+           "comem_rope_append")
+
+
+def comem_rope_append_paged(plan, rope: RopeConfig, q, q_stride, new_k, k_stride, new_v, v_stride, q_start, q_lens,
+                            max_q_len, positions, q_out, k_pages, v_pages, stride_page, stride_token, stride_head,
+                            page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len,
+                            stream) -> None:
+    _check(load_library().comem_rope_append_paged(plan, ctypes.byref(rope), q, q_stride, new_k, k_stride, new_v,
+                                                  v_stride, q_start, q_lens, max_q_len, positions, q_out, k_pages,
+                                                  v_pages, stride_page, stride_token, stride_head, page_size,
+                                                  num_pages, block_table, max_pages_per_seq, ctx_lens, batch,
+                                                  max_ctx_len, stream), "comem_rope_append_paged")
+
+
+def comem_kv_pages_workspace(plan, pages: PagesState) -> int:
+    nbytes = ctypes.c_size_t()
+    _check(load_library().comem_kv_pages_workspace(plan, ctypes.byref(pages), ctypes.byref(nbytes)),
+           "comem_kv_pages_workspace")
+    return nbytes.value
+
+
+def comem_kv_reserve(plan, pages: PagesState, add_lens, missing, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().comem_kv_reserve(plan, ctypes.byref(pages), add_lens, missing, workspace, workspace_bytes,
+                                           stream), "comem_kv_reserve")
+
+
+def comem_kv_fork(plan, pages: PagesState, parents, children, n, missing, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().comem_kv_fork(plan, ctypes.byref(pages), parents, children, n, missing, workspace,
+                                        workspace_bytes, stream), "comem_kv_fork")
+
+
+def comem_kv_compact(plan, pages: PagesState, rows, keep, keep_total, keep_start, keep_lens, n, missing, workspace,
+                     workspace_bytes, stream) -> None:
+    _check(load_library().comem_kv_compact(plan, ctypes.byref(pages), rows, keep, keep_total, keep_start, keep_lens, n,
+                                           missing, workspace, workspace_bytes, stream), "comem_kv_compact")
+
+
+def comem_kv_release(plan, pages: PagesState, rows, n, stream) -> None:
+    _check(load_library().comem_kv_release(plan, ctypes.byref(pages), rows, n, stream), "comem_kv_release")
+
+
 def _cost_call(name, *args) -> float:
     out = ctypes.c_double()
     _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
@@ -411,6 +510,27 @@ def _fits(t, tensor, dtypes, device, shape) -> bool:
 
 
 # ------------------------------------------------------------ torch wrapper
+
+
+def _call_on(op, stream, entry, *args) -> None:
+    """entry(*args, stream) with the plan's device current (a stream belongs to its device)."""
+    import torch
+
+    if op._torch_device.type == "cuda" and torch.cuda.current_device() != op.device:
+        with torch.cuda.device(op.device):
+            entry(*args, op._stream(stream))
+    else:
+        entry(*args, op._stream(stream))
+
+
+def _empty_on(op, stream, shape, dtype):
+    """Memory from the allocator of the call's stream, so that it is not handed on while the call still runs."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=op._torch_device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=op._torch_device)
 
 
 # Placement of V relative to K that the C header recommends
@@ -776,3 +896,201 @@ class DecodeAttention:
         else:
             comem_prefill_attn_split_paged(*args, ws.data_ptr(), ws.nbytes, self._stream(stream))
         return out, lse
+
+    # Queries, keys and values of new tokens: norms, rotation and the cache store in one launch.
+
+    def _check_part(self, name, t, heads, rows):
+        """A projection's part: [rows, heads, d], a token's heads side by side."""
+        import torch
+
+        if (isinstance(t, torch.Tensor) and t.dtype in self._q_dtypes and t.device == self._torch_device
+                and t.shape == (rows, heads, self.head_dim) and t.stride()[1:] == (self.head_dim, 1)):
+            return
+        _check_tensor(name, t, self._q_dtypes, self._torch_device, shape=(rows, heads, self.head_dim),
+                      contiguous=False)
+        _need((t.stride(1) == self.head_dim or heads == 1 or rows == 0) and t.stride(2) == 1,
+              f"{name} must hold each token's heads side by side")
+
+    @staticmethod
+    def _row_stride(t, rows):
+        """Elements from a row to the next (of a single row torch may report any)."""
+        return t.stride(0) if rows > 1 else t.shape[1] * t.shape[2]
+
+    def _rope_args(self, q, new_k, new_v, ctx_lens, max_ctx_len, cos_sin, q_weight, k_weight, eps, q_start, q_lens,
+                   max_q_len, positions, interleaved, q_out, stream):
+        import torch
+
+        tensor, dev, i32 = torch.Tensor, self._torch_device, (torch.int32,)
+        _need(isinstance(q, tensor) and q.dim() == 3, "q must be a torch tensor [rows, heads, head_dim]")
+        rows = q.shape[0]
+        self._check_part("q", q, self.num_q_heads, rows)
+        self._check_part("new_k", new_k, self.num_kv_heads, rows)
+        self._check_part("new_v", new_v, self.num_kv_heads, rows)
+        if not (isinstance(cos_sin, tensor) and cos_sin.dtype == torch.float32 and cos_sin.device == dev
+                and cos_sin.dim() == 2 and cos_sin.is_contiguous()):
+            _check_tensor("cos_sin", cos_sin, (torch.float32,), dev, ndim=2)
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and not _fits(w, tensor, (q.dtype,), dev, (self.head_dim,)):
+                _check_tensor(name, w, (q.dtype,), dev, shape=(self.head_dim,))
+        _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
+        batch = rows if q_lens is None else (ctx_lens.shape[0] if isinstance(ctx_lens, tensor) and ctx_lens.dim() == 1
+                                             else -1)
+        if q_lens is not None:
+            if not (_fits(q_lens, tensor, i32, dev, (batch,)) and _fits(q_start, tensor, (torch.int64,), dev, (batch,))):
+                _check_tensor("ctx_lens", ctx_lens, i32, dev, ndim=1)
+                _check_tensor("q_start", q_start, (torch.int64,), dev, shape=(batch,))
+                _check_tensor("q_lens", q_lens, i32, dev, shape=(batch,))
+        if positions is not None and not _fits(positions, tensor, i32, dev, (rows,)):
+            _check_tensor("positions", positions, i32, dev, shape=(rows,))
+        self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_ctx_len)
+        if q_out is None:
+            q_out = _empty_on(self, stream, (rows, self.num_q_heads, self.head_dim), q.dtype)
+        elif not _fits(q_out, tensor, (q.dtype,), dev, (rows, self.num_q_heads, self.head_dim)):
+            _check_tensor("q_out", q_out, (q.dtype,), dev, shape=(rows, self.num_q_heads, self.head_dim))
+        rope = RopeConfig(None if q_weight is None else q_weight.data_ptr(),
+                          None if k_weight is None else k_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0],
+                          cos_sin.shape[1], eps, ROPE_INTERLEAVED if interleaved else 0)
+        head = (self.plan, rope, q.data_ptr(), self._row_stride(q, rows), new_k.data_ptr(),
+                self._row_stride(new_k, rows), new_v.data_ptr(), self._row_stride(new_v, rows),
+                None if q_start is None else q_start.data_ptr(), None if q_lens is None else q_lens.data_ptr(),
+                int(max_q_len), None if positions is None else positions.data_ptr(), q_out.data_ptr())
+        return batch, q_out, head
+
+    def rope_append(self, q, new_k, new_v, k, v, seq_start, ctx_lens, max_ctx_len: int, cos_sin, q_weight=None,
+                    k_weight=None, eps: float = 1e-6, q_start=None, q_lens=None, max_q_len: int = 1, positions=None,
+                    interleaved: bool = False, q_out=None, stream=None):
+        """Normalise and rotate the new tokens' queries and keys and store their keys and values; returns the queries.
+
+        q [rows, Hq, D], new_k and new_v [rows, Hkv, D] may be parts of one projection's output (each token's heads
+        side by side); cos_sin is float32 [positions, rot_dim], cosines first. Without q_start and q_lens each sequence
+        has one new token, else as in prefill. Give q_out=q to rotate dense queries in place.
+        """
+        batch, q_out, head = self._rope_args(q, new_k, new_v, ctx_lens, max_ctx_len, cos_sin, q_weight, k_weight, eps,
+                                             q_start, q_lens, max_q_len, positions, interleaved, q_out, stream)
+        self._check_cache(k, v, paged=False)
+        self._check_lengths(ctx_lens, batch, seq_start=seq_start)
+        _call_on(self, stream, comem_rope_append, *head, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                 seq_start.data_ptr(), ctx_lens.data_ptr(), batch, int(max_ctx_len))
+        return q_out
+
+    def rope_append_paged(self, q, new_k, new_v, k_pages, v_pages, block_table, ctx_lens, max_ctx_len: int, cos_sin,
+                          q_weight=None, k_weight=None, eps: float = 1e-6, q_start=None, q_lens=None,
+                          max_q_len: int = 1, positions=None, interleaved: bool = False, q_out=None, stream=None):
+        """The same into a paged cache."""
+        batch, q_out, head = self._rope_args(q, new_k, new_v, ctx_lens, max_ctx_len, cos_sin, q_weight, k_weight, eps,
+                                             q_start, q_lens, max_q_len, positions, interleaved, q_out, stream)
+        self._check_cache(k_pages, v_pages, paged=True)
+        self._check_lengths(ctx_lens, batch, block_table=block_table)
+        _call_on(self, stream, comem_rope_append_paged, *head, k_pages.data_ptr(), v_pages.data_ptr(),
+                 k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), k_pages.shape[1], k_pages.shape[0],
+                 block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len))
+        return q_out
+
+
+class KVPages:
+    """The pages of a paged cache, kept on the GPU: a block table and reference counts changed by kernels only.
+
+    op: the DecodeAttention whose plan the cache belongs to. k_pages, v_pages: [P, page_size, Hkv, D], or
+    [layers, P, page_size, Hkv, D] where one block table serves several layers. block_table int32 [R, width],
+    ctx_lens int32 [R] and refcounts int32 [P] are changed in place (all zero, and any table, to begin with). The object
+    holds these tensors and a workspace; its calls must be ordered, by one stream or by events.
+
+    reserve, fork and compact return the pages that were missing, a device int32 tensor of no dimension: 0, or the call
+    has changed nothing.
+    """
+
+    def __init__(self, op: DecodeAttention, k_pages, v_pages, block_table, ctx_lens, refcounts, max_ctx_len: int):
+        import torch
+
+        dev, i32 = op._torch_device, (torch.int32,)
+        layered = isinstance(k_pages, torch.Tensor) and k_pages.dim() == 5
+        if layered:
+            _need(isinstance(v_pages, torch.Tensor) and v_pages.shape == k_pages.shape
+                  and v_pages.stride() == k_pages.stride() and k_pages.shape[0] > 0,
+                  "k and v must have the same shape and strides, and a layer at least")
+            op._check_cache(k_pages[0], v_pages[0], paged=True)
+        else:
+            op._check_cache(k_pages, v_pages, paged=True)
+        pool = k_pages.shape[1:] if layered else k_pages.shape
+        strides = k_pages.stride() if layered else (0, *k_pages.stride())
+        _check_tensor("block_table", block_table, i32, dev, ndim=2)
+        _check_tensor("ctx_lens", ctx_lens, i32, dev, shape=(block_table.shape[0],))
+        _check_tensor("refcounts", refcounts, i32, dev, shape=(pool[0],))
+        op._check_bound(max_ctx_len)
+        self.op = op
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.block_table, self.ctx_lens, self.refcounts = block_table, ctx_lens, refcounts
+        self.max_ctx_len = int(max_ctx_len)
+        self._state = PagesState(k_pages.data_ptr(), v_pages.data_ptr(), *strides[:4],
+                                 k_pages.shape[0] if layered else 1, pool[1], pool[0], refcounts.data_ptr(),
+                                 block_table.data_ptr(), ctx_lens.data_ptr(), block_table.shape[0],
+                                 block_table.shape[1], self.max_ctx_len)
+        self.workspace_bytes = comem_kv_pages_workspace(op.plan, self._state)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+
+    def _list(self, name, t, dtype=None, shape=None):
+        import torch
+
+        dtypes = (dtype or torch.int32,)
+        if not (isinstance(t, torch.Tensor) and t.dim() == 1 and _fits(t, torch.Tensor, dtypes, self.op._torch_device,
+                                                                      t.shape if shape is None else shape)):
+            _check_tensor(name, t, dtypes, self.op._torch_device, shape=(None,) if shape is None else shape)
+        return t.data_ptr()
+
+    def _missing(self, missing, stream):
+        import torch
+
+        if missing is None:
+            return _empty_on(self.op, stream, (), torch.int32)
+        _need(isinstance(missing, torch.Tensor) and missing.dtype == torch.int32 and missing.numel() == 1
+              and missing.device == self.op._torch_device, f"missing must be one int32 on {self.op._torch_device}")
+        return missing
+
+    def reserve(self, add_lens, missing=None, stream=None):
+        """Room for add_lens[r] (int32 [R]) more tokens in every row: pages where they are needed, ctx_lens grown."""
+        add = self._list("add_lens", add_lens, shape=(self.block_table.shape[0],))
+        missing = self._missing(missing, stream)
+        _call_on(self.op, stream, comem_kv_reserve, self.op.plan, self._state, add, missing.data_ptr(),
+                 self.workspace.data_ptr(), self.workspace_bytes)
+        return missing
+
+    def fork(self, parents, children, missing=None, stream=None):
+        """Empty rows children[i] become second sequences on the tokens of parents[i] (int32 [n], children distinct)."""
+        src = self._list("parents", parents)
+        dst = self._list("children", children, shape=parents.shape)
+        missing = self._missing(missing, stream)
+        if parents.shape[0] == 0:
+            return missing.zero_() if stream is None else self._zeroed(missing, stream)
+        _call_on(self.op, stream, comem_kv_fork, self.op.plan, self._state, src, dst, parents.shape[0],
+                 missing.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes)
+        return missing
+
+    def compact(self, rows, keep, keep_start, keep_lens, missing=None, stream=None):
+        """Cut rows[i] (int32 [n], distinct) to the tokens keep[keep_start[i] : keep_start[i] + keep_lens[i]] of it,
+        strictly increasing positions (keep int32, keep_start int64 [n], keep_lens int32 [n])."""
+        import torch
+
+        at = self._list("rows", rows)
+        which = self._list("keep", keep)
+        start = self._list("keep_start", keep_start, torch.int64, rows.shape)
+        count = self._list("keep_lens", keep_lens, shape=rows.shape)
+        missing = self._missing(missing, stream)
+        if rows.shape[0] == 0:
+            return missing.zero_() if stream is None else self._zeroed(missing, stream)
+        _call_on(self.op, stream, comem_kv_compact, self.op.plan, self._state, at, which, keep.shape[0], start, count,
+                 rows.shape[0], missing.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes)
+        return missing
+
+    def release(self, rows, stream=None) -> None:
+        """Rows rows[i] (int32 [n]) give up their pages and become empty."""
+        at = self._list("rows", rows)
+        if rows.shape[0] > 0:
+            _call_on(self.op, stream, comem_kv_release, self.op.plan, self._state, at, rows.shape[0])
+
+    @staticmethod
+    def _zeroed(missing, stream):
+        import torch
+
+        with torch.cuda.stream(stream):
+            return missing.zero_()

@@ -17,8 +17,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libcomem_attn.so"
-SOURCES = ["api.cpp", "api_prefill.cpp", "kernel_mfma.hip", "kernel_valu.hip", "kernel_append.hip", "kernel_prefill.hip",
-           "noalloc.hip", "cost_model.cpp"]
+SOURCES = ["api.cpp", "api_prefill.cpp", "api_rope.cpp", "api_kv_pages.cpp", "kernel_mfma.hip", "kernel_valu.hip",
+           "kernel_append.hip", "kernel_prefill.hip", "kernel_rope.hip", "kernel_kv_pages.hip", "noalloc.hip",
+           "cost_model.cpp"]
 PROBE_LIB_NAME = "libcomem_probe.so"
 PROBE_SOURCES = ["probe.hip"]
 ARCH = "gfx950"

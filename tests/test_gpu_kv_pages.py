@@ -1,0 +1,329 @@
+"""The page operators on the GPU against host lists: tables, counts and lengths exactly, copied tokens bit for bit."""
+
+import random
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests.gpu_util import say  # noqa: E402
+from tests.ops_util import PagesModel, pages_of  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DTYPES = {"f32": (torch.float32, np.float32, 4), "bf16": (torch.bfloat16, np.int16, 2), "fp8": (torch.uint8, np.uint8, 1)}
+
+
+def _i32(values):
+    return torch.tensor(values, dtype=torch.int32, device=DEV)
+
+
+class Both:
+    """The state on the GPU and the model of it."""
+
+    def __init__(self, rows, num_pages, page, max_ctx, dtype="bf16", heads=2, d=64, layers=1, seed=1, width=None):
+        from paper_2605_30842_amd.binding import DecodeAttention, KVPages
+
+        t, n, size = DTYPES[dtype]
+        width = width or pages_of(max_ctx, page)
+        g = torch.Generator().manual_seed(seed)
+        shape = (layers, num_pages, page, heads, d)
+        raw = [torch.randint(0, 100, (*shape[:-1], d * size), generator=g, dtype=torch.uint8) for _ in range(2)]
+        pools = [r.to(DEV).view(t) for r in raw]
+        self.m = PagesModel(rows, width, num_pages, page, max_ctx, *(r.numpy().view(n).copy() for r in raw))
+        self.dtype = n
+        self.op = DecodeAttention(heads, heads, d, dtype, 0.1, max(rows, 1), max_ctx)
+        self.table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+        self.ctx, self.counts = _i32([0] * rows), _i32([0] * num_pages)
+        self.k, self.v = pools
+        one = layers == 1
+        self.p = KVPages(self.op, self.k[0] if one else self.k, self.v[0] if one else self.v, self.table, self.ctx,
+                         self.counts, max_ctx)
+
+    def reserve(self, add):
+        assert int(self.p.reserve(_i32(add))) == self.m.reserve(add)
+
+    def fork(self, parents, children):
+        got = int(self.p.fork(_i32(parents), _i32(children)))
+        assert got == self.m.fork(parents, children)
+        return got
+
+    def compact(self, rows, keeps):
+        starts = [sum(len(k) for k in keeps[:i]) for i in range(len(keeps))]
+        got = int(self.p.compact(_i32(rows), _i32([p for k in keeps for p in k]),
+                                 torch.tensor(starts, dtype=torch.int64, device=DEV), _i32([len(k) for k in keeps])))
+        assert got == self.m.compact(rows, keeps)
+        return got
+
+    def release(self, rows):
+        self.p.release(_i32(rows))
+        self.m.release(rows)
+
+    def check(self, pools=True):
+        torch.cuda.synchronize()
+        assert self.ctx.tolist() == self.m.ctx
+        assert self.table.tolist() == self.m.table
+        assert self.counts.tolist() == self.m.counts
+        if pools:
+            for got, want in ((self.k, self.m.k), (self.v, self.m.v)):
+                assert np.array_equal(got.view(torch.uint8).cpu().numpy().view(self.dtype), want)
+
+
+def _keep(rng, n):
+    kind = rng.choice(["all", "none", "head", "tail", "both", "some", "one"])
+    if kind in ("all", "none"):
+        return list(range(n)) if kind == "all" else []
+    if kind == "head":
+        return list(range(rng.randint(0, n)))
+    if kind == "tail":
+        return list(range(rng.randint(0, n), n))
+    if kind == "both":
+        a = rng.randint(0, n)
+        return list(range(a)) + list(range(rng.randint(a, n), n))
+    if kind == "one":
+        return [rng.randrange(n)] if n else []
+    return [t for t in range(n) if rng.random() < 0.6]
+
+
+@pytest.mark.parametrize("dtype,heads,d,layers", [("bf16", 2, 64, 1), ("fp8", 1, 64, 3), ("f32", 3, 128, 2),
+                                                  ("fp8", 8, 128, 1), ("bf16", 5, 128, 2)])
+@pytest.mark.parametrize("page", [1, 8, 16, 64])
+def test_random_lives(dtype, heads, d, layers, page):
+    """Sequences of calls, lists with bad rows and too few pages among them, the state checked after each."""
+    rng = random.Random(page * 100 + heads + d)
+    rows, max_ctx = 6, 150
+    b = Both(rows, max(4, 420 // page) + 3, page, max_ctx, dtype, heads, d, layers, width=pages_of(max_ctx, page) + 1)
+    short = 0
+    for step in range(30):
+        kind = rng.choice(["reserve", "reserve", "fork", "compact", "release"])
+        say("pages", dtype, page, step, kind)
+        if kind == "reserve":
+            b.reserve([rng.choice([0, 1, 1, 17, 60, -3, 1000]) for _ in range(rows)])
+        elif kind == "fork":
+            n = rng.randint(1, 3)
+            short += b.fork([rng.randrange(-1, rows + 1) for _ in range(n)], rng.sample(range(-1, rows + 1), n)) > 0
+        elif kind == "compact":
+            n = rng.randint(1, 3)
+            which = rng.sample(range(rows), n)
+            b.compact(which + ([rows + 3] if n == 1 else []),
+                      [_keep(rng, b.m.ctx[r]) for r in which] + ([[0, 1]] if n == 1 else []))
+        else:
+            b.release([rng.randrange(-1, rows + 1) for _ in range(rng.randint(1, 2))] * rng.randint(1, 2))
+        b.check()
+
+
+def test_lowest_pages_in_order():
+    b = Both(3, 20, 16, 100)
+    b.reserve([20, 0, 40])
+    assert b.table[0, :2].tolist() == [0, 1] and b.table[2, :3].tolist() == [2, 3, 4]
+    b.release([0])
+    b.reserve([0, 60, 0])
+    assert b.table[1, :4].tolist() == [0, 1, 5, 6]
+    b.check()
+
+
+@pytest.mark.parametrize("num_pages", [1, 15, 16, 17, 16383, 16384, 16385, 70001])
+def test_pools_of_many_sizes(num_pages):
+    """The look through the counts in steps and its ragged end: all pages but three are held, then all of them."""
+    say("pool of", num_pages)
+    b = Both(4, num_pages, 1, num_pages + 8, heads=1, d=64, dtype="fp8")
+    b.m.k = b.m.v = None
+    rng = random.Random(num_pages)
+    free = sorted(rng.sample(range(num_pages), min(3, num_pages)))
+    b.counts.fill_(1)
+    b.counts[torch.tensor(free, device=DEV)] = 0
+    b.m.counts = b.counts.tolist()
+    b.reserve([0, 0, len(free) - 1, 1])
+    b.check(pools=False)
+    b.reserve([0, 5, 1, 0])  # 6 short
+    b.check(pools=False)
+    b.release([3, 2])
+    b.reserve([len(free), 0, 0, 0])
+    b.check(pools=False)
+
+
+def test_more_rows_than_threads():
+    """3000 rows: their needs are added up over several rounds of the one workgroup."""
+    b = Both(3000, 9000, 4, 12, heads=1, d=64, dtype="fp8")
+    b.m.k = b.m.v = None
+    rng = random.Random(2)
+    for _ in range(3):
+        b.reserve([rng.randint(0, 4) for _ in range(3000)])
+        b.check(pools=False)
+    b.release([r for r in range(0, 3000, 3)])
+    b.check(pools=False)
+    full = b.fork(list(range(1, 3000, 3)), list(range(0, 3000, 3)))
+    b.check(pools=False)
+    assert full == 0
+
+
+def test_nothing_changes_when_pages_are_missing():
+    b = Both(3, 10, 16, 100, layers=2)
+    b.reserve([100, 33, 0])  # 7 + 3 pages: the pool is full
+    before = [t.clone() for t in (b.table, b.ctx, b.counts, b.k, b.v)]
+    assert b.fork([1], [2]) == 1
+    assert b.compact([0], [list(range(5, 100))]) == 6
+    b.reserve([0, 0, 17])
+    for was, now in zip(before, (b.table, b.ctx, b.counts, b.k, b.v)):
+        assert torch.equal(was, now)
+    b.release([1])
+    assert b.fork([0], [2]) == 0
+    b.check()
+
+
+def test_one_parent_several_children():
+    b = Both(6, 40, 16, 90)
+    b.reserve([70, 0, 0, 0, 0, 0])
+    b.fork([0, 0, 0], [1, 2, 5])
+    assert b.counts[:5].tolist() == [4, 4, 4, 4, 1]
+    b.check()
+    b.fork([1, 5], [3, 4])  # children of children
+    b.reserve([1, 1, 1, 0, 0, 1])
+    b.check()
+    b.release([0, 0, 1, 2, 3, 4])
+    b.release([5])
+    assert int(b.counts.abs().sum()) == 0
+    b.check()
+
+
+def test_fork_pairs_that_are_left_out():
+    b = Both(5, 40, 16, 90)
+    b.reserve([40, 7, 0, 0, 0])
+    for pair in (([0], [0]), ([0], [1]), ([9], [2]), ([-1], [3]), ([0], [7]), ([0], [-1])):
+        b.fork(*pair)
+        b.check()
+    b.fork([2], [4])  # of an empty row: an empty row
+    b.check()
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 32, 100])
+def test_compact_at_page_borders(n):
+    """Everything kept, nothing, and cuts around the ends of pages; the kept whole pages stay where they are."""
+    for keep in ([], [0], [n - 1], list(range(n)), list(range(n // 2)), list(range(n // 2, n)), list(range(1, n))):
+        b = Both(2, 30, 16, 100, seed=n)
+        b.reserve([n, 0])
+        b.fork([0], [1])
+        b.compact([1], [keep])
+        b.check()
+
+
+def test_compact_lists_outside_the_contract():
+    """Too long a list, one outside keep, a bad row: left as they are. Positions past the row: the nearest."""
+    b = Both(4, 40, 16, 90)
+    b.reserve([40, 33, 20, 10])
+    keep, start = _i32([1, 2, 3, 4, 5]), torch.tensor([0, 2, -1, 3], dtype=torch.int64, device=DEV)
+    assert int(b.p.compact(_i32([0, 1, 2, 3]), keep, start, _i32([41, 4, 2, -1]))) == 0
+    b.check()
+    assert int(b.p.compact(_i32([1]), _i32([0, 5, 900]), start[:1], _i32([3]))) == 0
+    assert b.m.compact([1], [[0, 5, 900]]) == 0
+    b.check()
+
+
+def test_lengths_and_entries_outside_the_contract():
+    """A row with a bad length is left out; a bad entry is read as page 0 and not counted."""
+    b = Both(4, 20, 16, 64)
+    b.reserve([40, 20, 0, 0])
+    b.ctx[1] = 65
+    b.p.reserve(_i32([0, 1, 0, 0]))
+    b.p.fork(_i32([1]), _i32([2]))
+    b.p.release(_i32([1]))
+    b.ctx[1] = -5
+    b.p.reserve(_i32([0, 1, 0, 0]))
+    b.p.fork(_i32([1]), _i32([2]))
+    b.p.release(_i32([1]))
+    b.p.compact(_i32([1]), _i32([0]), torch.zeros(1, dtype=torch.int64, device=DEV), _i32([1]))
+    b.ctx[1] = 20
+    b.check()
+    for bad in (-1, 20, 1 << 30):
+        b.table[0, 2] = b.table[0, 0] = bad
+        counts = b.counts.clone()
+        assert int(b.p.fork(_i32([0]), _i32([3]))) == 0
+        new = int(b.table[3, 2])
+        assert b.table[3].tolist()[:2] == [bad, 1]
+        assert torch.equal(b.k[0, new, :8], b.k[0, 0, :8]) and torch.equal(b.v[0, new, :8], b.v[0, 0, :8])
+        b.p.release(_i32([3]))
+        counts_after = b.counts.clone()
+        assert torch.equal(counts, counts_after)
+
+
+def test_graph_of_a_decode_loop_takes_pages_as_it_goes():
+    b = Both(5, 60, 16, 200, layers=2)
+    b.reserve([16, 15, 0, 100, 31])
+    one, missing = _i32([1, 1, 0, 1, 1]), _i32([0])
+    b.p.reserve(_i32([0] * 5), missing=missing)  # warm
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.p.reserve(one, missing=missing)
+    for i in range(40):
+        graph.replay()
+        b.m.reserve([1, 1, 0, 1, 1])
+        if i % 8 == 0:
+            b.check()
+    b.check()
+    assert int(missing) == 0
+
+
+def test_graph_with_fork_compact_release():
+    b = Both(4, 60, 16, 200)
+    b.reserve([77, 50, 0, 0])
+    parents, children = _i32([0, 1]), _i32([2, 3])
+    keep, start = _i32([0, 1, 2, 40, 41, 5, 6, 7]), torch.tensor([0, 5], dtype=torch.int64, device=DEV)
+    count, missing = _i32([5, 3]), _i32([9, 9])
+
+    def step():
+        b.p.release(children)
+        b.p.fork(parents, children, missing=missing[:1])
+        b.p.compact(children, keep, start, count, missing=missing[1:])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    b.m.fork([0, 1], [2, 3])
+    b.m.compact([2, 3], [[0, 1, 2, 40, 41], [5, 6, 7]])
+    for _ in range(3):
+        missing.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert missing.tolist() == [0, 0]
+        b.check()
+
+
+def test_other_stream():
+    b = Both(3, 40, 16, 200)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = b.p.reserve(_i32([100, 3, 0]), stream=side)
+    side.synchronize()
+    assert int(got) == 0 and b.m.reserve([100, 3, 0]) == 0
+    torch.cuda.synchronize()
+    rows = _i32([0]), _i32([2])
+    torch.cuda.synchronize()
+    got = b.p.fork(*rows, stream=side)
+    side.synchronize()
+    assert int(got) == 0 and b.m.fork([0], [2]) == 0
+    b.check()
+
+
+def test_copies_past_4_gib():
+    """Pages whose offsets, within a layer and over layers, pass 32 bits."""
+    from paper_2605_30842_amd.binding import DecodeAttention, KVPages
+
+    layers, pages, page = 2, 330, 4096  # 8 MB a page
+    k = torch.zeros((layers, pages, page, 8, 128), dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    counts = torch.ones(pages, dtype=torch.int32, device=DEV)
+    counts[pages - 2:] = 0
+    table, ctx = torch.full((2, 1), -1, dtype=torch.int32, device=DEV), _i32([0, 0])
+    p = KVPages(DecodeAttention(8, 8, 128, "bf16", 0.1, 2, page), k, v, table, ctx, counts, page)
+    assert int(p.reserve(_i32([100, 0]))) == 0
+    x = torch.randn((layers, 100, 8, 128), device=DEV).to(torch.bfloat16)
+    k[:, pages - 2, :100], v[:, pages - 2, :100] = x, -x
+    assert int(p.fork(_i32([0]), _i32([1]))) == 0
+    assert table.tolist() == [[pages - 2], [pages - 1]]
+    assert torch.equal(k[:, pages - 1, :100], x) and torch.equal(v[:, pages - 1, :100], -x)
+    assert int(torch.count_nonzero(k[:, pages - 1, 100:])) == 0 and int(torch.count_nonzero(k[:, :pages - 2])) == 0

@@ -1,0 +1,247 @@
+"""comem_kv_pages.h without a GPU: exported symbols, host-side validation, the wrapper's checks, the plain model."""
+
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2605_30842_amd import binding as B
+from tests.ops_util import PagesModel
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+A = 1 << 20
+
+
+def test_header_and_library():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "comem_kv_pages.h")).read(), flags=re.S)
+    assert sorted(set(re.findall(r"\b(comem_kv_[a-z_]+)\s*\(", text))) == sorted(B.PAGES_EXPORTED)
+    for name in B.PAGES_EXPORTED:
+        assert hasattr(B.load_library(), name)
+
+
+@pytest.fixture
+def plan():
+    p, _ = B.comem_decode_attn_init(B.Config(num_q_heads=32, num_kv_heads=8, head_dim=128, dtype=B.BF16, scale=0.088,
+                                             max_batch=4, max_ctx_len=4096), B.NO_DEVICE)
+    yield p
+    B.comem_decode_attn_destroy(p)
+
+
+def _state(**kw):
+    s = dict(k_pages=A, v_pages=A, stride_layer=100 * 16 * 1024, stride_page=16 * 1024, stride_token=1024,
+             stride_head=128, num_layers=2, page_size=16, num_pages=100, refcounts=A, block_table=A, ctx_lens=A,
+             num_rows=8, max_pages_per_seq=256, max_ctx_len=4096)
+    s.update(kw)
+    return B.PagesState(**s)
+
+
+def _bytes(plan, **kw):
+    n = ctypes.c_size_t()
+    assert B.load_library().comem_kv_pages_workspace(plan, ctypes.byref(_state(**kw)), ctypes.byref(n)) == B.OK
+    return n.value
+
+
+def _calls(plan, state, n=3, lists=A, missing=A, workspace=A, nbytes=None, keep=A, keep_total=50):
+    lib, s = B.load_library(), None if state is None else ctypes.byref(state)
+    nbytes = _bytes(plan) if nbytes is None else nbytes
+    return dict(
+        reserve=lib.comem_kv_reserve(plan, s, lists, missing, workspace, nbytes, None),
+        fork=lib.comem_kv_fork(plan, s, lists, lists, n, missing, workspace, nbytes, None),
+        compact=lib.comem_kv_compact(plan, s, lists, keep, keep_total, lists, lists, n, missing, workspace, nbytes,
+                                     None),
+        release=lib.comem_kv_release(plan, s, lists, n, None))
+
+
+def test_good_calls_stop_at_the_device(plan):
+    assert set(_calls(plan, _state()).values()) == {B.ERR_NO_DEVICE}
+    assert set(_calls(plan, _state(num_layers=1, stride_layer=0)).values()) == {B.ERR_NO_DEVICE}
+    assert _calls(plan, _state(), keep=None, keep_total=0)["compact"] == B.ERR_NO_DEVICE
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(page_size=0), B.ERR_INVALID_SHAPE), (dict(page_size=48), B.ERR_INVALID_SHAPE),
+    (dict(page_size=8192), B.ERR_INVALID_SHAPE), (dict(num_pages=0), B.ERR_INVALID_SHAPE),
+    (dict(num_pages=1 << 31), B.ERR_INVALID_SHAPE), (dict(num_rows=0), B.ERR_INVALID_SHAPE),
+    (dict(num_rows=65536), B.ERR_INVALID_SHAPE), (dict(max_ctx_len=0), B.ERR_INVALID_SHAPE),
+    (dict(max_ctx_len=4097), B.ERR_INVALID_SHAPE), (dict(max_pages_per_seq=255), B.ERR_INVALID_SHAPE),
+    (dict(refcounts=None), B.ERR_NULL_POINTER), (dict(block_table=None), B.ERR_NULL_POINTER),
+    (dict(ctx_lens=None), B.ERR_NULL_POINTER), (dict(refcounts=A + 4), B.ERR_MISALIGNED),
+    (dict(block_table=A + 2), B.ERR_MISALIGNED)], ids=str)
+def test_state_refusals(plan, kw, status):
+    assert set(_calls(plan, _state(**kw)).values()) == {status}
+    n = ctypes.c_size_t()
+    assert B.load_library().comem_kv_pages_workspace(plan, ctypes.byref(_state(**kw)), ctypes.byref(n)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(k_pages=None), B.ERR_NULL_POINTER), (dict(v_pages=None), B.ERR_NULL_POINTER),
+    (dict(num_layers=0), B.ERR_INVALID_SHAPE), (dict(stride_layer=0), B.ERR_INVALID_SHAPE),
+    (dict(stride_page=0), B.ERR_INVALID_SHAPE), (dict(stride_token=0), B.ERR_INVALID_SHAPE),
+    (dict(stride_head=0), B.ERR_INVALID_SHAPE), (dict(stride_token=1 << 40), B.ERR_INVALID_SHAPE),
+    (dict(stride_page=16 * 1024 + 4), B.ERR_MISALIGNED), (dict(stride_layer=12), B.ERR_MISALIGNED),
+    (dict(k_pages=A + 8), B.ERR_MISALIGNED)], ids=str)
+def test_pool_refusals(plan, kw, status):
+    """Calls that copy tokens look at the pools, the others do not."""
+    got = _calls(plan, _state(**kw))
+    assert got["fork"] == got["compact"] == status
+    assert got["reserve"] == got["release"] == B.ERR_NO_DEVICE
+
+
+def test_argument_refusals(plan):
+    s = _state()
+    assert set(_calls(plan, None).values()) == {B.ERR_NULL_POINTER}
+    assert set(_calls(None, s, nbytes=0).values()) == {B.ERR_BAD_HANDLE}
+    assert set(_calls(plan, s, lists=None).values()) == {B.ERR_NULL_POINTER}
+    assert set(_calls(plan, s, lists=A + 2).values()) == {B.ERR_MISALIGNED}
+    assert _calls(plan, s, lists=A + 4)["compact"] == B.ERR_MISALIGNED  # keep_start is int64
+    for n in (-1, 9):
+        got = _calls(plan, s, n=n)
+        assert {got["fork"], got["compact"], got["release"]} == {B.ERR_INVALID_SHAPE}
+    got = _calls(plan, s, n=0, lists=None, missing=None, workspace=None)
+    assert {got["fork"], got["compact"], got["release"]} == {B.OK}
+    for kw, status in [(dict(missing=None), B.ERR_NULL_POINTER), (dict(workspace=None), B.ERR_NULL_POINTER),
+                       (dict(missing=A + 2), B.ERR_MISALIGNED), (dict(workspace=A + 64), B.ERR_MISALIGNED),
+                       (dict(nbytes=_bytes(plan) - 1), B.ERR_WORKSPACE_TOO_SMALL)]:
+        got = _calls(plan, s, **kw)
+        assert {got["reserve"], got["fork"], got["compact"]} == {status}
+    assert _calls(plan, s, keep=None)["compact"] == B.ERR_NULL_POINTER
+    assert _calls(plan, s, keep_total=-1)["compact"] == B.ERR_INVALID_SHAPE
+
+
+def test_workspace_covers_its_parts(plan):
+    """Seven item arrays, the fresh pages and the rows' old entries."""
+    assert _bytes(plan) >= 4 * (7 * 8 + 100 + 8 * 256)
+    assert _bytes(plan, num_pages=1 << 20) >= 4 * (7 * 8 + 8 * 256 * 2)
+    n = ctypes.c_size_t()
+    assert B.load_library().comem_kv_pages_workspace(plan, ctypes.byref(_state()), None) == B.ERR_NULL_POINTER
+    assert B.load_library().comem_kv_pages_workspace(None, ctypes.byref(_state()), ctypes.byref(n)) == B.ERR_BAD_HANDLE
+
+
+# ------------------------------------------------------------ the wrapper
+
+
+class Reached(Exception):
+    pass
+
+
+@pytest.fixture
+def op(monkeypatch):
+    def sentinel(*a, **k):
+        raise Reached()
+
+    for name in B.PAGES_EXPORTED[1:]:
+        monkeypatch.setattr(B, name, sentinel)
+    o = object.__new__(B.DecodeAttention)
+    o.plan, _ = B.comem_decode_attn_init(B.Config(num_q_heads=8, num_kv_heads=2, head_dim=64, dtype=B.BF16, scale=0.1,
+                                                  max_batch=4, max_ctx_len=64), B.NO_DEVICE)
+    o.dtype, o.device = "bf16", 0
+    o.num_q_heads, o.num_kv_heads, o.head_dim = 8, 2, 64
+    o._torch_device = torch.device("cpu")
+    o._q_dtypes, o._kv_dtypes = B._torch_dtypes("bf16")
+    o._stream = lambda s: 0
+    return o
+
+
+def _pages(op, layers=0, **kw):
+    i32 = torch.int32
+    shape = ((layers,) if layers else ()) + (10, 16, 2, 64)
+    d = dict(k_pages=torch.zeros(shape, dtype=torch.bfloat16), v_pages=torch.zeros(shape, dtype=torch.bfloat16),
+             block_table=torch.zeros(3, 4, dtype=i32), ctx_lens=torch.zeros(3, dtype=i32),
+             refcounts=torch.zeros(10, dtype=i32), max_ctx_len=64)
+    d.update(kw)
+    return B.KVPages(op, **d)
+
+
+def test_wrapper_reads_the_pools(op):
+    one, two = _pages(op)._state, _pages(op, layers=2)._state
+    assert (one.num_layers, one.num_pages, one.page_size, one.stride_page) == (1, 10, 16, 16 * 128)
+    assert (two.num_layers, two.num_pages, two.page_size, two.stride_page) == (2, 10, 16, 16 * 128)
+    assert two.stride_layer == 10 * 16 * 128 and two.stride_token == 128 and two.stride_head == 64
+
+
+@pytest.mark.parametrize("change", [
+    dict(k_pages=torch.zeros(10, 16, 2, 64)), dict(v_pages=torch.zeros(9, 16, 2, 64, dtype=torch.bfloat16)),
+    dict(k_pages=torch.zeros(2, 10, 16, 2, 64, dtype=torch.bfloat16)), dict(block_table=torch.zeros(3, 4)),
+    dict(ctx_lens=torch.zeros(2, dtype=torch.int32)), dict(refcounts=torch.zeros(9, dtype=torch.int32)),
+    dict(refcounts=torch.zeros(10, dtype=torch.int64)), dict(max_ctx_len=64.0)], ids=lambda c: next(iter(c)))
+def test_wrapper_refuses_state(op, change):
+    with pytest.raises(ValueError):
+        _pages(op, **change)
+
+
+def test_wrapper_refuses_what_the_library_refuses(op):
+    with pytest.raises(B.ComemError):
+        _pages(op, block_table=torch.zeros(3, 3, dtype=torch.int32))  # 3 pages of 16 for 64 tokens
+    with pytest.raises(B.ComemError):
+        _pages(op, max_ctx_len=65)
+
+
+def test_wrapper_checks_lists(op):
+    p, i32 = _pages(op), torch.int32
+    two, three = torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)
+    start = torch.zeros(2, dtype=torch.int64)
+    for call in (lambda: p.reserve(three), lambda: p.fork(two, two), lambda: p.release(two),
+                 lambda: p.compact(two, three, start, two)):
+        with pytest.raises(Reached):
+            call()
+    for call in (lambda: p.reserve(two), lambda: p.reserve([1, 2, 3]), lambda: p.fork(two, three),
+                 lambda: p.fork(two.long(), two), lambda: p.fork(two[None], two[None]), lambda: p.release(two.float()),
+                 lambda: p.compact(two, three, two, two), lambda: p.compact(two, three, start, three),
+                 lambda: p.compact(two, three.long(), start, two),
+                 lambda: p.reserve(three, missing=torch.zeros(2, dtype=i32)),
+                 lambda: p.reserve(three, missing=torch.zeros(1))):
+        with pytest.raises(ValueError):
+            call()
+    none = torch.zeros(0, dtype=i32)
+    p.release(none)
+    assert int(p.fork(none, none)) == 0
+    assert int(p.compact(none, none, none.long(), none, missing=torch.ones((), dtype=i32))) == 0
+
+
+# ------------------------------------------------------------ the plain model
+
+
+def test_model_by_hand():
+    m = PagesModel(3, 4, 6, 4, 16)
+    assert m.reserve([5, 0, 4]) == 0
+    assert m.table == [[0, 1, -1, -1], [-1] * 4, [2, -1, -1, -1]] and m.counts == [1, 1, 1, 0, 0, 0]
+    assert m.fork([0], [1]) == 0
+    assert m.table[1][:2] == [0, 3] and m.counts == [2, 1, 1, 1, 0, 0]
+    assert m.compact([0], [[0, 1, 2, 3, 4]]) == 0  # the whole page stays, the partial one is copied
+    assert m.table[0][:2] == [0, 4] and m.counts == [2, 0, 1, 1, 1, 0]
+    assert m.compact([1], [[1, 3]]) == 0
+    assert m.table[1] == [1, -1, -1, -1] and m.counts == [1, 1, 1, 0, 1, 0]
+    assert m.reserve([0, 0, 12]) == 1 and m.counts == [1, 1, 1, 0, 1, 0]
+    m.release([0, 0, 2])
+    assert m.counts == [0, 1, 0, 0, 0, 0] and m.ctx == [0, 2, 0]
+
+
+def test_model_keeps_counts_true():
+    import random
+
+    rng = random.Random(5)
+    m = PagesModel(6, 8, 30, 4, 30)
+    for _ in range(400):
+        kind = rng.choice(["reserve", "fork", "compact", "release"])
+        if kind == "reserve":
+            m.reserve([rng.choice([0, 1, 5, -1]) for _ in range(6)])
+        elif kind == "fork":
+            m.fork([rng.randrange(-1, 7) for _ in range(2)], rng.sample(range(6), 2))
+        elif kind == "compact":
+            r = rng.randrange(6)
+            m.compact([r], [[t for t in range(m.ctx[r]) if rng.random() < 0.7]])
+        else:
+            m.release([rng.randrange(6)])
+        held = [0] * 30
+        for r in range(6):
+            n = -(-m.ctx[r] // 4)
+            assert all(e >= 0 for e in m.table[r][:n]) and all(e == -1 for e in m.table[r][n:])
+            for e in m.table[r][:n]:
+                held[e] += 1
+        assert held == m.counts
+        for e in range(30):  # a shared page is full in every row
+            if held[e] > 1:
+                for r in range(6):
+                    assert e not in m.table[r][m.ctx[r] // 4:]
