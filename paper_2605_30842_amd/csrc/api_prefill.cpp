@@ -34,7 +34,7 @@ comem_status prepare_prefill(const comem_decode_attn_plan& p, const void* q, con
                              int64_t stride_token, int64_t stride_head, const int32_t* ctx_lens, int32_t batch,
                              int64_t max_ctx_len, float* out, float* lse, const void* workspace,
                              comem::PrefillParams& a) {
-  if (p.cfg.dtype != COMEM_BF16) return COMEM_ERR_UNSUPPORTED;
+  if (p.cfg.dtype == COMEM_F32) return COMEM_ERR_UNSUPPORTED;
   comem_status st = check_bounds(p, batch, max_q_len, max_ctx_len);
   if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
   st = validate_common(p, q, k, v, stride_token, stride_head, ctx_lens, batch, max_ctx_len, out, lse, workspace);
@@ -56,7 +56,8 @@ comem_status prepare_prefill(const comem_decode_attn_plan& p, const void* q, con
   a.num_q_heads = p.cfg.num_q_heads;
   a.group = group_of(p.cfg);
   a.tokens_per_block = comem::kPrefillRows / a.group;
-  a.scale_log2 = p.cfg.scale * 1.4426950408889634f;
+  a.scale_log2 = p.cfg.scale * (is_fp8(p.cfg) ? p.cfg.k_scale : 1.f) * 1.4426950408889634f;
+  a.out_scale = is_fp8(p.cfg) ? p.cfg.v_scale : 1.f;
   a.max_ctx = static_cast<int32_t>(max_ctx_len);
   a.max_q = max_q_len;
   return COMEM_OK;
@@ -146,7 +147,7 @@ comem_status launch_prefill(const comem_decode_attn_plan& p, const comem::Prefil
   args.splits = static_cast<int32_t>(
       plan_splits(p, batch, max_q_len, a.max_ctx, workspace == nullptr ? 0 : workspace_bytes));
   comem::PrefillKernelFn fn =
-      comem::select_prefill_kernel(p.cfg.head_dim, paged ? a.page_mask + 1 : 0, args.splits > 1);
+      comem::select_prefill_kernel(p.cfg.head_dim, paged ? a.page_mask + 1 : 0, args.splits > 1, is_fp8(p.cfg));
   comem::PrefillKernelFn merge = comem::select_prefill_merge_kernel(p.cfg.head_dim);
   if (fn == nullptr || merge == nullptr) return COMEM_ERR_UNSUPPORTED;
   if (args.splits > 1) {
@@ -179,7 +180,7 @@ comem_status comem_prefill_attn_workspace(const comem_decode_attn_plan* plan, in
   if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
   if (workspace_bytes_out == nullptr) return COMEM_ERR_NULL_POINTER;
   *workspace_bytes_out = 0;
-  if (p->cfg.dtype != COMEM_BF16) return COMEM_ERR_UNSUPPORTED;
+  if (p->cfg.dtype == COMEM_F32) return COMEM_ERR_UNSUPPORTED;
   const comem_status st = check_bounds(*p, batch, max_q_len, max_ctx_len);
   if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
   const int64_t items =

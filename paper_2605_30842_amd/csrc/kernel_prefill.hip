@@ -1,4 +1,4 @@
-// Matrix-core prefill attention over a cached prefix, bf16 caches, gfx950.
+// Matrix-core prefill attention over a cached prefix, bf16 and FP8 caches, gfx950.
 //
 // The operation (paper Algorithm 1 and the k-step-off pipeline of Sec. 3.2):
 // sequence b holds L_b cached tokens whose last M_b are new (their keys and
@@ -60,6 +60,11 @@
 // (4 chunks of 4 consecutive rows) and the stores are all free of bank
 // conflicts. Paged caches look their block-table entries up ahead of the
 // requests (scalar loads for pages of 16 rows or more).
+//
+// FP8 caches run the same stages. Codes are exact in bf16 and in f16: K meets
+// Q in bf16, V the probabilities in f16, split into two f16 values (see
+// split_f16). How the codes are widened stands at the V stage; the K scale is
+// part of the score scale, the V scale multiplies the outputs.
 #include "attn_common.h"
 #include "prefill.h"
 
@@ -68,6 +73,9 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -77,11 +85,18 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 constexpr float kLazyMax = 8.f;        // log2 of the largest probability the lazy maximum allows
 constexpr float kLazyMaxProb = 256.f;  // 2^kLazyMax
 
+// FP8 caches: log2 of the factor that probabilities carry, and their bound.
+// With the factor the largest is 2^15, within f16 (see split_f16).
+constexpr float kProbShift = 9.f;
+constexpr float kLazyMaxFp8 = 6.f;
+constexpr float kLazyMaxProbFp8 = 32768.f;  // 2^(kLazyMaxFp8 + kProbShift)
+
 // Chunk swizzle of a row (depends on its low 4 bits only).
-template <int D>
+template <int RB>
 __device__ inline int swizzle(int r) {
-  if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
-  return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  if constexpr (RB == 256) return ((r & 3) << 2) | ((r >> 2) & 3);
+  if constexpr (RB == 128) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  return (r >> 2) & 3;
 }
 
 enum class PLayout { kContig, kPaged, kPagedFine };
@@ -103,9 +118,12 @@ __device__ inline uint32_t lds_address(char* p) {
 // arrive as zeros (checked on the device); a zero V row times a zero weight
 // adds nothing. Small pages (a 16-row group spanning pages) take per-lane
 // addresses, with rows past the needed keys clamped to the last one.
-template <int D, PLayout LAYOUT>
+//
+// WIDEN (V of an FP8 cache): lane l takes 8 codes of a row into registers,
+// which are its 16-byte chunk in f16, to be stored when the slot is free.
+template <int RB, PLayout LAYOUT, bool WIDEN>
 struct TileLoader {
-  static constexpr int CH = D / 8;      // 16-byte chunks per row
+  static constexpr int CH = RB / 16;    // 16-byte chunks per row of RB bytes in LDS
   static constexpr int RPI = 64 / CH;   // rows per wave instruction (1 KiB)
   static constexpr int NI = 16 / RPI;   // instructions per 16-row group
   const char* kbase;  // K of this KV head (contiguous: at the sequence's first row)
@@ -118,6 +136,7 @@ struct TileLoader {
   int kend;  // keys [0, kend) are needed
   int w, lane;
   uint32_t voff[NI];     // lane offset of instruction u within a 16-row group
+  uint32_t loff[NI];     // WIDEN: LDS offset of the lane's chunk within them
 
   __device__ void init(int wave, int ln) {
     w = wave;
@@ -125,7 +144,9 @@ struct TileLoader {
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
       const int r = RPI * u + lane / CH;
-      voff[u] = static_cast<uint32_t>(r * stride_token + 16 * ((lane % CH) ^ swizzle<D>(r)));
+      const int chunk = (lane % CH) ^ swizzle<RB>(r);
+      voff[u] = static_cast<uint32_t>(r * stride_token + (WIDEN ? 8 * (lane % CH) : 16 * chunk));
+      loff[u] = static_cast<uint32_t>(r * RB + 16 * chunk);
     }
   }
 
@@ -204,12 +225,11 @@ struct TileLoader {
   // m0 itself; the s_nop covers the wait state an LDS-bound load needs after
   // an m0 write.
   __device__ void issue(const TileReq& q, uint32_t lds_rows, int u) const {
-    constexpr int RB = D * 2;
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_rows + u * RPI * RB);  // uniform; m0 takes an SGPR
     if constexpr (LAYOUT == PLayout::kPagedFine) {
       const int t = fine_key(q.t0, u);
       const int64_t off = static_cast<int64_t>(q.pg.fine[u]) * stride_page + static_cast<int64_t>(t & page_mask) * stride_token +
-                          16 * ((lane % CH) ^ swizzle<D>(RPI * u + lane / CH));
+                          16 * ((lane % CH) ^ swizzle<RB>(RPI * u + lane / CH));
       asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(q.base + off), "{m0}"(lds) : "memory");
     } else {
       asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff[u]), "s"(q.rsrc), "{m0}"(lds)
@@ -217,8 +237,22 @@ struct TileLoader {
     }
   }
 
+  // WIDEN: the lane's 8 codes of instruction u of a tile request.
+  __device__ u32x2 fetch(const TileReq& q, int u) const {
+    if constexpr (LAYOUT == PLayout::kPagedFine) {
+      const int t = fine_key(q.t0, u);
+      const int64_t off = static_cast<int64_t>(q.pg.fine[u]) * stride_page + static_cast<int64_t>(t & page_mask) * stride_token;
+      return *reinterpret_cast<const u32x2*>(q.base + off + 8 * (lane % CH));
+    } else {
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          reinterpret_cast<void*>(static_cast<uint64_t>(q.rsrc[0]) | static_cast<uint64_t>(q.rsrc[1]) << 32), 0,
+          static_cast<int>(q.rsrc[2]), kBufferConfig);
+      return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, voff[u], 0, 0));
+    }
+  }
+
   // LDS address of this wave's first row in a tile slot.
-  __device__ uint32_t lds_rows(char* slot) const { return lds_address(slot + 16 * w * (D * 2)); }
+  __device__ uint32_t lds_rows(char* slot) const { return lds_address(slot + 16 * w * RB); }
 
 };
 
@@ -235,26 +269,61 @@ __device__ inline void split_truncated(float p0, float p1, uint32_t& hi, uint32_
   lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, bf16x2));
 }
 
+// p0, p1 -> (hi, lo) f16 pairs: hi is the value, lo the exact fp32 remainder,
+// both rounded to nearest. FP8 caches take this form: their codes are exact
+// in f16 as they are in bf16 and the products of f16 cost the same, while the
+// split takes 4 instructions a pair instead of 6 (a remainder is one
+// multiply-add of mixed types) and keeps 22 significant bits instead of 16.
+// f16 ends at 2^-24, so the probabilities are taken 2^9 times as large (the
+// sums carry the factor, the division takes it away): a weight is off by at
+// most 2^-23 of itself, or by 2^-34 of the row's largest weight where that is
+// more, which is for weights below 2^-11 of it.
+__device__ inline void split_f16(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
+  const f32x2 r = {p0 - static_cast<float>(h[0]), p1 - static_cast<float>(h[1])};
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, f16x2));
+}
+
+// 8 E4M3 codes as 8 bf16 (K) or f16 (V) values, exactly.
+template <bool F16>
+__device__ inline u32x4 widen_codes(u32x2 w) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (F16) {
+      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.f, false));
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.f, true));
+    } else {
+      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false));
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, true));
+    }
+  }
+  return r;
+}
+
 // Per-lane LDS offsets, fixed for the whole kernel.
-template <int D>
+template <int D, bool FP8>
 struct LaneOffsets {
-  int k;     // K reads: row j, logical chunk h, with the row's swizzle (XOR 32 ks for step ks)
+  int k;     // K reads: row j, logical chunk h, with the row's swizzle (XOR 32 ks for step ks; FP8: a
+             // chunk of 16 codes serves two steps, XOR 32 kp for the pair kp)
   int v[2];  // V transpose reads, step half c2: key 8 c2 + 4 h + k / 4 of the step, head_dim 4 (k % 4)
              // + 16 (group parity) of n-tile 0 (XOR 64 n for n-tile n)
 };
 
-template <int D>
-__device__ inline LaneOffsets<D> lane_offsets(int lane) {
-  LaneOffsets<D> o;
+template <int D, bool FP8>
+__device__ inline LaneOffsets<D, FP8> lane_offsets(int lane) {
+  constexpr int RB = D * 2, KB = FP8 ? D : D * 2;
+  LaneOffsets<D, FP8> o;
   const int j = lane & 31, h = lane >> 5;
-  o.k = j * (D * 2) + ((h ^ swizzle<D>(j)) << 4);
+  o.k = j * KB + ((h ^ swizzle<KB>(j)) << 4);
   const int k16 = lane & 15, gpar = (lane >> 4) & 1;
   const int hb = 2 * (k16 & 3) * 4;  // byte offset of head_dim 4 (k % 4) within 32 head_dim entries
 #pragma unroll
   for (int c2 = 0; c2 < 2; ++c2) {
     const int r = 8 * c2 + 4 * h + (k16 >> 2);
     const int byte = 32 * gpar + hb;  // within the first 64 bytes (n-tile 0)
-    o.v[c2] = r * (D * 2) + (((byte >> 4) ^ swizzle<D>(r)) << 4) + (byte & 15);
+    o.v[c2] = r * RB + (((byte >> 4) ^ swizzle<RB>(r)) << 4) + (byte & 15);
   }
   return o;
 }
@@ -263,15 +332,16 @@ __device__ inline LaneOffsets<D> lane_offsets(int lane) {
 // (scores of this tile, products of the previous one) and a vector stage
 // (softmax of this tile), so that the two wave groups sharing the SIMDs can
 // run one stage each at the same time.
-template <int D>
+template <int RB>
 struct alignas(16) LdsTile {
-  char b[kPrefillTileKeys * D * 2];
+  char b[kPrefillTileKeys * RB];
 };
 
-// P^T operands of the four 16-key steps of a tile, hi and lo halves.
+// P^T operands of the four 16-key steps of a tile, hi and lo halves (8 bf16;
+// FP8 caches: 8 f16).
 struct PTile {
-  bf16x8 hi[2][2];
-  bf16x8 lo[2][2];
+  u32x4 hi[2][2];
+  u32x4 lo[2][2];
 };
 
 // Schedule N LDS reads and N products of a block so that the reads run A
@@ -292,13 +362,40 @@ __device__ inline void pipeline_reads() {
 constexpr int AHEAD_K = 6, AHEAD_V = 8;
 
 // S^T = K_tile . Q^T for the 32 rows of a wave.
-template <int D>
-__device__ inline void qk_scores(const char* kt, const LaneOffsets<D>& lo, const bf16x8 (&qop)[D / 16],
+template <int D, bool FP8>
+__device__ inline void qk_scores(const char* kt, const LaneOffsets<D, FP8>& lo, const bf16x8 (&qop)[D / 16],
                                  f32x16 (&s)[2]) {
   constexpr int KS = D / 16;
   constexpr int RB = D * 2;
   s[0] = f32x16{};
   s[1] = f32x16{};
+  if constexpr (FP8) {
+    // The reduction index is a dummy: lane half h takes head_dim 32 kp + 16 h
+    // .. + 16 in the steps 2 kp and 2 kp + 1, as its Q operand does.
+#pragma unroll
+    for (int kp = 0; kp < KS / 2; ++kp) {
+      const int off = lo.k ^ (32 * kp);
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) {
+        const u32x4 c = *reinterpret_cast<const u32x4*>(kt + off + 32 * sb * D);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bf16x8 kop = __builtin_bit_cast(bf16x8, widen_codes<false>(u32x2{c[2 * e], c[2 * e + 1]}));
+          s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qop[2 * kp + e], s[sb], 0, 0, 0);
+        }
+      }
+    }
+    // 4 reads ahead of their products; the conversions find their own place
+    // (fixing theirs too made the tile 3% slower).
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < KS - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+    return;
+  }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int off = lo.k ^ (32 * ks);
@@ -316,7 +413,7 @@ __device__ inline void qk_scores(const char* kt, const LaneOffsets<D>& lo, const
 // sum goes to psum. hook(part) runs after each quarter of the exponentials
 // (tile requests placed there, kept there: requests issued back to back
 // stall the wave while the address unit drains them).
-template <typename Hook>
+template <bool FP8, typename Hook>
 __device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2, float& psum, PTile& pt, Hook&& hook) {
 #pragma unroll
   for (int sb = 0; sb < 2; ++sb)
@@ -328,10 +425,14 @@ __device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2
         const float p0 = fast_exp2(__builtin_fmaf(s[sb][8 * s2 + e], scale_log2, -mb));
         const float p1 = fast_exp2(__builtin_fmaf(s[sb][8 * s2 + e + 1], scale_log2, -mb));
         psum += p0 + p1;
-        split_truncated(p0, p1, ph[e >> 1], pl[e >> 1]);
+        if constexpr (FP8) {
+          split_f16(p0, p1, ph[e >> 1], pl[e >> 1]);
+        } else {
+          split_truncated(p0, p1, ph[e >> 1], pl[e >> 1]);
+        }
       }
-      pt.hi[sb][s2] = __builtin_bit_cast(bf16x8, u32x4{ph[0], ph[1], ph[2], ph[3]});
-      pt.lo[sb][s2] = __builtin_bit_cast(bf16x8, u32x4{pl[0], pl[1], pl[2], pl[3]});
+      pt.hi[sb][s2] = u32x4{ph[0], ph[1], ph[2], ph[3]};
+      pt.lo[sb][s2] = u32x4{pl[0], pl[1], pl[2], pl[3]};
       __builtin_amdgcn_sched_barrier(0);
       hook(2 * sb + s2);
       __builtin_amdgcn_sched_barrier(0);
@@ -351,10 +452,11 @@ __device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2
 // says so and takes the probabilities again, the same steps as without the
 // first try. The common case so skips the maximum (32 comparisons, a
 // shuffle and a vote per lane).
-template <int D, typename Hook>
+template <int D, bool FP8, typename Hook>
 __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int limit, int h, float scale_log2,
                                      float& m_run, float& l_run, f32x16 (&acc)[D / 32], PTile& pt, Hook&& hook) {
   constexpr int NT = D / 32;
+  constexpr float shift = FP8 ? kProbShift : 0.f;
   if (masked) {
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb)
@@ -366,8 +468,8 @@ __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int li
   }
   // The first try runs in every wave (its hook issues the tile requests).
   float psum = 0.f;
-  probs_at(s, m_run == -INFINITY ? 0.f : m_run * scale_log2, scale_log2, psum, pt, hook);
-  const bool redo = m_run == -INFINITY || !(psum <= kLazyMaxProb);
+  probs_at<FP8>(s, m_run == -INFINITY ? 0.f : m_run * scale_log2 - shift, scale_log2, psum, pt, hook);
+  const bool redo = m_run == -INFINITY || !(psum <= (FP8 ? kLazyMaxProbFp8 : kLazyMaxProb));
   if (__builtin_amdgcn_ballot_w64(redo) != 0) {
     float mt = -INFINITY;
 #pragma unroll
@@ -375,7 +477,7 @@ __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int li
 #pragma unroll
       for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[sb][r]);
     mt = fmaxf(mt, __shfl_xor(mt, 32));
-    if (__builtin_amdgcn_ballot_w64((mt - m_run) * scale_log2 > kLazyMax) != 0) {
+    if (__builtin_amdgcn_ballot_w64((mt - m_run) * scale_log2 > (FP8 ? kLazyMaxFp8 : kLazyMax)) != 0) {
       const float m_new = fmaxf(m_run, mt);
       float alpha = fast_exp2((m_run - m_new) * scale_log2);
       alpha = m_new == -INFINITY ? 1.f : alpha;
@@ -384,16 +486,23 @@ __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int li
       l_run *= alpha;
       m_run = m_new;
     }
-    const float mb = m_run == -INFINITY ? 0.f : m_run * scale_log2;
+    const float mb = m_run == -INFINITY ? 0.f : m_run * scale_log2 - shift;
     psum = 0.f;
-    probs_at(s, mb, scale_log2, psum, pt, [](int) {});
+    probs_at<FP8>(s, mb, scale_log2, psum, pt, [](int) {});
   }
   l_run += psum;
 }
 
 // O^T += V_tile^T . P^T.
-template <int D>
-__device__ inline void pv_accumulate(const char* vt, const LaneOffsets<D>& lo, const PTile& pt, f32x16 (&acc)[D / 32]) {
+template <bool FP8>
+__device__ inline f32x16 pv_product(bf16x8 v, u32x4 p, f32x16 acc) {
+  if constexpr (FP8)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, p), acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p), acc, 0, 0, 0);
+}
+
+template <int D, bool FP8>
+__device__ inline void pv_accumulate(const char* vt, const LaneOffsets<D, FP8>& lo, const PTile& pt, f32x16 (&acc)[D / 32]) {
   constexpr int NT = D / 32;
   constexpr int RB = D * 2;
 #pragma unroll
@@ -406,8 +515,8 @@ __device__ inline void pv_accumulate(const char* vt, const LaneOffsets<D>& lo, c
         const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vt + step + (lo.v[0] ^ (64 * n))));
         const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vt + step + (lo.v[1] ^ (64 * n))));
         const bf16x8 vop = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, pt.hi[sb][s2], acc[n], 0, 0, 0);
-        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, pt.lo[sb][s2], acc[n], 0, 0, 0);
+        acc[n] = pv_product<FP8>(vop, pt.hi[sb][s2], acc[n]);
+        acc[n] = pv_product<FP8>(vop, pt.lo[sb][s2], acc[n]);
       }
     }
   pipeline_reads<8 * NT, AHEAD_V>();
@@ -422,6 +531,13 @@ template <int N>
 __device__ inline void wait_vm() {
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(N));
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Wait until this wave's LDS accesses are done.
+__device__ inline void wait_lds() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), the other counters left alone
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -455,11 +571,14 @@ constexpr int kXcds = 8;  // XCDs of the GPU; workgroups are dealt to them round
 // SPLIT: the workgroup takes one of p.splits equal shares of the block's keys
 // and leaves a partial result. A form of its own, since the extra scalars
 // spill and cost an unsplit call 0.6%.
-template <int D, PLayout LAYOUT, bool SPLIT>
+template <int D, PLayout LAYOUT, bool SPLIT, bool FP8>
 __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const PrefillParams p) {
   constexpr int KS = D / 16;
   constexpr int NT = D / 32;
   constexpr bool PAGED = LAYOUT != PLayout::kContig;
+  constexpr int KB = FP8 ? D : D * 2;  // bytes of a K row in LDS
+  using KLoader = TileLoader<KB, LAYOUT, false>;
+  using Loader = TileLoader<D * 2, LAYOUT, FP8>;
   // Work item of the workgroup. Workgroups go to the XCDs in turn (linear
   // id modulo 8). When the (sequence, KV head) pairs divide evenly over the
   // XCDs, pair hb runs all its query blocks on XCD hb % 8, so the K/V tiles
@@ -521,26 +640,31 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   const int qh = hk * p.group + g;
   const int limit = prefix + ic;
 
-  TileLoader<D, LAYOUT> ld;
-  ld.kbase = p.k + hk * p.stride_head + seq0 * p.stride_token;
-  ld.vbase = p.v + hk * p.stride_head + seq0 * p.stride_token;
-  ld.bt_row = PAGED ? p.block_table + static_cast<int64_t>(b) * p.max_pages : nullptr;
-  ld.stride_token = p.stride_token;
-  ld.stride_page = p.stride_page;
-  ld.num_pages = p.num_pages;
-  ld.page_shift = p.page_shift;
-  ld.page_mask = p.page_mask;
-  ld.kend = kend;
-  ld.init(w, lane);
+  auto set_up = [&](auto& l) {
+    l.kbase = p.k + hk * p.stride_head + seq0 * p.stride_token;
+    l.vbase = p.v + hk * p.stride_head + seq0 * p.stride_token;
+    l.bt_row = PAGED ? p.block_table + static_cast<int64_t>(b) * p.max_pages : nullptr;
+    l.stride_token = p.stride_token;
+    l.stride_page = p.stride_page;
+    l.num_pages = p.num_pages;
+    l.page_shift = p.page_shift;
+    l.page_mask = p.page_mask;
+    l.kend = kend;
+    l.init(w, lane);
+  };
+  Loader ld;
+  set_up(ld);
+  KLoader kl;  // bf16 caches: the same as ld
+  set_up(kl);
 
   // Q^T operand: row j, head_dim 16 ks + 8 h .. + 8 (requested after the first tile).
   bf16x8 qop[KS];
   auto load_q = [&]() {
     const char* qrow = p.q + ((qs + ic) * p.num_q_heads + qh) * (D * 2);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qop[ks] = *reinterpret_cast<const bf16x8*>(qrow + 32 * ks + 16 * h);
+    for (int ks = 0; ks < KS; ++ks) qop[ks] = *reinterpret_cast<const bf16x8*>(qrow + (FP8 ? 64 * (ks >> 1) + 32 * h + 16 * (ks & 1) : 32 * ks + 16 * h));
   };
-  const LaneOffsets<D> lo = lane_offsets<D>(lane);
+  const LaneOffsets<D, FP8> lo = lane_offsets<D, FP8>(lane);
   f32x16 acc[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = f32x16{};
@@ -559,20 +683,54 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   // barriers, with stages past their own tiles left empty.
   // Slots: K of tile i in ks[i % 2], V of tile i in vs[i % 2], one entry
   // per half.
-  __shared__ LdsTile<D> ks0[2], ks1[2], vs0[2], vs1[2];
-  using Pages = typename TileLoader<D, LAYOUT>::Pages;
+  __shared__ LdsTile<KB> ks0[2], ks1[2];
+  __shared__ LdsTile<D * 2> vs0[2], vs1[2];
+  using Pages = typename Loader::Pages;
   const int steps = (ntiles + 1) / 2;
   const int t_first = first_tile + kh * steps;
   const int t_count = max(0, min(steps, ntiles - kh * steps));
   constexpr int TK = kPrefillTileKeys;
-  LdsTile<D>& k0 = ks0[kh];
-  LdsTile<D>& k1 = ks1[kh];
-  LdsTile<D>& v0 = vs0[kh];
-  LdsTile<D>& v1 = vs1[kh];
-  constexpr int NI = TileLoader<D, LAYOUT>::NI;
-  const uint32_t lk0 = ld.lds_rows(k0.b), lk1 = ld.lds_rows(k1.b), lv0 = ld.lds_rows(v0.b), lv1 = ld.lds_rows(v1.b);
+  LdsTile<KB>& k0 = ks0[kh];
+  LdsTile<KB>& k1 = ks1[kh];
+  LdsTile<D * 2>& v0 = vs0[kh];
+  LdsTile<D * 2>& v1 = vs1[kh];
+  constexpr int NI = Loader::NI;
+  const uint32_t lk0 = kl.lds_rows(k0.b), lk1 = kl.lds_rows(k1.b), lv0 = ld.lds_rows(v0.b), lv1 = ld.lds_rows(v1.b);
   Pages pg_v, pg_k;  // page lookups of the next V and the next K tile to request
-  {
+  // FP8: V's codes on their way, one tile ahead of the slots' contents.
+  u32x2 rv[NI];
+  auto put_v = [&](char* slot, int u) {
+    *reinterpret_cast<u32x4*>(slot + 16 * w * (D * 2) + ld.loff[u]) = widen_codes<true>(rv[u]);
+  };
+  using KPages = typename KLoader::Pages;
+  KPages kpg;  // FP8: K's lookup of the tile that pg_v is for (the same page, but for small ones)
+  auto k_pages = [&](int t0) {
+    if constexpr (LAYOUT == PLayout::kPagedFine) return kl.pages_of(t0);
+    KPages pg{};
+    pg.page = pg_v.page;
+    return pg;
+  };
+  if constexpr (FP8) {
+    const auto vq0 = ld.tile_req(ld.vbase, TK * t_first, ld.pages_of(TK * t_first));
+    const auto kq0 = kl.tile_req(kl.kbase, TK * t_first, kl.pages_of(TK * t_first));
+    const auto vq1 = ld.tile_req(ld.vbase, TK * (t_first + 1), ld.pages_of(TK * (t_first + 1)));
+    const auto kq1 = kl.tile_req(kl.kbase, TK * (t_first + 1), kl.pages_of(TK * (t_first + 1)));
+#pragma unroll
+    for (int u = 0; u < NI; ++u) rv[u] = ld.fetch(vq0, u);
+    load_q();
+#pragma unroll
+    for (int u = 0; u < NI; ++u) put_v(v0.b, u);
+#pragma unroll
+    for (int u = 0; u < NI; ++u) rv[u] = ld.fetch(vq1, u);
+#pragma unroll
+    for (int u = 0; u < KLoader::NI; ++u) {
+      kl.issue(kq0, lk0, u);
+      kl.issue(kq1, lk1, u);
+    }
+    pg_v = ld.pages_of(TK * (t_first + 2));
+    kpg = k_pages(TK * (t_first + 2));
+    wait_vm<0>();
+  } else {
     const Pages pg0 = ld.pages_of(TK * t_first);
     const Pages pg1 = ld.pages_of(TK * (t_first + 1));
     const auto rk0 = ld.tile_req(ld.kbase, TK * t_first, pg0);
@@ -586,24 +744,57 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     }
     pg_v = pg1;
     pg_k = ld.pages_of(TK * (t_first + 2));
+    load_q();
+    wait_vm<0>();
   }
-  load_q();
-  wait_vm<0>();
   __syncthreads();
 
   f32x16 s[2];  // scores of a tile between its M and V stages
   PTile pt;     // probabilities of a tile between its V stage and the next M stage
-  auto m_stage = [&](const LdsTile<D>& kcur, const LdsTile<D>& vprev, int c) {
-    if (c >= 1 && c <= t_count) pv_accumulate<D>(vprev.b, lo, pt, acc);
-    if (c < t_count) qk_scores<D>(kcur.b, lo, qop, s);
+  auto m_stage = [&](const LdsTile<KB>& kcur, const LdsTile<D * 2>& vprev, int c) {
+    if (c >= 1 && c <= t_count) pv_accumulate<D, FP8>(vprev.b, lo, pt, acc);
+    if (c < t_count) qk_scores<D, FP8>(kcur.b, lo, qop, s);
+    if constexpr (FP8) wait_lds();  // the next stage stores into what this one read
   };
   // Every V stage requests two tiles (past the half's range they are
   // unused; rows past the keys arrive as zeros), so the wait at its end
   // leaves only its own requests in flight: those of the previous V stage,
   // read in the next M stage, have landed. Both target slots were last read
   // in the M stage just before.
-  constexpr int kStageLoads = 2 * TileLoader<D, LAYOUT>::NI;
-  auto v_stage = [&](uint32_t kslot, uint32_t vslot, int c) {
+  //
+  // FP8: K's codes go straight into their slot, two tiles ahead, and are
+  // widened by every wave that reads them, in the M stage, which has vector
+  // instructions to spare. V's go through registers: those of tile i + 1 were
+  // requested a V stage earlier and are widened here, each wave its quarter,
+  // between the parts of the exponentials, and stored where the M stage's
+  // transpose reads find them; those of tile i + 2 are requested in their
+  // place. (Measured in us, 1024 tokens over 33792 / 8192 uncached / eight
+  // sequences in pages of 16: both widened in the M stage 709 / 734 / 4110,
+  // both in the V stage 693 / 720 / 4070, this 681 / 706 / 4000; a bf16
+  // cache 651 / 678 / 3770.)
+  constexpr int kStageLoads = 2 * NI;
+  auto v_stage = [&](uint32_t kslot, uint32_t vslot, LdsTile<D * 2>& vst, int c) {
+    if constexpr (FP8) {
+      if (c < t_count) {
+        const int t = t_first + c;
+        const auto vq = ld.tile_req(ld.vbase, TK * (t + 2), pg_v);
+        const auto kq = kl.tile_req(kl.kbase, TK * (t + 2), kpg);
+        pg_v = ld.pages_of(TK * (t + 3));
+        kpg = k_pages(TK * (t + 3));
+        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
+#pragma unroll
+          for (int u = part * NI / 4; u < (part + 1) * NI / 4; ++u) {
+            put_v(vst.b, u);
+            rv[u] = ld.fetch(vq, u);
+          }
+#pragma unroll
+          for (int u = part * KLoader::NI / 4; u < (part + 1) * KLoader::NI / 4; ++u) kl.issue(kq, kslot, u);
+        });
+        wait_lds();
+        wait_vm<NI + KLoader::NI>();  // this stage's requests stay in flight
+      }
+      return;
+    }
     if (c < t_count) {
       const int t = t_first + c;
       const auto rv = ld.tile_req(ld.vbase, TK * (t + 1), pg_v);
@@ -617,10 +808,10 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
           ld.issue(rv, vslot, u);
           ld.issue(rk, kslot, u);
         }
-        softmax_probs<D>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [](int) {});
+        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [](int) {});
       } else {
         // Instructions spread over the four parts of the exponentials.
-        softmax_probs<D>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
+        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
 #pragma unroll
           for (int u = part * NI / 4; u < (part + 1) * NI / 4; ++u) {
             ld.issue(rv, vslot, u);
@@ -636,12 +827,12 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     m_stage(k0, v1, c);
     stage_barrier();
     if (c < steps) {
-      v_stage(lk0, lv1, c);
+      v_stage(lk0, lv1, v1, c);
       stage_barrier();
       m_stage(k1, v0, c + 1);
       stage_barrier();
       if (c + 1 < steps) {
-        v_stage(lk1, lv0, c + 1);
+        v_stage(lk1, lv0, v0, c + 1);
         stage_barrier();
       }
     }
@@ -650,8 +841,8 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   l_run += __shfl_xor(l_run, 32);
   // Half 1 leaves its state in LDS, once the last requests (unused tiles)
   // have landed; half 0 merges it into its own, waves 0-1 then waves 2-3
-  // (each wave's accumulators take one 16 KB slot; lane-interleaved 16-byte
-  // stores and loads, free of bank conflicts).
+  // (each wave's accumulators take one 16 KB slot, of V where K's are half as
+  // large; lane-interleaved 16-byte stores and loads, free of bank conflicts).
   wait_vm<0>();
   __syncthreads();
   float* ml = reinterpret_cast<float*>(vs0[0].b);  // m then l, [w][64 lanes] each
@@ -660,7 +851,7 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     ml[256 + w * 64 + lane] = l_run;
   }
   for (int pass = 0; pass < 2; ++pass) {
-    float4* st = reinterpret_cast<float4*>(ks0[w & 1].b);  // [4 NT][64 lanes]
+    float4* st = reinterpret_cast<float4*>(FP8 ? vs1[w & 1].b : ks0[w & 1].b);  // [4 NT][64 lanes]
     if (kh == 1 && (w >> 1) == pass) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -694,7 +885,8 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   }
   if (kh == 1) return;
   if (i >= M) return;
-  float inv = 1.f / l_run;
+  float inv = (FP8 ? p.out_scale : 1.f) / l_run;
+  const float lse2 = m_run * p.scale_log2 + log2f(l_run) - (FP8 ? kProbShift : 0.f);
   const int64_t orow = (qs + i) * p.num_q_heads + qh;
   float* o = p.out + orow * D;
   if constexpr (SPLIT) {
@@ -704,7 +896,7 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     const int64_t part = prefill_part(p, b, hk, q, split) + row;
     o = p.o_part + part * D;
     if (l_run == 0.f) inv = 0.f;
-    if (h == 0) p.lse_part[part] = l_run == 0.f ? -INFINITY : m_run * p.scale_log2 + log2f(l_run);
+    if (h == 0) p.lse_part[part] = l_run == 0.f ? -INFINITY : lse2;
   }
   // acc[n] register r holds head_dim 32 n + 8 (r / 4) + 4 h + r % 4.
 #pragma unroll
@@ -714,7 +906,7 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
       *reinterpret_cast<float4*>(o + 32 * n + 8 * r4 + 4 * h) =
           make_float4(acc[n][4 * r4] * inv, acc[n][4 * r4 + 1] * inv, acc[n][4 * r4 + 2] * inv,
                       acc[n][4 * r4 + 3] * inv);
-  if (h == 0 && p.lse != nullptr && !SPLIT) p.lse[orow] = (m_run * p.scale_log2 + log2f(l_run)) * kLn2;
+  if (h == 0 && p.lse != nullptr && !SPLIT) p.lse[orow] = lse2 * kLn2;
 }
 
 // Merge of a split call's partial results. A lane takes 4 head_dim entries
@@ -782,9 +974,11 @@ __global__ __launch_bounds__(kPrefillMergeThreads) void prefill_merge_kernel(con
 
 // Every form the host may launch, instantiated explicitly (clang emitted the
 // host launch stubs of only some of the instantiations referenced below).
-#define COMEM_PREFILL_FORMS(D, L)                                                              \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, false>(const PrefillParams); \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, true>(const PrefillParams);
+#define COMEM_PREFILL_FORMS(D, L)                                                                 \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, false>(const PrefillParams); \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, false>(const PrefillParams);  \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, true>(const PrefillParams);  \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, true>(const PrefillParams);
 COMEM_PREFILL_FORMS(128, kContig)
 COMEM_PREFILL_FORMS(128, kPaged)
 COMEM_PREFILL_FORMS(128, kPagedFine)
@@ -797,14 +991,14 @@ template __global__ void prefill_merge_kernel<64>(const PrefillParams);
 
 }  // namespace
 
-template <int D, bool SPLIT>
+template <int D, bool SPLIT, bool FP8>
 PrefillKernelFn prefill_by_layout(int page_size) {
   // page_size 0: contiguous cache. A paged cache takes the per-group path when
   // a wave's 16-row group of a tile fits in a page (it starts at a multiple of
   // 16 for either head_dim).
-  PrefillKernelFn fn = prefill_mfma_kernel<D, PLayout::kPagedFine, SPLIT>;
-  if (page_size == 0) fn = prefill_mfma_kernel<D, PLayout::kContig, SPLIT>;
-  else if (page_size >= 16) fn = prefill_mfma_kernel<D, PLayout::kPaged, SPLIT>;
+  PrefillKernelFn fn = prefill_mfma_kernel<D, PLayout::kPagedFine, SPLIT, FP8>;
+  if (page_size == 0) fn = prefill_mfma_kernel<D, PLayout::kContig, SPLIT, FP8>;
+  else if (page_size >= 16) fn = prefill_mfma_kernel<D, PLayout::kPaged, SPLIT, FP8>;
   return fn;
 }
 
@@ -812,9 +1006,15 @@ PrefillKernelFn select_prefill_merge_kernel(int head_dim) {
   return head_dim == 128 ? prefill_merge_kernel<128> : (head_dim == 64 ? prefill_merge_kernel<64> : nullptr);
 }
 
-PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split) {
-  if (head_dim == 128) return split ? prefill_by_layout<128, true>(page_size) : prefill_by_layout<128, false>(page_size);
-  if (head_dim == 64) return split ? prefill_by_layout<64, true>(page_size) : prefill_by_layout<64, false>(page_size);
+template <int D>
+PrefillKernelFn prefill_by_cache(int page_size, bool split, bool fp8) {
+  if (fp8) return split ? prefill_by_layout<D, true, true>(page_size) : prefill_by_layout<D, false, true>(page_size);
+  return split ? prefill_by_layout<D, true, false>(page_size) : prefill_by_layout<D, false, false>(page_size);
+}
+
+PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8) {
+  if (head_dim == 128) return prefill_by_cache<128>(page_size, split, fp8);
+  if (head_dim == 64) return prefill_by_cache<64>(page_size, split, fp8);
   return nullptr;
 }
 

@@ -13,7 +13,7 @@ constexpr int kPrefillTileKeys = 64;  // keys per K/V tile staged in LDS
 // Offsets and strides are in bytes.
 struct PrefillParams {
   const char* q;               // [total_q, Hq, D] bf16, sequence b's new tokens from row q_start[b]
-  const char* k;               // contiguous: [T, Hkv, D] rows; paged: page pool
+  const char* k;               // bf16 or E4M3 codes; contiguous: [T, Hkv, D] rows; paged: page pool
   const char* v;
   float* out;                  // [total_q, Hq, D]
   float* lse;                  // [total_q, Hq] or nullptr
@@ -31,7 +31,8 @@ struct PrefillParams {
   int32_t num_q_heads;
   int32_t group;               // G = Hq / Hkv
   int32_t tokens_per_block;    // kPrefillRows / G new tokens per workgroup
-  float scale_log2;            // scale * log2(e)
+  float scale_log2;            // scale * log2(e), times the K scale of an FP8 cache
+  float out_scale;             // FP8 caches: multiplies every output (the V scale)
   int32_t max_ctx;             // ctx_lens[b] is clamped to [0, max_ctx]
   int32_t max_q;               // q_lens[b] is clamped to [0, min(L_b, max_q)]
   int64_t num_pages;           // paged layout: entries outside [0, num_pages) read page 0
@@ -43,7 +44,7 @@ struct PrefillParams {
 
 using PrefillKernelFn = void (*)(PrefillParams);
 // page_size 0 selects the contiguous-cache kernel.
-PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split);
+PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8);
 
 constexpr int kPrefillMergeThreads = 256;
 constexpr int kPrefillMergeRows = 16;  // rows per workgroup of the merge kernel

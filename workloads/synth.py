@@ -383,7 +383,7 @@ def generate_prefill(spec: PrefillSpec, seed: Optional[int] = None, **kv_kw) -> 
     q_start[1:] = np.cumsum(m.astype(np.int64))[:-1]
     total = int(m.astype(np.int64).sum())
     s = spec.kv
-    q = _draw_tensor(q_ss, (max(total, 1), s.num_q_heads, s.head_dim), s.dtype)[:total]
+    q = _draw_tensor(q_ss, (max(total, 1), s.num_q_heads, s.head_dim), s.q_dtype)[:total]
     return PrefillWorkload(spec, kv, q, q_start, m)
 
 
