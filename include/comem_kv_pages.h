@@ -15,7 +15,7 @@
  * one sequence each, ctx_lens[r] tokens long, and refcounts[p], the number of
  * table entries that hold page p. A page with count 0 is free. The entries
  * i < ceil(ctx_lens[r] / page_size) of row r hold pages, the others nothing
- * (-1 by custom; they are not read). To begin with: zero refcounts and
+ * (-1 by custom; what they say plays no part). To begin with: zero refcounts and
  * ctx_lens. A caller that keeps a page for itself sets its count to 1.
  *
  * A page that several rows hold is full in all of them: forks share whole

@@ -901,61 +901,83 @@ class DecodeAttention:
 
     def _check_part(self, name, t, heads, rows):
         """A projection's part: [rows, heads, d], a token's heads side by side."""
-        import torch
-
-        if (isinstance(t, torch.Tensor) and t.dtype in self._q_dtypes and t.device == self._torch_device
-                and t.shape == (rows, heads, self.head_dim) and t.stride()[1:] == (self.head_dim, 1)):
-            return
         _check_tensor(name, t, self._q_dtypes, self._torch_device, shape=(rows, heads, self.head_dim),
                       contiguous=False)
         _need((t.stride(1) == self.head_dim or heads == 1 or rows == 0) and t.stride(2) == 1,
               f"{name} must hold each token's heads side by side")
 
-    @staticmethod
-    def _row_stride(t, rows):
-        """Elements from a row to the next (of a single row torch may report any)."""
-        return t.stride(0) if rows > 1 else t.shape[1] * t.shape[2]
+    def _check_rope(self, q, new_k, new_v, ctx_lens, cos_sin, q_weight, k_weight, q_start, q_lens, positions, q_out):
+        """Every tensor of a rope call but the cache's (where the common case did not hold in one expression)."""
+        import torch
+
+        dev, i32 = self._torch_device, (torch.int32,)
+        _need(isinstance(q, torch.Tensor) and q.dim() == 3, "q must be a torch tensor [rows, heads, head_dim]")
+        rows = q.shape[0]
+        self._check_part("q", q, self.num_q_heads, rows)
+        self._check_part("new_k", new_k, self.num_kv_heads, rows)
+        self._check_part("new_v", new_v, self.num_kv_heads, rows)
+        _check_tensor("cos_sin", cos_sin, (torch.float32,), dev, ndim=2)
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                _check_tensor(name, w, (q.dtype,), dev, shape=(self.head_dim,))
+        _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
+        _check_tensor("ctx_lens", ctx_lens, i32, dev, ndim=1)
+        if q_lens is not None:
+            _check_tensor("q_start", q_start, (torch.int64,), dev, shape=ctx_lens.shape)
+            _check_tensor("q_lens", q_lens, i32, dev, shape=ctx_lens.shape)
+        if positions is not None:
+            _check_tensor("positions", positions, i32, dev, shape=(rows,))
+        if q_out is not None:
+            _check_tensor("q_out", q_out, (q.dtype,), dev, shape=(rows, self.num_q_heads, self.head_dim))
 
     def _rope_args(self, q, new_k, new_v, ctx_lens, max_ctx_len, cos_sin, q_weight, k_weight, eps, q_start, q_lens,
                    max_q_len, positions, interleaved, q_out, stream):
         import torch
 
-        tensor, dev, i32 = torch.Tensor, self._torch_device, (torch.int32,)
-        _need(isinstance(q, tensor) and q.dim() == 3, "q must be a torch tensor [rows, heads, head_dim]")
-        rows = q.shape[0]
-        self._check_part("q", q, self.num_q_heads, rows)
-        self._check_part("new_k", new_k, self.num_kv_heads, rows)
-        self._check_part("new_v", new_v, self.num_kv_heads, rows)
-        if not (isinstance(cos_sin, tensor) and cos_sin.dtype == torch.float32 and cos_sin.device == dev
-                and cos_sin.dim() == 2 and cos_sin.is_contiguous()):
-            _check_tensor("cos_sin", cos_sin, (torch.float32,), dev, ndim=2)
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None and not _fits(w, tensor, (q.dtype,), dev, (self.head_dim,)):
-                _check_tensor(name, w, (q.dtype,), dev, shape=(self.head_dim,))
-        _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
-        batch = rows if q_lens is None else (ctx_lens.shape[0] if isinstance(ctx_lens, tensor) and ctx_lens.dim() == 1
-                                             else -1)
-        if q_lens is not None:
-            if not (_fits(q_lens, tensor, i32, dev, (batch,)) and _fits(q_start, tensor, (torch.int64,), dev, (batch,))):
-                _check_tensor("ctx_lens", ctx_lens, i32, dev, ndim=1)
-                _check_tensor("q_start", q_start, (torch.int64,), dev, shape=(batch,))
-                _check_tensor("q_lens", q_lens, i32, dev, shape=(batch,))
-        if positions is not None and not _fits(positions, tensor, i32, dev, (rows,)):
-            _check_tensor("positions", positions, i32, dev, shape=(rows,))
+        tensor, dev, d = torch.Tensor, self._torch_device, self.head_dim
+        at = dev.index if dev.type == "cuda" else -1
+        # The call of a decode step in one expression; everything else, and what is wrong, in _check_rope.
+        fast, rows_stride = False, None
+        if (q_lens is None and q_start is None and isinstance(q, tensor) and isinstance(new_k, tensor)
+                and isinstance(new_v, tensor) and isinstance(cos_sin, tensor)):
+            shape, strides = q.shape, (q.stride(), new_k.stride(), new_v.stride())
+            dtype, inner = q.dtype, (d, 1)
+            fast = (len(shape) == 3 and shape[1] == self.num_q_heads and shape[2] == d and dtype in self._q_dtypes
+                    and new_k.shape == (shape[0], self.num_kv_heads, d) and new_k.shape == new_v.shape
+                    and strides[0][1:] == inner and strides[1][1:] == inner and strides[2][1:] == inner
+                    and new_k.dtype is dtype and new_v.dtype is dtype and cos_sin.dtype is torch.float32
+                    and q.get_device() == at and new_k.get_device() == at and new_v.get_device() == at
+                    and cos_sin.get_device() == at and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+                    and (q_weight is None or (isinstance(q_weight, tensor) and q_weight.dtype is dtype
+                                              and q_weight.get_device() == at and q_weight.shape == (d,)
+                                              and q_weight.is_contiguous()))
+                    and (k_weight is None or (isinstance(k_weight, tensor) and k_weight.dtype is dtype
+                                              and k_weight.get_device() == at and k_weight.shape == (d,)
+                                              and k_weight.is_contiguous()))
+                    and (positions is None or _fits(positions, tensor, (torch.int32,), dev, shape[:1]))
+                    and (q_out is None or _fits(q_out, tensor, (dtype,), dev, shape)))
+            rows_stride = strides[0][:1] + strides[1][:1] + strides[2][:1]
+        if not fast:
+            self._check_rope(q, new_k, new_v, ctx_lens, cos_sin, q_weight, k_weight, q_start, q_lens, positions, q_out)
         self._check_bound(max_q_len, "max_q_len")
         self._check_bound(max_ctx_len)
+        rows = q.shape[0]
         if q_out is None:
-            q_out = _empty_on(self, stream, (rows, self.num_q_heads, self.head_dim), q.dtype)
-        elif not _fits(q_out, tensor, (q.dtype,), dev, (rows, self.num_q_heads, self.head_dim)):
-            _check_tensor("q_out", q_out, (q.dtype,), dev, shape=(rows, self.num_q_heads, self.head_dim))
+            if stream is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            else:
+                q_out = _empty_on(self, stream, q.shape, q.dtype)
         rope = RopeConfig(None if q_weight is None else q_weight.data_ptr(),
                           None if k_weight is None else k_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0],
                           cos_sin.shape[1], eps, ROPE_INTERLEAVED if interleaved else 0)
-        head = (self.plan, rope, q.data_ptr(), self._row_stride(q, rows), new_k.data_ptr(),
-                self._row_stride(new_k, rows), new_v.data_ptr(), self._row_stride(new_v, rows),
+        if rows <= 1:  # torch may report any stride from a single row to the next
+            step = (self.num_q_heads * d, self.num_kv_heads * d, self.num_kv_heads * d)
+        else:
+            step = rows_stride or (q.stride(0), new_k.stride(0), new_v.stride(0))
+        head = (self.plan, rope, q.data_ptr(), step[0], new_k.data_ptr(), step[1], new_v.data_ptr(), step[2],
                 None if q_start is None else q_start.data_ptr(), None if q_lens is None else q_lens.data_ptr(),
                 int(max_q_len), None if positions is None else positions.data_ptr(), q_out.data_ptr())
-        return batch, q_out, head
+        return rows if q_lens is None else ctx_lens.shape[0], q_out, head
 
     def rope_append(self, q, new_k, new_v, k, v, seq_start, ctx_lens, max_ctx_len: int, cos_sin, q_weight=None,
                     k_weight=None, eps: float = 1e-6, q_start=None, q_lens=None, max_q_len: int = 1, positions=None,
@@ -982,9 +1004,10 @@ class DecodeAttention:
                                              q_start, q_lens, max_q_len, positions, interleaved, q_out, stream)
         self._check_cache(k_pages, v_pages, paged=True)
         self._check_lengths(ctx_lens, batch, block_table=block_table)
-        _call_on(self, stream, comem_rope_append_paged, *head, k_pages.data_ptr(), v_pages.data_ptr(),
-                 k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), k_pages.shape[1], k_pages.shape[0],
-                 block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len))
+        pool, strides = k_pages.shape, k_pages.stride()
+        _call_on(self, stream, comem_rope_append_paged, *head, k_pages.data_ptr(), v_pages.data_ptr(), strides[0],
+                 strides[1], strides[2], pool[1], pool[0], block_table.data_ptr(), block_table.shape[1],
+                 ctx_lens.data_ptr(), batch, int(max_ctx_len))
         return q_out
 
 
@@ -1028,14 +1051,19 @@ class KVPages:
                                  block_table.shape[1], self.max_ctx_len)
         self.workspace_bytes = comem_kv_pages_workspace(op.plan, self._state)
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self._workspace = self.workspace.data_ptr()
+        self._rows = ctx_lens.shape
+        self._at = dev.index if dev.type == "cuda" else -1
 
     def _list(self, name, t, dtype=None, shape=None):
+        """The address of a dense list on the plan's device: int32, or dtype; of the given shape, or of any length."""
         import torch
 
-        dtypes = (dtype or torch.int32,)
-        if not (isinstance(t, torch.Tensor) and t.dim() == 1 and _fits(t, torch.Tensor, dtypes, self.op._torch_device,
-                                                                      t.shape if shape is None else shape)):
-            _check_tensor(name, t, dtypes, self.op._torch_device, shape=(None,) if shape is None else shape)
+        if dtype is None:
+            dtype = torch.int32
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self._at
+                and (t.dim() == 1 if shape is None else t.shape == shape) and t.is_contiguous()):
+            _check_tensor(name, t, (dtype,), self.op._torch_device, shape=(None,) if shape is None else shape)
         return t.data_ptr()
 
     def _missing(self, missing, stream):
@@ -1049,10 +1077,10 @@ class KVPages:
 
     def reserve(self, add_lens, missing=None, stream=None):
         """Room for add_lens[r] (int32 [R]) more tokens in every row: pages where they are needed, ctx_lens grown."""
-        add = self._list("add_lens", add_lens, shape=(self.block_table.shape[0],))
+        add = self._list("add_lens", add_lens, shape=self._rows)
         missing = self._missing(missing, stream)
         _call_on(self.op, stream, comem_kv_reserve, self.op.plan, self._state, add, missing.data_ptr(),
-                 self.workspace.data_ptr(), self.workspace_bytes)
+                 self._workspace, self.workspace_bytes)
         return missing
 
     def fork(self, parents, children, missing=None, stream=None):
@@ -1063,7 +1091,7 @@ class KVPages:
         if parents.shape[0] == 0:
             return missing.zero_() if stream is None else self._zeroed(missing, stream)
         _call_on(self.op, stream, comem_kv_fork, self.op.plan, self._state, src, dst, parents.shape[0],
-                 missing.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes)
+                 missing.data_ptr(), self._workspace, self.workspace_bytes)
         return missing
 
     def compact(self, rows, keep, keep_start, keep_lens, missing=None, stream=None):
@@ -1079,7 +1107,7 @@ class KVPages:
         if rows.shape[0] == 0:
             return missing.zero_() if stream is None else self._zeroed(missing, stream)
         _call_on(self.op, stream, comem_kv_compact, self.op.plan, self._state, at, which, keep.shape[0], start, count,
-                 rows.shape[0], missing.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes)
+                 rows.shape[0], missing.data_ptr(), self._workspace, self.workspace_bytes)
         return missing
 
     def release(self, rows, stream=None) -> None:

@@ -49,16 +49,22 @@ comem_status check_pools(const comem_decode_attn_plan& p, const comem_kv_pages& 
   return COMEM_OK;
 }
 
-// Bytes of the workspace's parts: items, the fresh pages, the old entries.
+int32_t chunks_of(const comem_kv_pages& s) {
+  return static_cast<int32_t>(ceil_div(s.num_pages, comem::kChunkPages));
+}
+
+// Bytes of the workspace's parts: items, the chunks' free pages, the fresh
+// pages, the old entries.
 struct Layout {
-  size_t item, fresh, old;
-  size_t total() const { return 256 + 7 * item + fresh + old; }
+  size_t item, chunks, fresh, old;
+  size_t total() const { return 256 + 7 * item + chunks + fresh + old; }
 };
 
 Layout layout_of(const comem_kv_pages& s) {
   const int64_t entries = static_cast<int64_t>(s.num_rows) * s.max_pages_per_seq;
   Layout l;
   l.item = align256(static_cast<size_t>(s.num_rows) * 4);
+  l.chunks = align256(static_cast<size_t>(chunks_of(s)) * 4);
   l.fresh = align256(static_cast<size_t>(std::min(s.num_pages, entries)) * 4);
   l.old = align256(static_cast<size_t>(entries) * 4);
   return l;
@@ -77,6 +83,7 @@ comem::PageParams params_of(const comem_decode_attn_plan& p, const comem_kv_page
   a.max_pages = s.max_pages_per_seq;
   a.page_shift = log2_of(s.page_size);
   a.n = n;
+  a.chunks = chunks_of(s);
   a.num_kv_heads = p.cfg.num_kv_heads;
   a.piece_shift = log2_of(static_cast<int32_t>(p.cfg.head_dim * e / 16));
   return a;
@@ -109,6 +116,8 @@ void set_workspace(const comem_kv_pages& s, void* workspace, comem::PageParams& 
     *item = reinterpret_cast<int32_t*>(at);
     at += l.item;
   }
+  a.free_counts = reinterpret_cast<int32_t*>(at);
+  at += l.chunks;
   a.fresh = reinterpret_cast<int32_t*>(at);
   a.old = reinterpret_cast<int32_t*>(at + l.fresh);
 }
@@ -121,14 +130,23 @@ bool launched(comem::PageKernelFn fn, dim3 grid, int threads, comem::PageParams&
 
 // `moved`: the most tokens of an item that a call may copy.
 comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved, void* stream) {
-  const unsigned n = static_cast<unsigned>(a.n);
-  const int64_t units = ceil_div(moved, comem::kMoveTokens) * a.num_layers;
-  const int64_t movers = std::min(ceil_div(units, comem::kPageThreads / 64), std::max<int64_t>(1, kMovers / a.n));
-  const bool ok =
-      (op != comem::PageOp::kCompact || launched(comem::page_scan_kernel(), dim3(n), comem::kPageThreads, a, stream)) &&
-      launched(comem::select_page_take_kernel(op), dim3(1), comem::kTakeThreads, a, stream) &&
-      launched(comem::select_page_apply_kernel(op), dim3(static_cast<unsigned>(1 + movers), n), comem::kPageThreads, a,
-               stream);
+  using comem::PageOp;
+  const bool compact = op == PageOp::kCompact, alone = a.chunks == 1 && !compact;
+  bool ok = true;
+  if (!alone) {
+    const int64_t items = compact ? a.n : ceil_div(a.n, comem::kPageThreads);
+    const int64_t blocks = items + (a.chunks > 1 ? a.chunks : 0);
+    ok = launched(comem::select_page_find_kernel(op), dim3(static_cast<unsigned>(blocks)), comem::kPageThreads, a, stream);
+  }
+  ok = ok && launched(comem::select_page_give_kernel(op, alone), dim3(static_cast<unsigned>(a.chunks)),
+                      comem::kPageThreads, a, stream);
+  if (op != PageOp::kReserve) {
+    const int64_t units = ceil_div(moved, comem::kMoveTokens) * a.num_layers;
+    const int64_t movers = std::min(ceil_div(units, comem::kApplyThreads / 64), std::max<int64_t>(1, kMovers / a.n));
+    ok = ok && launched(comem::select_page_apply_kernel(op),
+                        dim3(static_cast<unsigned>(1 + movers), static_cast<unsigned>(a.n)), comem::kApplyThreads, a,
+                        stream);
+  }
   return ok ? COMEM_OK : COMEM_ERR_HIP;
 }
 

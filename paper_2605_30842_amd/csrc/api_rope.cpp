@@ -105,7 +105,7 @@ comem_status launch_rope(const comem_decode_attn_plan& p, comem::RopeParams& a, 
   const comem::RopeKernelFn fn = comem::select_rope_kernel(p.cfg.head_dim, cache, paged);
   if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
   const int64_t heads = p.cfg.num_q_heads + 2 * int64_t{p.cfg.num_kv_heads};
-  const int64_t passes = ceil_div(heads, 512 / p.cfg.head_dim);
+  const int64_t passes = ceil_div(heads, 1024 / p.cfg.head_dim);
   const int64_t tokens = static_cast<int64_t>(batch) * a.max_q;
   const int64_t want = std::max<int64_t>(1, 8 * p.num_cus / tokens);
   a.part_passes = static_cast<int32_t>(ceil_div(passes, std::min(want, passes)));

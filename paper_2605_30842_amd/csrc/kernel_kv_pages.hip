@@ -2,13 +2,14 @@
 // (gfx950). Nothing here computes; the tables take launches and round trips,
 // the copied tokens memory bandwidth.
 //
-// A call that needs fresh pages runs in two launches. In the first, one
-// workgroup finds what every item needs, adds it up in order and lists the
-// lowest free pages, so that the result depends on the state alone. In the
-// second, each item's first workgroup edits its table row and the counts, and
-// the others move tokens. A compact call has a launch before these, a
-// workgroup an item, that looks for the first token to move and copies the
-// row's entries, which the second launch reads while it replaces them.
+// Which pages a call gives out depends on the state alone: the lowest free
+// ones, to its items in order. With a pool of one chunk (8192 pages) one
+// workgroup finds the items' needs, ranks the free pages and hands them on.
+// With more, a launch before counts each chunk's free pages and a workgroup
+// per chunk hands out its own: the counts before it give its first rank.
+// Fork and compact calls then edit the tables and move tokens in one more
+// launch: an item's first workgroup the tables, the others the tokens. The
+// counts of given-up pages go down only there, after every look for free ones.
 #include "kv_pages.h"
 
 namespace comem {
@@ -22,99 +23,109 @@ __device__ inline int32_t pages_for(int64_t tokens, int shift) {
 
 __device__ inline bool in_pool(const PageParams& p, int32_t page) { return page >= 0 && page < p.num_pages; }
 
-// Inclusive sum over the lanes of a wave up to this one.
-__device__ inline int64_t wave_scan(int64_t x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp_add(uint32_t x) {
+  return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xf, false));
 }
 
-__device__ inline int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+// Inclusive sum over the lanes of a wave up to this one (within each row of
+// 16, then the rows' last lanes on to the next rows).
+__device__ inline uint32_t wave_scan(uint32_t x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
 }
+
+// Minimum over the wave, in its last lane.
+template <int CTRL, int ROWS>
+__device__ inline int dpp_min(int x) {
+  const int y = __builtin_amdgcn_update_dpp(INT32_MAX, x, CTRL, ROWS, 0xf, false);
+  return x < y ? x : y;
+}
+
+__device__ inline int wave_min(int x) {
+  x = dpp_min<0x111, 0xf>(x);
+  x = dpp_min<0x112, 0xf>(x);
+  x = dpp_min<0x114, 0xf>(x);
+  x = dpp_min<0x118, 0xf>(x);
+  x = dpp_min<0x142, 0xa>(x);
+  return dpp_min<0x143, 0xc>(x);
+}
+
+// Pages needed: sums of up to 2^31 each pass 32 bits, so they are summed in
+// two parts of which no workgroup's sum does.
+constexpr int kLowBits = 20;
+struct NeedSums {
+  uint32_t low[kPageThreads / 64], high[kPageThreads / 64];
+};
 
 // Sum of the workgroup's values before this thread's, and of all of them.
 // `sums` is one of two buffers used in turn: a barrier stands between a
 // buffer's reads and its next writes.
-template <typename T>
-__device__ inline T block_scan(T x, T* sums, T& total) {
+__device__ inline int64_t block_scan(int64_t x, NeedSums& sums, int64_t& total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const T upto = wave_scan(x, lane);
-  if (lane == 63) sums[w] = upto;
+  const uint32_t low = static_cast<uint32_t>(x) & ((1u << kLowBits) - 1), high = static_cast<uint32_t>(x >> kLowBits);
+  const uint32_t lo = wave_scan(low), hi = wave_scan(high);
+  if (lane == 63) {
+    sums.low[w] = lo;
+    sums.high[w] = hi;
+  }
   __syncthreads();
-  T before = 0, all = 0;
+  uint32_t lo_before = 0, hi_before = 0, lo_all = 0, hi_all = 0;
 #pragma unroll
-  for (int i = 0; i < kTakeThreads / 64; ++i) {
-    const T s = sums[i];
-    before += i < w ? s : 0;
-    all += s;
+  for (int i = 0; i < kPageThreads / 64; ++i) {
+    lo_before += i < w ? sums.low[i] : 0;
+    hi_before += i < w ? sums.high[i] : 0;
+    lo_all += sums.low[i];
+    hi_all += sums.high[i];
   }
-  total = all;
-  return before + upto - x;
+  total = (static_cast<int64_t>(hi_all) << kLowBits) + lo_all;
+  return (static_cast<int64_t>(hi_before + hi - high) << kLowBits) + (lo_before + lo - low);
 }
 
-__global__ __launch_bounds__(kPageThreads) void page_scan(const PageParams p) {
-  __shared__ int first_moved;
-  const int i = blockIdx.x;
-  const int r = p.rows[i];
-  const int64_t n = p.keep_lens[i], start = p.keep_start[i];
-  int64_t len = -1;
-  if (r >= 0 && r < p.num_rows) len = p.ctx_lens[r];
-  const bool valid = len >= 0 && len <= p.max_ctx && n >= 0 && n <= len && start >= 0 && start <= p.keep_total - n;
-  if (threadIdx.x == 0) first_moved = static_cast<int>(valid ? n : 0);
-  __syncthreads();
-  if (!valid) {
-    if (threadIdx.x == 0) {
-      p.items.row[i] = -1;
-      p.items.need[i] = 0;
-    }
-    return;
+// Free pages of chunk `chunk` as wave masks: bit l of mask k of a wave is page
+// 64 (16 w' + k) + l of the chunk, w' the wave's place. Returns the wave's count.
+constexpr int kMasks = kChunkPages / kPageThreads;
+__device__ inline int free_masks(const PageParams& p, int chunk, uint64_t (&mask)[kMasks]) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t c0 = static_cast<int64_t>(chunk) * kChunkPages + w * (64 * kMasks) + lane;
+  int32_t x[kMasks];
+#pragma unroll
+  for (int k = 0; k < kMasks; ++k) x[k] = c0 + 64 * k < p.num_pages ? p.refcounts[c0 + 64 * k] : 1;
+  int count = 0;
+#pragma unroll
+  for (int k = 0; k < kMasks; ++k) {
+    mask[k] = __builtin_amdgcn_ballot_w64(x[k] == 0);
+    count += __popcll(mask[k]);
   }
-  int moved = static_cast<int>(n);
-  for (int t = threadIdx.x; t < n; t += kPageThreads) {
-    if (p.keep[start + t] != t) {
-      moved = t;
-      break;
-    }
-  }
-  atomicMin(&first_moved, moved);
-  const int held = pages_for(len, p.page_shift);
-  const int32_t* entries = p.block_table + static_cast<int64_t>(r) * p.max_pages;
-  int32_t* old = p.old + static_cast<int64_t>(i) * p.max_pages;
-  for (int e = threadIdx.x; e < held; e += kPageThreads) old[e] = entries[e];
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const int first = first_moved >> p.page_shift;
-    p.items.row[i] = r;
-    p.items.len[i] = static_cast<int32_t>(len);
-    p.items.grown[i] = static_cast<int32_t>(n);
-    p.items.first[i] = first;
-    p.items.need[i] = pages_for(n, p.page_shift) - first;
-  }
+  return count;
 }
 
-// What item i of a call needs.
+struct Item {
+  int row, grown, first, need;
+};
+
+__device__ inline Item read_item(const PageParams& p, int i) {
+  return Item{p.items.row[i], p.items.grown[i], p.items.first[i], p.items.need[i]};
+}
+
+// Item i of a reserve or fork call.
 template <PageOp OP>
-__device__ inline int find_item(const PageParams& p, int i) {
-  if constexpr (OP == PageOp::kCompact) return p.items.need[i];
-  int row = -1, from = -1, first = 0, need = 0;
-  int64_t len = -1, grown = -1;
+__device__ inline Item find_item(const PageParams& p, int i) {
+  Item item{-1, -1, 0, 0};
+  int from = -1;
+  int64_t len = -1;
   if constexpr (OP == PageOp::kReserve) {
     const int64_t add = p.add_lens[i];
     len = p.ctx_lens[i];
-    grown = len + add;
-    if (len >= 0 && add >= 0 && grown <= p.max_ctx) {
-      row = i;
-      first = pages_for(len, p.page_shift);
-      need = pages_for(grown, p.page_shift) - first;
+    if (len >= 0 && add >= 0 && len + add <= p.max_ctx) {
+      item.row = i;
+      item.grown = static_cast<int>(len + add);
+      item.first = pages_for(len, p.page_shift);
+      item.need = pages_for(len + add, p.page_shift) - item.first;
     }
   } else {
     const int child = p.children[i];
@@ -122,69 +133,195 @@ __device__ inline int find_item(const PageParams& p, int i) {
     if (from >= 0 && from < p.num_rows && child >= 0 && child < p.num_rows && child != from && p.ctx_lens[child] == 0)
       len = p.ctx_lens[from];
     if (len >= 0 && len <= p.max_ctx) {
-      row = child;
-      grown = len;
-      first = static_cast<int>(len >> p.page_shift);
-      need = pages_for(len, p.page_shift) - first;
+      item.row = child;
+      item.grown = static_cast<int>(len);
+      item.first = static_cast<int>(len >> p.page_shift);
+      item.need = pages_for(len, p.page_shift) - item.first;
     }
+    p.items.from[i] = from;
+    p.items.len[i] = static_cast<int32_t>(len);
   }
-  p.items.row[i] = row;
-  p.items.from[i] = from;
-  p.items.len[i] = static_cast<int32_t>(len);
-  p.items.grown[i] = static_cast<int32_t>(grown);
-  p.items.first[i] = first;
-  p.items.need[i] = need;
-  return need;
+  p.items.row[i] = item.row;
+  p.items.grown[i] = item.grown;
+  p.items.first[i] = item.first;
+  p.items.need[i] = item.need;
+  return item;
 }
 
-// Gives out the lowest free pages: items' needs summed in order, then the
-// counts looked through from page 0 until there are enough zeros. A thread
-// takes 16 neighbouring counts a step.
-template <PageOp OP>
-__global__ __launch_bounds__(kTakeThreads) void page_take(const PageParams p) {
-  constexpr int kCounts = 16;
-  constexpr int kStep = kCounts * kTakeThreads;
-  __shared__ int64_t need_sums[2][kTakeThreads / 64];
-  __shared__ int free_sums[2][kTakeThreads / 64];
-  int64_t need_all = 0;
-  int turn = 0;
-  for (int i0 = 0; i0 < p.n; i0 += kTakeThreads, turn ^= 1) {
-    const int i = i0 + static_cast<int>(threadIdx.x);
-    const int64_t need = i < p.n ? find_item<OP>(p, i) : 0;
-    int64_t total;
-    const int64_t base = need_all + block_scan<int64_t>(need, need_sums[turn], total);
-    // Past 2^31 the call has no pages and the base is not used.
-    if (i < p.n) p.items.base[i] = static_cast<int32_t>(base);
-    need_all += total;
-  }
-  int64_t found = 0;
-  turn = 0;
-  for (int64_t c0 = 0; c0 < p.num_pages && found < need_all; c0 += kStep, turn ^= 1) {
-    const int64_t c = c0 + kCounts * static_cast<int64_t>(threadIdx.x);
-    uint32_t zeros = 0;
-    if (c + kCounts <= p.num_pages) {
-      const int4* counts = reinterpret_cast<const int4*>(p.refcounts + c);
+// Item i of a compact call, by a whole workgroup: the first token that moves,
+// and the row's entries, which are replaced later, while tokens are read
+// through them.
+__device__ inline void find_cut(const PageParams& p, int i) {
+  __shared__ int first_moved;
+  constexpr int kAtOnce = 4;
+  const int r = p.rows[i];
+  const int64_t n = p.keep_lens[i], start = p.keep_start[i];
+  if (threadIdx.x == 0) first_moved = INT32_MAX;
+  __syncthreads();
+  // The list, the row's length and its entries (as many as a row can have)
+  // are asked for together: none waits for another.
+  const bool listed = n >= 0 && n <= p.max_ctx && start >= 0 && start <= p.keep_total - n;
+  const bool has_row = r >= 0 && r < p.num_rows;
+  const int32_t* entries = p.block_table + static_cast<int64_t>(has_row ? r : 0) * p.max_pages;
+  int32_t* old = p.old + static_cast<int64_t>(i) * p.max_pages;
+  const int64_t len = has_row ? p.ctx_lens[r] : -1;
+  const int most = has_row ? pages_for(p.max_ctx, p.page_shift) : 0;
+  const int kept = listed ? static_cast<int>(n) : 0;
+  int moved = kept;
+  const int tid = threadIdx.x;
+  for (int64_t t0 = tid; t0 < (kept > most ? kept : most); t0 += kAtOnce * kPageThreads) {
+    int32_t at[kAtOnce], page[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < kCounts / 4; ++k) {
-        const int4 x = counts[k];
-        zeros |= ((x.x == 0 ? 1u : 0u) | (x.y == 0 ? 2u : 0u) | (x.z == 0 ? 4u : 0u) | (x.w == 0 ? 8u : 0u)) << (4 * k);
-      }
-    } else {
-      for (int k = 0; k < kCounts && c + k < p.num_pages; ++k) zeros |= (p.refcounts[c + k] == 0 ? 1u : 0u) << k;
+    for (int a = 0; a < kAtOnce; ++a) {
+      const int64_t t = t0 + a * kPageThreads;
+      at[a] = t < moved ? p.keep[start + t] : 0;
+      page[a] = t < most ? entries[t] : 0;
     }
-    int total;
-    int64_t rank = found + block_scan<int>(__popc(zeros), free_sums[turn], total);
-    while (zeros != 0 && rank < need_all) {
-      const int k = __ffs(zeros) - 1;
-      zeros &= zeros - 1;
-      p.fresh[rank++] = static_cast<int32_t>(c + k);
+#pragma unroll
+    for (int a = 0; a < kAtOnce; ++a) {
+      const int64_t t = t0 + a * kPageThreads;
+      if (t < moved && at[a] != t) moved = static_cast<int>(t);
+      if (t < most) old[t] = page[a];
     }
-    found += total;
   }
+  moved = wave_min(moved);
+  if ((tid & 63) == 63) atomicMin(&first_moved, moved);
+  const bool valid = has_row && listed && len >= 0 && len <= p.max_ctx && n <= len;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    const int64_t missing = need_all > found ? need_all - found : 0;
+    const int first = valid ? first_moved >> p.page_shift : 0;
+    p.items.row[i] = valid ? r : -1;
+    p.items.len[i] = static_cast<int32_t>(len);
+    p.items.grown[i] = static_cast<int32_t>(n);
+    p.items.first[i] = first;
+    p.items.need[i] = valid ? pages_for(n, p.page_shift) - first : 0;
+  }
+}
+
+template <PageOp OP>
+__global__ __launch_bounds__(kPageThreads) void page_find(const PageParams p) {
+  const int counted = p.chunks > 1 ? p.chunks : 0;
+  if (static_cast<int>(blockIdx.x) < counted) {
+    __shared__ int32_t waves[kPageThreads / 64];
+    uint64_t mask[kMasks];
+    const int count = free_masks(p, blockIdx.x, mask);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = count;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int all = 0;
+      for (int w = 0; w < kPageThreads / 64; ++w) all += waves[w];
+      p.free_counts[blockIdx.x] = all;
+    }
+  } else if constexpr (OP == PageOp::kCompact) {
+    find_cut(p, blockIdx.x - counted);
+  } else {
+    const int64_t i = static_cast<int64_t>(blockIdx.x - counted) * kPageThreads + threadIdx.x;
+    if (i < p.n) find_item<OP>(p, static_cast<int>(i));
+  }
+}
+
+// Hands the chunk's free pages to the items whose places fall to them: into
+// the table (reserve) or the list of fresh pages (fork, compact).
+template <PageOp OP, bool ALONE>
+__global__ __launch_bounds__(kPageThreads) void page_give(const PageParams p) {
+  constexpr int kWaves = kPageThreads / 64;
+  __shared__ NeedSums sums[2];
+  __shared__ int32_t wave_free[kWaves];
+  __shared__ int64_t tile_base[kPageThreads];
+  __shared__ int32_t tile_need[kPageThreads], tile_first[kPageThreads];
+  __shared__ int32_t pages[kChunkPages];  // the chunk's free pages in order
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int chunk = ALONE ? 0 : blockIdx.x;
+  // The first tile of items stays in registers: with up to 1024 items no
+  // other is looked at.
+  Item item{};
+  if (static_cast<int>(threadIdx.x) < p.n) item = ALONE ? find_item<OP>(p, threadIdx.x) : read_item(p, threadIdx.x);
+  uint64_t mask[kMasks];
+  const int mine = free_masks(p, chunk, mask);
+  if (lane == 0) wave_free[w] = mine;
+  int64_t need_all, tile;
+  int64_t base = block_scan(item.need, sums[0], need_all);
+  tile = need_all;
+  int place = 0, own = 0;  // the wave's place among the chunk's free pages, and their number
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    place += i < w ? wave_free[i] : 0;
+    own += wave_free[i];
+  }
+  if (p.n > kPageThreads) {
+    int64_t more = 0, all;
+    for (int i = threadIdx.x + kPageThreads; i < p.n; i += kPageThreads)
+      more += ALONE ? find_item<OP>(p, i).need : p.items.need[i];
+    block_scan(more, sums[1], all);
+    need_all += all;
+    __syncthreads();
+  }
+  // Free pages of the chunks before this one and of all.
+  int64_t before = 0, free_all = own;
+  if (!ALONE && p.chunks > 1) {
+    int64_t f = 0, b = 0;
+    for (int c = threadIdx.x; c < p.chunks; c += kPageThreads) {
+      f += p.free_counts[c];
+      b += c < chunk ? p.free_counts[c] : 0;
+    }
+    block_scan(b, sums[1], before);
+    block_scan(f, sums[0], free_all);
+  }
+  const int64_t missing = need_all > free_all ? need_all - free_all : 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     *p.granted = missing == 0 ? 1 : 0;
     *p.missing = static_cast<int32_t>(missing < INT32_MAX ? missing : INT32_MAX);
+  }
+  if (missing != 0) return;
+
+#pragma unroll
+  for (int k = 0; k < kMasks; ++k) {
+    if ((mask[k] >> lane) & 1) {
+      const int64_t page = static_cast<int64_t>(chunk) * kChunkPages + (w * kMasks + k) * 64 + lane;
+      pages[place + __popcll(mask[k] & ((uint64_t{1} << lane) - 1))] = static_cast<int32_t>(page);
+    }
+    place += __popcll(mask[k]);
+  }
+  const int64_t end = before + own < need_all ? before + own : need_all;  // places [before, end) are this chunk's
+  if constexpr (OP != PageOp::kReserve) {
+    __syncthreads();
+    for (int64_t r = before + static_cast<int64_t>(threadIdx.x); r < end; r += kPageThreads) p.fresh[r] = pages[r - before];
+    if (blockIdx.x != 0) return;
+  }
+  // Items in tiles of 1024. Reserve: each wave fills the entries of its items.
+  int64_t tile_start = 0;
+  int turn = 1;
+  for (int i0 = 0;;) {
+    const int i = i0 + static_cast<int>(threadIdx.x);
+    if constexpr (OP == PageOp::kReserve) {
+      tile_base[threadIdx.x] = base;
+      tile_need[threadIdx.x] = item.need;
+      tile_first[threadIdx.x] = item.first;
+      if (blockIdx.x == 0 && i < p.n && item.row >= 0) p.ctx_lens[i] = item.grown;
+      __syncthreads();
+      for (int k = w; k < kPageThreads && i0 + k < p.n; k += kWaves) {
+        const int64_t b = tile_base[k];
+        const int64_t lo = b > before ? b : before, hi = b + tile_need[k] < end ? b + tile_need[k] : end;
+        if (lo >= hi) continue;
+        int32_t* entries = p.block_table + static_cast<int64_t>(i0 + k) * p.max_pages + tile_first[k];
+        for (int64_t r = lo + lane; r < hi; r += 64) {
+          const int32_t page = pages[r - before];
+          entries[r - b] = page;
+          p.refcounts[page] = 1;
+        }
+      }
+    } else if (i < p.n) {
+      p.items.base[i] = static_cast<int32_t>(base);
+    }
+    i0 += kPageThreads;
+    tile_start += tile;
+    // Of the other chunks' workgroups, those whose places are filled stop.
+    if (i0 >= p.n || (blockIdx.x != 0 && tile_start >= end)) return;
+    __syncthreads();
+    const int next = i0 + static_cast<int>(threadIdx.x);
+    item = next < p.n ? read_item(p, next) : Item{};
+    base = tile_start + block_scan(item.need, sums[turn], tile);
+    turn ^= 1;
   }
 }
 
@@ -195,7 +332,7 @@ __device__ inline void edit_table(const PageParams& p, int i, int row) {
   const int32_t* fresh = p.fresh + p.items.base[i];
   if constexpr (OP == PageOp::kFork) {
     const int32_t* from = p.block_table + static_cast<int64_t>(p.items.from[i]) * p.max_pages;
-    for (int e = threadIdx.x; e < first; e += kPageThreads) {
+    for (int e = threadIdx.x; e < first; e += kApplyThreads) {
       const int32_t page = from[e];
       entries[e] = page;
       if (in_pool(p, page)) atomicAdd(p.refcounts + page, 1);
@@ -204,12 +341,12 @@ __device__ inline void edit_table(const PageParams& p, int i, int row) {
   if constexpr (OP == PageOp::kCompact) {
     const int32_t* old = p.old + static_cast<int64_t>(i) * p.max_pages;
     const int held = pages_for(len, p.page_shift);
-    for (int e = first + static_cast<int>(threadIdx.x); e < held; e += kPageThreads) {
+    for (int e = first + static_cast<int>(threadIdx.x); e < held; e += kApplyThreads) {
       if (in_pool(p, old[e])) atomicSub(p.refcounts + old[e], 1);
       if (e >= first + need) entries[e] = -1;
     }
   }
-  for (int e = threadIdx.x; e < need; e += kPageThreads) {
+  for (int e = threadIdx.x; e < need; e += kApplyThreads) {
     entries[first + e] = fresh[e];
     p.refcounts[fresh[e]] = 1;
   }
@@ -241,7 +378,7 @@ __device__ inline void move_tokens(const PageParams& p, int i, int mover, int mo
                                              : p.old + static_cast<int64_t>(i) * p.max_pages;
   const int64_t start = OP == PageOp::kCompact ? p.keep_start[i] : 0;
   const int pieces = p.num_kv_heads << p.piece_shift;
-  const int waves = kPageThreads / 64;
+  const int waves = kApplyThreads / 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int64_t u = static_cast<int64_t>(mover) * waves + wave; u < units; u += static_cast<int64_t>(movers) * waves) {
     const int layer = static_cast<int>(u / groups);
@@ -283,13 +420,13 @@ __device__ inline void move_tokens(const PageParams& p, int i, int mover, int mo
 }
 
 template <PageOp OP>
-__global__ __launch_bounds__(kPageThreads) void page_apply(const PageParams p) {
+__global__ __launch_bounds__(kApplyThreads) void page_apply(const PageParams p) {
   const int i = blockIdx.y;
   const int row = p.items.row[i];
   if (*p.granted == 0 || row < 0) return;
   if (blockIdx.x == 0) {
     edit_table<OP>(p, i, row);
-  } else if constexpr (OP != PageOp::kReserve) {
+  } else {
     move_tokens<OP>(p, i, blockIdx.x - 1, gridDim.x - 1);
   }
 }
@@ -312,15 +449,18 @@ __global__ __launch_bounds__(kPageThreads) void page_release(const PageParams p)
 
 }  // namespace
 
-PageKernelFn page_scan_kernel() { return page_scan; }
+PageKernelFn select_page_find_kernel(PageOp op) {
+  if (op == PageOp::kReserve) return page_find<PageOp::kReserve>;
+  return op == PageOp::kFork ? page_find<PageOp::kFork> : page_find<PageOp::kCompact>;
+}
 
-PageKernelFn select_page_take_kernel(PageOp op) {
-  if (op == PageOp::kReserve) return page_take<PageOp::kReserve>;
-  return op == PageOp::kFork ? page_take<PageOp::kFork> : page_take<PageOp::kCompact>;
+PageKernelFn select_page_give_kernel(PageOp op, bool alone) {
+  if (op == PageOp::kReserve) return alone ? page_give<PageOp::kReserve, true> : page_give<PageOp::kReserve, false>;
+  if (op == PageOp::kFork) return alone ? page_give<PageOp::kFork, true> : page_give<PageOp::kFork, false>;
+  return page_give<PageOp::kCompact, false>;
 }
 
 PageKernelFn select_page_apply_kernel(PageOp op) {
-  if (op == PageOp::kReserve) return page_apply<PageOp::kReserve>;
   return op == PageOp::kFork ? page_apply<PageOp::kFork> : page_apply<PageOp::kCompact>;
 }
 

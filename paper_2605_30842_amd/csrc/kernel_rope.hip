@@ -7,13 +7,14 @@
 // b c + a s). Queries go to q_out, keys and values to the cache row of the
 // token, in the cache's type (FP8: the code nearest to value / scale).
 //
-// D / 8 lanes take a head, 8 elements each, so that both elements of every
-// rotated pair are in one lane: elements 4j .. 4j + 3 and rot / 2 + 4j .. of a
-// head rotated in halves, 8j .. 8j + 7 otherwise and past the rotated ones.
-// The sum of squares crosses the head's lanes by data-parallel moves. A
-// wave's lanes so hold 4 (8) heads of one token in a pass and keep the
-// position's cosines and sines, which are 2 to 4 times as large as a head, in
-// registers over all passes; kRopeBatch passes' rows are in flight together.
+// D / 16 lanes take a head, 16 elements each, 8 and 8, so that both elements
+// of every rotated pair are in one lane and every access is 16 bytes wide
+// (8 bytes for codes): elements 8j .. 8j + 7 and rot / 2 + 8j .. of a head
+// rotated in halves, 16j .. 16j + 15 otherwise and past the rotated ones. The
+// sum of squares crosses the head's lanes by data-parallel moves. A wave's
+// lanes so hold 8 (16) heads of one token in a pass and keep the position's
+// cosines and sines, which are 2 to 4 times as large as a head, in registers
+// over all passes; kRopeBatch passes' rows are in flight together.
 #include <type_traits>
 
 #include "rope.h"
@@ -21,51 +22,51 @@
 namespace comem {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+typedef float f32x8 __attribute__((ext_vector_type(8), aligned(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
 struct F32Row {
-  static constexpr int kBytes = 4;
-  using Raw = f32x4;  // 4 elements
-  static __device__ f32x4 widen(Raw r) { return r; }
-  static __device__ Raw narrow(f32x4 x) { return x; }
+  using Elem = float;
+  using Raw = f32x8;  // 8 elements
+  static __device__ f32x8 widen(Raw r) { return r; }
+  static __device__ Raw narrow(f32x8 x) { return x; }
 };
 
 struct Bf16Row {
-  static constexpr int kBytes = 2;
-  using Raw = u32x2;
-  static __device__ f32x4 widen(Raw r) {
-    return f32x4{__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16),
-                 __uint_as_float(r[1] & 0xffff0000u)};
-  }
-  static __device__ Raw narrow(f32x4 x) {  // to nearest even
-    return Raw{__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2)),
-               __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2))};
-  }
+  using Elem = __bf16;
+  using Raw = bf16x8;
+  static __device__ f32x8 widen(Raw r) { return __builtin_convertvector(r, f32x8); }
+  static __device__ Raw narrow(f32x8 x) { return __builtin_convertvector(x, bf16x8); }  // to nearest even
 };
 
-// The E4M3 codes nearest to 4 values; 448 is the largest magnitude, NaN stays NaN.
-__device__ inline uint32_t fp8_codes(f32x4 x) {
+// The E4M3 codes nearest to 8 values; 448 is the largest magnitude, NaN stays NaN.
+__device__ inline u32x2 fp8_codes(f32x8 x) {
+  u32x2 r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = __builtin_fabsf(x[e]) > 448.f ? __builtin_copysignf(448.f, x[e]) : x[e];
-  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true));
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_fabsf(x[e]) > 448.f ? __builtin_copysignf(448.f, x[e]) : x[e];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+    r[i] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], lo, true));
+  }
+  return r;
 }
+
+__device__ inline f32x8 load8(const float* p) { return *reinterpret_cast<const f32x8*>(p); }
 
 template <int CTRL>
 __device__ inline float moved(float x) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(x)), CTRL, 0xf, 0xf, true));
 }
 
-// Sum over the D / 8 lanes of a head (neighbours, pairs, the 8 mirrored, the 16 mirrored).
+// Sum over the D / 16 lanes of a head (neighbours, pairs, the 8 mirrored).
 template <int D>
 __device__ inline float head_sum(float x) {
   x += moved<0xb1>(x);
   x += moved<0x4e>(x);
-  x += moved<0x141>(x);
-  if constexpr (D == 128) x += moved<0x140>(x);
+  if constexpr (D == 128) x += moved<0x141>(x);
   return x;
 }
 
@@ -73,9 +74,10 @@ template <int D, RopeCache CACHE, bool PAGED>
 __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const RopeParams p) {
   using Row = typename std::conditional<CACHE == RopeCache::kF32, F32Row, Bf16Row>::type;
   using Raw = typename Row::Raw;
-  constexpr int kLanes = D / 8;             // lanes of a head
-  constexpr int kHeads = 64 / kLanes;       // heads of a pass
-  constexpr int kStored = CACHE == RopeCache::kFp8 ? 1 : Row::kBytes;
+  using Elem = typename Row::Elem;
+  constexpr int kLanes = D / 16;       // lanes of a head
+  constexpr int kHeads = 64 / kLanes;  // heads of a pass
+  constexpr int kRow = D * static_cast<int>(sizeof(Elem));
   const int b = blockIdx.y;
   const int lane = threadIdx.x & 63;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kRopeWaves + (threadIdx.x >> 6));
@@ -100,28 +102,28 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
     at = start < 0 ? -1 : (start + t) * p.stride_token;
   }
 
-  // Elements of this lane: 4 from e0 on and 4 from e1 on.
+  // Elements of this lane: 8 from e0 on and 8 from e1 on.
   const int j = lane % kLanes;
   const int half = p.rot_dim / 2;
-  const bool turned = 8 * j < p.rot_dim;
+  const bool turned = 16 * j < p.rot_dim;
   const bool halves = turned && p.interleaved == 0;
-  const int e0 = halves ? 4 * j : 8 * j;
-  const int e1 = halves ? half + 4 * j : 8 * j + 4;
-  f32x4 c = {1.f, 1.f, 1.f, 1.f}, s = {0.f, 0.f, 0.f, 0.f};
+  const int e0 = halves ? 8 * j : 16 * j;
+  const int e1 = halves ? half + 8 * j : 16 * j + 8;
+  f32x8 c{}, s{};
   if (turned) {
     const int32_t pos = min(max(p.positions == nullptr ? t : p.positions[row], 0), p.num_positions - 1);
-    const float* angles = p.cos_sin + static_cast<int64_t>(pos) * p.rot_dim + 4 * j;
-    c = *reinterpret_cast<const f32x4*>(angles);
-    s = *reinterpret_cast<const f32x4*>(angles + half);
+    const float* angles = p.cos_sin + static_cast<int64_t>(pos) * p.rot_dim + 8 * j;
+    c = load8(angles);
+    s = load8(angles + half);
   }
   Raw wq0{}, wq1{}, wk0{}, wk1{};
   if (p.q_weight != nullptr) {
-    wq0 = *reinterpret_cast<const Raw*>(p.q_weight + e0 * Row::kBytes);
-    wq1 = *reinterpret_cast<const Raw*>(p.q_weight + e1 * Row::kBytes);
+    wq0 = *reinterpret_cast<const Raw*>(p.q_weight + e0 * sizeof(Elem));
+    wq1 = *reinterpret_cast<const Raw*>(p.q_weight + e1 * sizeof(Elem));
   }
   if (p.k_weight != nullptr) {
-    wk0 = *reinterpret_cast<const Raw*>(p.k_weight + e0 * Row::kBytes);
-    wk1 = *reinterpret_cast<const Raw*>(p.k_weight + e1 * Row::kBytes);
+    wk0 = *reinterpret_cast<const Raw*>(p.k_weight + e0 * sizeof(Elem));
+    wk1 = *reinterpret_cast<const Raw*>(p.k_weight + e1 * sizeof(Elem));
   }
 
   // Heads in order: queries, keys, values.
@@ -135,11 +137,11 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
       r0[u] = Raw{};
       r1[u] = Raw{};
       if (h < end) {
-        const char* src = h < p.num_q_heads ? p.q + row * p.q_stride + h * (D * Row::kBytes)
-                          : h < first_v     ? p.new_k + row * p.k_stride + (h - p.num_q_heads) * (D * Row::kBytes)
-                                            : p.new_v + row * p.v_stride + (h - first_v) * (D * Row::kBytes);
-        r0[u] = *reinterpret_cast<const Raw*>(src + e0 * Row::kBytes);
-        r1[u] = *reinterpret_cast<const Raw*>(src + e1 * Row::kBytes);
+        const char* src = h < p.num_q_heads ? p.q + row * p.q_stride + h * kRow
+                          : h < first_v     ? p.new_k + row * p.k_stride + (h - p.num_q_heads) * kRow
+                                            : p.new_v + row * p.v_stride + (h - first_v) * kRow;
+        r0[u] = *reinterpret_cast<const Raw*>(src + e0 * sizeof(Elem));
+        r1[u] = *reinterpret_cast<const Raw*>(src + e1 * sizeof(Elem));
       }
     }
 #pragma unroll
@@ -147,42 +149,44 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
       const int h = h0 + u * kHeads;
       if (h >= end) continue;
       const bool is_q = h < p.num_q_heads, is_v = h >= first_v;
-      f32x4 x0 = Row::widen(r0[u]), x1 = Row::widen(r1[u]);
+      f32x8 x0 = Row::widen(r0[u]), x1 = Row::widen(r1[u]);
       if (!is_v) {
         if ((is_q ? p.q_weight : p.k_weight) != nullptr) {
           float ss = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
+          for (int e = 0; e < 8; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
           const float r = rsqrtf(head_sum<D>(ss) * (1.f / D) + p.eps);
           x0 = x0 * r * Row::widen(is_q ? wq0 : wk0);
           x1 = x1 * r * Row::widen(is_q ? wq1 : wk1);
         }
         if (halves) {
-          const f32x4 y0 = x0 * c - x1 * s;
+          const f32x8 y0 = x0 * c - x1 * s;
           x1 = x1 * c + x0 * s;
           x0 = y0;
         } else if (turned) {
-          const f32x4 y0 = {x0[0] * c[0] - x0[1] * s[0], x0[1] * c[0] + x0[0] * s[0], x0[2] * c[1] - x0[3] * s[1],
-                            x0[3] * c[1] + x0[2] * s[1]};
-          const f32x4 y1 = {x1[0] * c[2] - x1[1] * s[2], x1[1] * c[2] + x1[0] * s[2], x1[2] * c[3] - x1[3] * s[3],
-                            x1[3] * c[3] + x1[2] * s[3]};
-          x0 = y0;
-          x1 = y1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float a0 = x0[2 * e], a1 = x1[2 * e];
+            x0[2 * e] = a0 * c[e] - x0[2 * e + 1] * s[e];
+            x0[2 * e + 1] = x0[2 * e + 1] * c[e] + a0 * s[e];
+            x1[2 * e] = a1 * c[e + 4] - x1[2 * e + 1] * s[e + 4];
+            x1[2 * e + 1] = x1[2 * e + 1] * c[e + 4] + a1 * s[e + 4];
+          }
         }
       }
       if (is_q) {
-        char* dst = p.q_out + (row * p.num_q_heads + h) * (D * Row::kBytes);
-        *reinterpret_cast<Raw*>(dst + e0 * Row::kBytes) = Row::narrow(x0);
-        *reinterpret_cast<Raw*>(dst + e1 * Row::kBytes) = Row::narrow(x1);
+        char* dst = p.q_out + (row * p.num_q_heads + h) * kRow;
+        *reinterpret_cast<Raw*>(dst + e0 * sizeof(Elem)) = Row::narrow(x0);
+        *reinterpret_cast<Raw*>(dst + e1 * sizeof(Elem)) = Row::narrow(x1);
       } else if (at >= 0) {
         char* dst = (is_v ? p.v : p.k) + at + (h - (is_v ? first_v : p.num_q_heads)) * p.stride_head;
         if constexpr (CACHE == RopeCache::kFp8) {
           const float inv = is_v ? p.inv_v_scale : p.inv_k_scale;
-          *reinterpret_cast<uint32_t*>(dst + e0 * kStored) = fp8_codes(x0 * inv);
-          *reinterpret_cast<uint32_t*>(dst + e1 * kStored) = fp8_codes(x1 * inv);
+          *reinterpret_cast<u32x2*>(dst + e0) = fp8_codes(x0 * inv);
+          *reinterpret_cast<u32x2*>(dst + e1) = fp8_codes(x1 * inv);
         } else {
-          *reinterpret_cast<Raw*>(dst + e0 * kStored) = is_v ? r0[u] : Row::narrow(x0);
-          *reinterpret_cast<Raw*>(dst + e1 * kStored) = is_v ? r1[u] : Row::narrow(x1);
+          *reinterpret_cast<Raw*>(dst + e0 * sizeof(Elem)) = is_v ? r0[u] : Row::narrow(x0);
+          *reinterpret_cast<Raw*>(dst + e1 * sizeof(Elem)) = is_v ? r1[u] : Row::narrow(x1);
         }
       }
     }

@@ -6,9 +6,10 @@
 
 namespace comem {
 
-constexpr int kPageThreads = 256;
-constexpr int kTakeThreads = 1024;  // the one workgroup that gives out pages
-constexpr int kMoveTokens = 8;      // tokens that a wave moves at a time
+constexpr int kPageThreads = 1024;   // kernels that edit tables and counts
+constexpr int kChunkPages = 8192;    // pages whose counts one workgroup looks through
+constexpr int kApplyThreads = 256;   // the kernel that also moves tokens
+constexpr int kMoveTokens = 4;       // tokens that a wave moves at a time
 
 // One item of a call: a row and the table entries that get fresh pages,
 // first .. first + need - 1. Workspace arrays, [num_rows] each.
@@ -19,7 +20,7 @@ struct PageItems {
   int32_t* grown;  // its tokens after the call
   int32_t* first;
   int32_t* need;
-  int32_t* base;   // place of the item's first page in `fresh`
+  int32_t* base;   // place of the item's first page in `fresh` (fork, compact)
 };
 
 // Offsets and strides are in bytes.
@@ -40,6 +41,7 @@ struct PageParams {
   int32_t max_pages;
   int32_t page_shift;
   int32_t n;                  // items
+  int32_t chunks;             // of kChunkPages pages
   int32_t num_kv_heads;
   int32_t piece_shift;        // log2 of the 16-byte pieces of a head's row
   const int32_t* rows;        // compact, release; fork: the parents
@@ -52,16 +54,21 @@ struct PageParams {
   int32_t* missing;
   PageItems items;            // workspace from here on
   int32_t* granted;           // [1]: whether the call has its pages
-  int32_t* fresh;             // the pages given out, in order
+  int32_t* free_counts;       // free pages of each chunk (more than one)
+  int32_t* fresh;             // fork, compact: the pages given out, in order
   int32_t* old;               // compact: the rows' entries before the call, [n, max_pages]
 };
 
 enum class PageOp { kReserve, kFork, kCompact };
 
 using PageKernelFn = void (*)(PageParams);
-PageKernelFn page_scan_kernel();                // compact: one workgroup per item
-PageKernelFn select_page_take_kernel(PageOp);   // one workgroup of kTakeThreads
-PageKernelFn select_page_apply_kernel(PageOp);  // grid (1 + movers, n)
+// Items and, of more than one chunk, the chunks' free pages: chunk_blocks +
+// (compact: n, else ceil(n / kPageThreads)) workgroups.
+PageKernelFn select_page_find_kernel(PageOp);
+// One workgroup per chunk. ALONE: of one chunk and no compact call, whose
+// items are found here as well.
+PageKernelFn select_page_give_kernel(PageOp, bool alone);
+PageKernelFn select_page_apply_kernel(PageOp);  // fork, compact: grid (1 + movers, n)
 PageKernelFn page_release_kernel();             // one workgroup per item
 
 }  // namespace comem

@@ -7,7 +7,7 @@
 namespace comem {
 
 constexpr int kRopeWaves = 4;  // waves per workgroup, each with a token or a part of its heads
-constexpr int kRopeBatch = 4;  // passes of a wave whose rows are in flight together
+constexpr int kRopeBatch = 3;  // passes of a wave whose rows are in flight together
 
 // Offsets and strides are in bytes.
 struct RopeParams {

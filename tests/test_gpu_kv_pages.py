@@ -124,7 +124,7 @@ def test_lowest_pages_in_order():
     b.check()
 
 
-@pytest.mark.parametrize("num_pages", [1, 15, 16, 17, 16383, 16384, 16385, 70001])
+@pytest.mark.parametrize("num_pages", [1, 63, 64, 65, 1023, 8191, 8192, 8193, 16384, 16385, 70001])
 def test_pools_of_many_sizes(num_pages):
     """The look through the counts in steps and its ragged end: all pages but three are held, then all of them."""
     say("pool of", num_pages)
@@ -144,8 +144,31 @@ def test_pools_of_many_sizes(num_pages):
     b.check(pools=False)
 
 
+@pytest.mark.parametrize("page", [1, 16])
+def test_random_lives_in_a_large_pool(page):
+    """Free pages here and there in several chunks of the counts, the rest held by others."""
+    rng = random.Random(page)
+    b = Both(5, 20011, page, 150, "fp8", 1, 64, 1)
+    held = torch.tensor([0 if rng.random() < 0.02 else 1 for _ in range(20011)], dtype=torch.int32)
+    b.counts.copy_(held)
+    b.m.counts = held.tolist()
+    for step in range(24):
+        kind = rng.choice(["reserve", "reserve", "fork", "compact", "release"])
+        say("large pool", page, step, kind)
+        if kind == "reserve":
+            b.reserve([rng.choice([0, 1, 17, 60, 150]) for _ in range(5)])
+        elif kind == "fork":
+            b.fork([rng.randrange(5)], [rng.randrange(5)])
+        elif kind == "compact":
+            r = rng.randrange(5)
+            b.compact([r], [_keep(rng, b.m.ctx[r])])
+        else:
+            b.release([rng.randrange(5)])
+        b.check(pools=step % 6 == 5)
+
+
 def test_more_rows_than_threads():
-    """3000 rows: their needs are added up over several rounds of the one workgroup."""
+    """3000 rows: their needs are added up in several tiles, by several workgroups."""
     b = Both(3000, 9000, 4, 12, heads=1, d=64, dtype="fp8")
     b.m.k = b.m.v = None
     rng = random.Random(2)
