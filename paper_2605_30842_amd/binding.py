@@ -516,9 +516,15 @@ def _call_on(op, stream, entry, *args) -> None:
     """entry(*args, stream) with the plan's device current (a stream belongs to its device)."""
     import torch
 
-    if op._torch_device.type == "cuda" and torch.cuda.current_device() != op.device:
+    if op._torch_device.type != "cuda":
+        entry(*args, op._stream(stream))
+        return
+    current = torch.cuda.current_device()
+    if current != op.device:
         with torch.cuda.device(op.device):
             entry(*args, op._stream(stream))
+    elif stream is None and hasattr(torch._C, "_cuda_getCurrentRawStream"):
+        entry(*args, torch._C._cuda_getCurrentRawStream(current))
     else:
         entry(*args, op._stream(stream))
 

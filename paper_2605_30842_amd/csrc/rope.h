@@ -53,6 +53,7 @@ struct RopeParams {
 enum class RopeCache { kF32, kBf16, kFp8 };
 
 using RopeKernelFn = void (*)(RopeParams);
-RopeKernelFn select_rope_kernel(int head_dim, RopeCache cache, bool paged);
+// stream: q_out, and cache rows that are no codes, are stored past the caches.
+RopeKernelFn select_rope_kernel(int head_dim, RopeCache cache, bool paged, bool stream);
 
 }  // namespace comem

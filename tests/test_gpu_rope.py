@@ -188,6 +188,25 @@ def test_long_chunk_many_waves_per_part(dtype):
     _run(Case(dtype, 32, 8, 128, 16, lens=(3001, 2000), new=(3001, 777)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+def test_more_than_the_caches_hold(dtype):
+    """Over 256 MB written: the same values as for each part of the tokens alone."""
+    n, hq, hkv = 17000, 64, 8
+    a = Case(dtype, hq, hkv, 128, 0, lens=(n,), new=(n,))
+    whole = a.call()[:n].clone()
+    k, v = a.k.clone(), a.v.clone()
+    a.k.fill_(3)
+    a.v.fill_(3)
+    for first in range(0, n, 4096):
+        last = min(first + 4096, n)
+        part = a.op.rope_append(a.q[first:last], a.new_k[first:last], a.new_v[first:last], a.k, a.v, a.seq_start,
+                                torch.tensor([last], dtype=torch.int32, device=DEV), n, a.cos_sin, a.q_weight, a.k_weight,
+                                a.eps, torch.zeros(1, dtype=torch.int64, device=DEV),
+                                torch.tensor([last - first], dtype=torch.int32, device=DEV), last - first)
+        assert torch.equal(part, whole[first:last])
+    assert torch.equal(a.k[:n], k[:n]) and torch.equal(a.v[:n], v[:n])
+
+
 def test_positions_and_their_bounds():
     c = Case("bf16", 8, 2, 64, 16, lens=(30, 12), new=(30, 5), positions=lambda r: (r * 7919) % 41 - 2, table_rows=33)
     _run(c)
