@@ -128,8 +128,11 @@ bool launched(comem::PageKernelFn fn, dim3 grid, int threads, comem::PageParams&
                          static_cast<hipStream_t>(stream)) == hipSuccess;
 }
 
-// `moved`: the most tokens of an item that a call may copy.
-comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved, void* stream) {
+// `moved`: the most tokens of an item that a call may copy; `bytes`: the most
+// that it may store in all. Tokens that the last cache (256 MB) cannot hold for
+// the attention that follows pass it by (us, compact calls that move 410 and
+// 799 MB 206 and 362 -> 190 and 344; 70 MB 59.3, past the caches 60.3).
+comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved, double bytes, void* stream) {
   using comem::PageOp;
   const bool compact = op == PageOp::kCompact, alone = a.chunks == 1 && !compact;
   bool ok = true;
@@ -143,7 +146,7 @@ comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved,
   if (op != PageOp::kReserve) {
     const int64_t units = ceil_div(moved, comem::kMoveTokens) * a.num_layers;
     const int64_t movers = std::min(ceil_div(units, comem::kApplyThreads / 64), std::max<int64_t>(1, kMovers / a.n));
-    ok = ok && launched(comem::select_page_apply_kernel(op),
+    ok = ok && launched(comem::select_page_apply_kernel(op, bytes > 256.0 * (1 << 20)),
                         dim3(static_cast<unsigned>(1 + movers), static_cast<unsigned>(a.n)), comem::kApplyThreads, a,
                         stream);
   }
@@ -181,7 +184,7 @@ comem_status comem_kv_reserve(const comem_decode_attn_plan* plan, const comem_kv
   set_workspace(*pages, workspace, a);
   a.add_lens = add_lens;
   a.missing = missing;
-  return launch_pages(comem::PageOp::kReserve, a, 0, hip_stream);
+  return launch_pages(comem::PageOp::kReserve, a, 0, 0, hip_stream);
 }
 
 comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* parents,
@@ -206,7 +209,7 @@ comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pa
   a.rows = parents;
   a.children = children;
   a.missing = missing;
-  return launch_pages(comem::PageOp::kFork, a, pages->page_size, hip_stream);
+  return launch_pages(comem::PageOp::kFork, a, pages->page_size, 0, hip_stream);
 }
 
 comem_status comem_kv_compact(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* rows,
@@ -238,7 +241,9 @@ comem_status comem_kv_compact(const comem_decode_attn_plan* plan, const comem_kv
   a.keep_start = keep_start;
   a.keep_lens = keep_lens;
   a.missing = missing;
-  return launch_pages(comem::PageOp::kCompact, a, std::min(keep_total, pages->max_ctx_len), hip_stream);
+  const double token = 2.0 * p->cfg.num_kv_heads * p->cfg.head_dim * elem_bytes(p->cfg) * pages->num_layers;
+  return launch_pages(comem::PageOp::kCompact, a, std::min(keep_total, pages->max_ctx_len),
+                      static_cast<double>(keep_total) * token, hip_stream);
 }
 
 comem_status comem_kv_release(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* rows,

@@ -360,10 +360,25 @@ __device__ inline int64_t of_lane(int64_t x, int lane) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
+// STREAM: past the caches.
+template <bool STREAM>
+__device__ inline u32x4 get16(const char* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return *reinterpret_cast<const u32x4*>(p);
+}
+template <bool STREAM>
+__device__ inline void put16(char* p, u32x4 x) {
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+  } else {
+    *reinterpret_cast<u32x4*>(p) = x;
+  }
+}
+
 // Tokens first << page_shift .. grown - 1 of item i to their fresh pages, K
 // and V of every layer. A wave takes kMoveTokens tokens of a layer: lane l
 // finds token l's rows, then the wave copies 4 tokens' pieces at a time.
-template <PageOp OP>
+template <PageOp OP, bool STREAM>
 __device__ inline void move_tokens(const PageParams& p, int i, int mover, int movers) {
   constexpr int kAtOnce = 4;
   const int lane = threadIdx.x & 63;
@@ -404,14 +419,14 @@ __device__ inline void move_tokens(const PageParams& p, int i, int mover, int mo
         u32x4 k[kAtOnce], v[kAtOnce];
 #pragma unroll
         for (int a = 0; a < kAtOnce; ++a) {
-          k[a] = *reinterpret_cast<const u32x4*>(p.k + s[a] + piece);
-          v[a] = *reinterpret_cast<const u32x4*>(p.v + s[a] + piece);
+          k[a] = get16<STREAM>(p.k + s[a] + piece);
+          v[a] = get16<STREAM>(p.v + s[a] + piece);
         }
 #pragma unroll
         for (int a = 0; a < kAtOnce; ++a) {
           if (k0 + a < count) {
-            *reinterpret_cast<u32x4*>(p.k + d[a] + piece) = k[a];
-            *reinterpret_cast<u32x4*>(p.v + d[a] + piece) = v[a];
+            put16<STREAM>(p.k + d[a] + piece, k[a]);
+            put16<STREAM>(p.v + d[a] + piece, v[a]);
           }
         }
       }
@@ -419,7 +434,7 @@ __device__ inline void move_tokens(const PageParams& p, int i, int mover, int mo
   }
 }
 
-template <PageOp OP>
+template <PageOp OP, bool STREAM>
 __global__ __launch_bounds__(kApplyThreads) void page_apply(const PageParams p) {
   const int i = blockIdx.y;
   const int row = p.items.row[i];
@@ -427,7 +442,7 @@ __global__ __launch_bounds__(kApplyThreads) void page_apply(const PageParams p) 
   if (blockIdx.x == 0) {
     edit_table<OP>(p, i, row);
   } else {
-    move_tokens<OP>(p, i, blockIdx.x - 1, gridDim.x - 1);
+    move_tokens<OP, STREAM>(p, i, blockIdx.x - 1, gridDim.x - 1);
   }
 }
 
@@ -460,8 +475,9 @@ PageKernelFn select_page_give_kernel(PageOp op, bool alone) {
   return page_give<PageOp::kCompact, false>;
 }
 
-PageKernelFn select_page_apply_kernel(PageOp op) {
-  return op == PageOp::kFork ? page_apply<PageOp::kFork> : page_apply<PageOp::kCompact>;
+PageKernelFn select_page_apply_kernel(PageOp op, bool stream) {
+  if (op == PageOp::kFork) return page_apply<PageOp::kFork, false>;
+  return stream ? page_apply<PageOp::kCompact, true> : page_apply<PageOp::kCompact, false>;
 }
 
 PageKernelFn page_release_kernel() { return page_release; }

@@ -68,7 +68,8 @@ PageKernelFn select_page_find_kernel(PageOp);
 // One workgroup per chunk. ALONE: of one chunk and no compact call, whose
 // items are found here as well.
 PageKernelFn select_page_give_kernel(PageOp, bool alone);
-PageKernelFn select_page_apply_kernel(PageOp);  // fork, compact: grid (1 + movers, n)
+// Fork, compact: grid (1 + movers, n). stream (compact): tokens pass the caches by.
+PageKernelFn select_page_apply_kernel(PageOp, bool stream);
 PageKernelFn page_release_kernel();             // one workgroup per item
 
 }  // namespace comem

@@ -332,6 +332,21 @@ def test_other_stream():
     b.check()
 
 
+def test_compact_of_more_than_the_caches_hold():
+    """A list of over 256 MB of tokens, strictly increasing, with gaps."""
+    n, page = 40000, 64
+    b = Both(2, 1400, page, n, dtype="bf16", heads=8, d=128, layers=2, seed=3)
+    b.reserve([n, 0])
+    keep = [t for t in range(n) if t < 200 or t % 7 != 3]
+    assert len(keep) * 2 * 8 * 128 * 2 * 2 > 256 << 20
+    src = b.k[:, b.table[0, :n // page].long()].flatten(1, 2)[:, torch.tensor(keep, device=DEV)].clone()
+    b.m.k = b.m.v = None
+    assert b.fork([0], [1]) == 0 and b.compact([1], [keep]) == 0
+    b.check(pools=False)
+    rows = b.table[1, :pages_of(len(keep), page)].long()
+    assert torch.equal(b.k[:, rows].flatten(1, 2)[:, :len(keep)], src)
+
+
 def test_copies_past_4_gib():
     """Pages whose offsets, within a layer and over layers, pass 32 bits."""
     from paper_2605_30842_amd.binding import DecodeAttention, KVPages
