@@ -1,6 +1,6 @@
 /*
  * comem_prefill_attn.h -- prefill attention over a cached prefix on AMD
- * Instinct MI355X (gfx950), for bf16 and FP8 caches.
+ * Instinct MI355X (gfx950), for bf16 caches.
  *
  * The operation (paper Algorithm 1, "cached" and "uncached" prefill of the
  * k-step-off pipeline, Sec. 3.2): while the agent's KV cache stays valid, a
@@ -20,17 +20,12 @@
  * decode step. Scores and sums are fp32; the probabilities enter the matrix
  * cores as a sum of two bf16 values, so an output differs from exact
  * arithmetic by at most about 2^-15 * sum_t softmax(s)_t * |V_b[t, h / G, d]|
- * plus fp32 rounding. Over an FP8 cache (K and V are codes, attended as in
- * comem_decode_attn.h; q is bf16) they enter as a sum of two f16 values: a
- * weight is off by at most 2^-23 of itself, or by 2^-34 of the row's largest
- * weight where that is more. A NaN code of K makes out and lse of the rows
- * that see it NaN; a NaN of V, in either cache type, the outputs at its place,
- * where the V of a new token may reach new tokens before it too.
+ * plus fp32 rounding.
  *
  * Both calls take a plan from comem_decode_attn_init (comem_decode_attn.h)
- * whose dtype is COMEM_BF16 or COMEM_FP8_E4M3; its heads, head_dim (64 or
- * 128), scale, FP8 scales, max_batch and max_ctx_len apply, its chunk_tokens
- * and variant do not. They
+ * whose dtype is COMEM_BF16 (FP8 caches: comem_prefill_fp8.h); its heads,
+ * head_dim (64 or 128), scale, max_batch and max_ctx_len apply, its
+ * chunk_tokens and variant do not. They
  * need no workspace, enqueue one kernel on the given stream and return; they
  * never allocate, synchronise, or read device memory from the host. The
  * split forms below take a workspace besides and are faster where a few new

@@ -34,6 +34,7 @@ EXPORTED = (
     "comem_decode_attn_noalloc", "comem_prefill_attn_workspace", "comem_prefill_attn_split",
     "comem_prefill_attn_split_paged",
 )
+PREFILL_FP8_EXPORTED = ("comem_prefill_fp8_workspace", "comem_prefill_fp8_attn", "comem_prefill_fp8_attn_paged")
 ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
 PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_fork", "comem_kv_compact",
                   "comem_kv_release")
@@ -204,7 +205,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comem_kv_fork.argtypes = [vp, pp, vp, vp, i32, vp, vp, sz, vp]
     lib.comem_kv_compact.argtypes = [vp, pp, vp, vp, i64, vp, vp, i32, vp, vp, sz, vp]
     lib.comem_kv_release.argtypes = [vp, pp, vp, i32, vp]
-    for name in ROPE_EXPORTED + PAGES_EXPORTED:
+    lib.comem_prefill_fp8_workspace.argtypes = lib.comem_prefill_attn_workspace.argtypes
+    lib.comem_prefill_fp8_attn.argtypes = lib.comem_prefill_attn_split.argtypes
+    lib.comem_prefill_fp8_attn_paged.argtypes = lib.comem_prefill_attn_split_paged.argtypes
+    for name in ROPE_EXPORTED + PAGES_EXPORTED + PREFILL_FP8_EXPORTED:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -389,6 +393,30 @@ def comem_prefill_attn_split_paged(plan, q, q_start, q_lens, max_q_len, k_pages,
                                                          block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len,
                                                          out, lse, workspace, workspace_bytes, stream),
            "comem_prefill_attn_split_paged")
+
+
+def comem_prefill_fp8_workspace(plan, batch, max_q_len, max_ctx_len) -> int:
+    nbytes = ctypes.c_size_t()
+    _check(load_library().comem_prefill_fp8_workspace(plan, batch, max_q_len, max_ctx_len, ctypes.byref(nbytes)),
+           "comem_prefill_fp8_workspace")
+    return nbytes.value
+
+
+def comem_prefill_fp8_attn(plan, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head, seq_start, ctx_lens,
+                           batch, max_ctx_len, out, lse, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().comem_prefill_fp8_attn(plan, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head,
+                                                 seq_start, ctx_lens, batch, max_ctx_len, out, lse, workspace,
+                                                 workspace_bytes, stream), "comem_prefill_fp8_attn")
+
+
+def comem_prefill_fp8_attn_paged(plan, q, q_start, q_lens, max_q_len, k_pages, v_pages, stride_page, stride_token,
+                                 stride_head, page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch,
+                                 max_ctx_len, out, lse, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().comem_prefill_fp8_attn_paged(plan, q, q_start, q_lens, max_q_len, k_pages, v_pages,
+                                                       stride_page, stride_token, stride_head, page_size, num_pages,
+                                                       block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len,
+                                                       out, lse, workspace, workspace_bytes, stream),
+           "comem_prefill_fp8_attn_paged")
 
 
 def comem_rope_append(plan, rope: RopeConfig, q, q_stride, new_k, k_stride, new_v, v_stride, q_start, q_lens, max_q_len,
@@ -830,6 +858,8 @@ class DecodeAttention:
 
     def prefill_workspace_bytes(self, batch: int, max_q_len: int, max_ctx_len: int) -> int:
         """Bytes of a workspace that a prefill call with these bounds can use (0: none)."""
+        if self.dtype == "fp8":
+            return comem_prefill_fp8_workspace(self.plan, batch, max_q_len, max_ctx_len)
         return comem_prefill_attn_workspace(self.plan, batch, max_q_len, max_ctx_len)
 
     def _prefill_workspace(self, batch, max_q_len, max_ctx_len, stream, given=None):
@@ -865,7 +895,7 @@ class DecodeAttention:
 
     def prefill(self, q, q_start, q_lens, max_q_len: int, k, v, seq_start, ctx_lens, max_ctx_len: int, out=None,
                 lse=None, stream=None, workspace=None):
-        """Prefill attention of the packed new tokens q [total, Hq, D] over a contiguous cache.
+        """Prefill attention of the packed new tokens q [total, Hq, D] over a contiguous cache (bf16 or FP8).
 
         workspace: device memory of any size that no other call uses at the same time (prefill_workspace_bytes says
         how much can be used). Without one, a call that gains from it takes scratch from torch's allocator, and in a
@@ -879,7 +909,10 @@ class DecodeAttention:
                 v.data_ptr(), k.stride(0), k.stride(1), seq_start.data_ptr(), ctx_lens.data_ptr(), ctx_lens.shape[0],
                 int(max_ctx_len), out.data_ptr(), None if lse is None else lse.data_ptr())
         ws = self._prefill_workspace(ctx_lens.shape[0], int(max_q_len), int(max_ctx_len), stream, workspace)
-        if ws is None:
+        if self.dtype == "fp8":
+            comem_prefill_fp8_attn(*args, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+                                   self._stream(stream))
+        elif ws is None:
             comem_prefill_attn(*args, self._stream(stream))
         else:
             comem_prefill_attn_split(*args, ws.data_ptr(), ws.nbytes, self._stream(stream))
@@ -897,7 +930,10 @@ class DecodeAttention:
                 k_pages.shape[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(),
                 ctx_lens.shape[0], int(max_ctx_len), out.data_ptr(), None if lse is None else lse.data_ptr())
         ws = self._prefill_workspace(ctx_lens.shape[0], int(max_q_len), int(max_ctx_len), stream, workspace)
-        if ws is None:
+        if self.dtype == "fp8":
+            comem_prefill_fp8_attn_paged(*args, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+                                         self._stream(stream))
+        elif ws is None:
             comem_prefill_attn_paged(*args, self._stream(stream))
         else:
             comem_prefill_attn_split_paged(*args, ws.data_ptr(), ws.nbytes, self._stream(stream))

@@ -1,5 +1,6 @@
-// Host side of the prefill-attention C ABI (comem_prefill_attn.h): argument
-// validation (before any HIP call) and launch of the prefill kernel.
+// Host side of the prefill-attention C ABI (comem_prefill_attn.h and, for FP8
+// caches, comem_prefill_fp8.h): argument validation (before any HIP call) and
+// launch of the prefill kernel.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -10,6 +11,7 @@
 #include "attn_common.h"
 #include "comem_decode_attn.h"
 #include "comem_prefill_attn.h"
+#include "comem_prefill_fp8.h"
 #include "plan.h"
 #include "prefill.h"
 
@@ -29,12 +31,13 @@ comem_status check_bounds(const comem_decode_attn_plan& p, int32_t batch, int32_
 }
 
 // Checks of a prefill call shared by both layouts; fills the kernel arguments.
-comem_status prepare_prefill(const comem_decode_attn_plan& p, const void* q, const int64_t* q_start,
+// `dtype`: the caches that the entry point is for.
+comem_status prepare_prefill(const comem_decode_attn_plan& p, int32_t dtype, const void* q, const int64_t* q_start,
                              const int32_t* q_lens, int32_t max_q_len, const void* k, const void* v,
                              int64_t stride_token, int64_t stride_head, const int32_t* ctx_lens, int32_t batch,
                              int64_t max_ctx_len, float* out, float* lse, const void* workspace,
                              comem::PrefillParams& a) {
-  if (p.cfg.dtype == COMEM_F32) return COMEM_ERR_UNSUPPORTED;
+  if (p.cfg.dtype != dtype) return COMEM_ERR_UNSUPPORTED;
   comem_status st = check_bounds(p, batch, max_q_len, max_ctx_len);
   if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
   st = validate_common(p, q, k, v, stride_token, stride_head, ctx_lens, batch, max_ctx_len, out, lse, workspace);
@@ -170,17 +173,13 @@ comem_status launch_prefill(const comem_decode_attn_plan& p, const comem::Prefil
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }
 
-}  // namespace
-
-extern "C" {
-
-comem_status comem_prefill_attn_workspace(const comem_decode_attn_plan* plan, int32_t batch, int32_t max_q_len,
-                                          int64_t max_ctx_len, size_t* workspace_bytes_out) {
+comem_status prefill_workspace(const comem_decode_attn_plan* plan, int32_t dtype, int32_t batch, int32_t max_q_len,
+                               int64_t max_ctx_len, size_t* workspace_bytes_out) {
   const comem_decode_attn_plan* p = checked(plan);
   if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
   if (workspace_bytes_out == nullptr) return COMEM_ERR_NULL_POINTER;
   *workspace_bytes_out = 0;
-  if (p->cfg.dtype == COMEM_F32) return COMEM_ERR_UNSUPPORTED;
+  if (p->cfg.dtype != dtype) return COMEM_ERR_UNSUPPORTED;
   const comem_status st = check_bounds(*p, batch, max_q_len, max_ctx_len);
   if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
   const int64_t items =
@@ -189,15 +188,15 @@ comem_status comem_prefill_attn_workspace(const comem_decode_attn_plan* plan, in
   return COMEM_OK;
 }
 
-comem_status comem_prefill_attn_split(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
-                                      const int32_t* q_lens, int32_t max_q_len, const void* k, const void* v,
-                                      int64_t stride_token, int64_t stride_head, const int64_t* seq_start,
-                                      const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out,
-                                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+comem_status prefill_contiguous(const comem_decode_attn_plan* plan, int32_t dtype, const void* q,
+                                const int64_t* q_start, const int32_t* q_lens, int32_t max_q_len, const void* k,
+                                const void* v, int64_t stride_token, int64_t stride_head, const int64_t* seq_start,
+                                const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
   const comem_decode_attn_plan* p = checked(plan);
   if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
   comem::PrefillParams a;
-  comem_status st = prepare_prefill(*p, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head, ctx_lens,
+  comem_status st = prepare_prefill(*p, dtype, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head, ctx_lens,
                                     batch, max_ctx_len, out, lse, workspace, a);
   if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
   if (seq_start == nullptr) return COMEM_ERR_NULL_POINTER;
@@ -205,6 +204,48 @@ comem_status comem_prefill_attn_split(const comem_decode_attn_plan* plan, const 
   if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
   a.seq_start = seq_start;
   return launch_prefill(*p, a, false, batch, max_q_len, workspace, workspace_bytes, hip_stream);
+}
+
+comem_status prefill_paged(const comem_decode_attn_plan* plan, int32_t dtype, const void* q, const int64_t* q_start,
+                           const int32_t* q_lens, int32_t max_q_len, const void* k_pages, const void* v_pages,
+                           int64_t stride_page, int64_t stride_token, int64_t stride_head, int32_t page_size,
+                           int64_t num_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                           const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const comem_decode_attn_plan* p = checked(plan);
+  if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
+  comem::PrefillParams a;
+  comem_status st = prepare_prefill(*p, dtype, q, q_start, q_lens, max_q_len, k_pages, v_pages, stride_token, stride_head,
+                                    ctx_lens, batch, max_ctx_len, out, lse, workspace, a);
+  if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
+  st = validate_paged(*p, stride_page, page_size, num_pages, block_table, max_pages_per_seq, max_ctx_len);
+  if (st != COMEM_OK) return st;
+  if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
+  a.block_table = block_table;
+  a.stride_page = stride_page * elem_bytes(p->cfg);
+  a.max_pages = max_pages_per_seq;
+  a.page_shift = log2_of(page_size);
+  a.page_mask = page_size - 1;
+  a.num_pages = num_pages;
+  return launch_prefill(*p, a, true, batch, max_q_len, workspace, workspace_bytes, hip_stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+comem_status comem_prefill_attn_workspace(const comem_decode_attn_plan* plan, int32_t batch, int32_t max_q_len,
+                                          int64_t max_ctx_len, size_t* workspace_bytes_out) {
+  return prefill_workspace(plan, COMEM_BF16, batch, max_q_len, max_ctx_len, workspace_bytes_out);
+}
+
+comem_status comem_prefill_attn_split(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
+                                      const int32_t* q_lens, int32_t max_q_len, const void* k, const void* v,
+                                      int64_t stride_token, int64_t stride_head, const int64_t* seq_start,
+                                      const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return prefill_contiguous(plan, COMEM_BF16, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head,
+                            seq_start, ctx_lens, batch, max_ctx_len, out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 comem_status comem_prefill_attn(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
@@ -223,22 +264,9 @@ comem_status comem_prefill_attn_split_paged(const comem_decode_attn_plan* plan, 
                                             const int32_t* block_table, int32_t max_pages_per_seq,
                                             const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out,
                                             float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  const comem_decode_attn_plan* p = checked(plan);
-  if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
-  comem::PrefillParams a;
-  comem_status st = prepare_prefill(*p, q, q_start, q_lens, max_q_len, k_pages, v_pages, stride_token, stride_head,
-                                    ctx_lens, batch, max_ctx_len, out, lse, workspace, a);
-  if (st != COMEM_OK || prefill_is_empty(batch, max_q_len)) return st;
-  st = validate_paged(*p, stride_page, page_size, num_pages, block_table, max_pages_per_seq, max_ctx_len);
-  if (st != COMEM_OK) return st;
-  if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
-  a.block_table = block_table;
-  a.stride_page = stride_page * elem_bytes(p->cfg);
-  a.max_pages = max_pages_per_seq;
-  a.page_shift = log2_of(page_size);
-  a.page_mask = page_size - 1;
-  a.num_pages = num_pages;
-  return launch_prefill(*p, a, true, batch, max_q_len, workspace, workspace_bytes, hip_stream);
+  return prefill_paged(plan, COMEM_BF16, q, q_start, q_lens, max_q_len, k_pages, v_pages, stride_page, stride_token,
+                       stride_head, page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len,
+                       out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 comem_status comem_prefill_attn_paged(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
@@ -252,6 +280,32 @@ comem_status comem_prefill_attn_paged(const comem_decode_attn_plan* plan, const 
                                         stride_token, stride_head, page_size, num_pages, block_table,
                                         max_pages_per_seq, ctx_lens, batch, max_ctx_len, out, lse, nullptr, 0,
                                         hip_stream);
+}
+
+comem_status comem_prefill_fp8_workspace(const comem_decode_attn_plan* plan, int32_t batch, int32_t max_q_len,
+                                         int64_t max_ctx_len, size_t* workspace_bytes_out) {
+  return prefill_workspace(plan, COMEM_FP8_E4M3, batch, max_q_len, max_ctx_len, workspace_bytes_out);
+}
+
+comem_status comem_prefill_fp8_attn(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
+                                    const int32_t* q_lens, int32_t max_q_len, const void* k, const void* v,
+                                    int64_t stride_token, int64_t stride_head, const int64_t* seq_start,
+                                    const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out,
+                                    float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return prefill_contiguous(plan, COMEM_FP8_E4M3, q, q_start, q_lens, max_q_len, k, v, stride_token, stride_head,
+                            seq_start, ctx_lens, batch, max_ctx_len, out, lse, workspace, workspace_bytes, hip_stream);
+}
+
+comem_status comem_prefill_fp8_attn_paged(const comem_decode_attn_plan* plan, const void* q, const int64_t* q_start,
+                                          const int32_t* q_lens, int32_t max_q_len, const void* k_pages,
+                                          const void* v_pages, int64_t stride_page, int64_t stride_token,
+                                          int64_t stride_head, int32_t page_size, int64_t num_pages,
+                                          const int32_t* block_table, int32_t max_pages_per_seq,
+                                          const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, float* out,
+                                          float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return prefill_paged(plan, COMEM_FP8_E4M3, q, q_start, q_lens, max_q_len, k_pages, v_pages, stride_page, stride_token,
+                       stride_head, page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len,
+                       out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"
