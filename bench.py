@@ -186,7 +186,8 @@ def _short_kernel_name(full):
     """decode_mfma_queue_kernel<128, Layout 1, true> -> decode_mfma_queue_D128_paged_fp8 (and similar).
 
     A bool template argument is the FP8 switch of the MFMA decode kernels,
-    the split switch of the prefill kernel and the paged switch of the others.
+    the split, FP8 and few-rows switches of the prefill kernel (in this order)
+    and the paged switch of the others.
     """
     import re
 
@@ -196,7 +197,7 @@ def _short_kernel_name(full):
     base, args = m.group(1), m.group(2)
     parts = [x.strip() for x in re.split(r",\s*(?![^()]*\))", args)]
     name = base
-    for a in parts:
+    for i, a in enumerate(parts):
         lay = re.search(r"Layout\)(\d)", a)
         if lay:
             name += "_" + ["contig", "paged", "pagedfine"][int(lay.group(1))]
@@ -209,7 +210,7 @@ def _short_kernel_name(full):
         elif a in ("true", "false") and base.startswith("decode_mfma"):
             name += "_fp8" if a == "true" else ""
         elif a in ("true", "false") and base.startswith("prefill"):
-            name += "_split" if a == "true" else ""
+            name += {2: "_split", 3: "_fp8", 4: "_few"}[i] if a == "true" else ""
         elif a in ("true", "false"):
             name += "_paged" if a == "true" else "_contig"
     return name

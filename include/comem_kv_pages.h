@@ -108,7 +108,9 @@ comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pa
  * tokens are copied to fresh pages (taken before the old ones are given back)
  * and the old entries are given up. The keys are copied as they are: their
  * rotation remains that of the position they were made at, and the positions
- * of later tokens (comem_rope_append) are the caller's to keep.
+ * of later tokens (comem_rope_append) are the caller's to keep. This is also
+ * the way to drop a row's last tokens (its list is then the first ones): a
+ * ctx_lens entry lowered by hand would leave its pages counted.
  *   rows       device int32 [n], distinct; 0 <= n <= num_rows (0: as above).
  *   keep       device int32 [keep_total] (NULL with keep_total = 0).
  *   keep_start device int64 [n]; keep_lens device int32 [n].

@@ -19,8 +19,9 @@
  * or, with COMEM_ROPE_INTERLEAVED, the same for the pairs (y_2j, y_2j+1) in
  * the places 2j and 2j + 1. All of it is float32; q_out and the cache get the
  * result rounded once: to nearest in the plan's type, or, for FP8 caches, the
- * E4M3 code nearest to z / k_scale (and v / v_scale), magnitudes above 448
- * becoming 448 and NaN staying NaN.
+ * E4M3 code nearest to z * (1 / k_scale) (and v * (1 / v_scale)), reciprocal
+ * and product in float32, magnitudes above 448 becoming 448 and NaN staying
+ * NaN.
  *
  * Sequence b holds L_b = ctx_lens[b] tokens, of which the last M_b are the new
  * ones, as in the prefill calls (comem_prefill_attn.h): new token i becomes
@@ -81,7 +82,8 @@ typedef struct {
  *   q_start    device int64 [batch]: first row of each sequence's new tokens.
  *   q_lens     device int32 [batch]: M_b. (Both or neither may be NULL.)
  *   max_q_len  host bound >= every q_lens[b], 0 .. max_ctx_len; 1 when q_lens
- *              is NULL. With max_q_len = 0 or batch = 0 nothing is enqueued
+ *              is NULL; COMEM_ERR_INVALID_SHAPE above 2^26 - 1, what one
+ *              launch holds. With max_q_len = 0 or batch = 0 nothing is enqueued
  *              and no pointer is looked at.
  *   positions  device int32, one for each row, or NULL.
  *   q_out      [rows, h_q, d_h] dense, q's type, 16-byte aligned. May be q

@@ -30,6 +30,13 @@ comem_status check_bounds(const comem_decode_attn_plan& p, int32_t batch, int32_
   return COMEM_OK;
 }
 
+// Whether a call's blocks have so few rows that waves share a tile's keys
+// instead (FP8 caches): more than 64 rows would be two blocks of such waves,
+// each of which reads all the keys.
+bool is_narrow(const comem_decode_attn_plan& p, int64_t max_q_len) {
+  return is_fp8(p.cfg) && max_q_len * group_of(p.cfg) <= comem::kPrefillNarrowRows;
+}
+
 // Checks of a prefill call shared by both layouts; fills the kernel arguments.
 // `dtype`: the caches that the entry point is for.
 comem_status prepare_prefill(const comem_decode_attn_plan& p, int32_t dtype, const void* q, const int64_t* q_start,
@@ -58,7 +65,7 @@ comem_status prepare_prefill(const comem_decode_attn_plan& p, int32_t dtype, con
   a.stride_head = stride_head * e;
   a.num_q_heads = p.cfg.num_q_heads;
   a.group = group_of(p.cfg);
-  a.tokens_per_block = comem::kPrefillRows / a.group;
+  a.tokens_per_block = (is_narrow(p, max_q_len) ? comem::kPrefillNarrowRows : comem::kPrefillRows) / a.group;
   a.scale_log2 = p.cfg.scale * (is_fp8(p.cfg) ? p.cfg.k_scale : 1.f) * 1.4426950408889634f;
   a.out_scale = is_fp8(p.cfg) ? p.cfg.v_scale : 1.f;
   a.max_ctx = static_cast<int32_t>(max_ctx_len);
@@ -82,7 +89,8 @@ size_t split_bytes(const comem_decode_attn_plan& p, int64_t items, int64_t split
 // Unsplit blocks differ: each sees the keys up to its own last token, so the
 // units need the rounds of the largest blocks, or, where blocks are many and
 // small, an even share of all tiles and half of the difference between the
-// largest and the smallest block.
+// largest and the smallest block. Tiles of an FP8 cache take 4 to 6% longer;
+// that moves both sides of a comparison alike, so the rule is the same.
 double prefill_us(const comem_decode_attn_plan& p, int64_t pairs, int64_t blocks, int64_t max_ctx_len,
                   int64_t splits) {
   const double units = p.num_cus, block_tiles = comem::kPrefillRows / group_of(p.cfg) / 64.0;
@@ -150,7 +158,8 @@ comem_status launch_prefill(const comem_decode_attn_plan& p, const comem::Prefil
   args.splits = static_cast<int32_t>(
       plan_splits(p, batch, max_q_len, a.max_ctx, workspace == nullptr ? 0 : workspace_bytes));
   comem::PrefillKernelFn fn =
-      comem::select_prefill_kernel(p.cfg.head_dim, paged ? a.page_mask + 1 : 0, args.splits > 1, is_fp8(p.cfg));
+      comem::select_prefill_kernel(p.cfg.head_dim, paged ? a.page_mask + 1 : 0, args.splits > 1, is_fp8(p.cfg),
+                                   is_narrow(p, max_q_len));
   comem::PrefillKernelFn merge = comem::select_prefill_merge_kernel(p.cfg.head_dim);
   if (fn == nullptr || merge == nullptr) return COMEM_ERR_UNSUPPORTED;
   if (args.splits > 1) {

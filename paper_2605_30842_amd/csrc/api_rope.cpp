@@ -41,6 +41,9 @@ comem_status prepare_rope(const comem_decode_attn_plan& p, const comem_rope_conf
   if (max_ctx_len < 0 || max_ctx_len > p.cfg.max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
   if (max_q_len < 0 || max_q_len > max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
   if (rope_is_empty(batch, max_q_len)) return COMEM_OK;
+  // A wave takes a token (parts of it only where tokens are few) and a launch
+  // has less than 2^32 threads along a dimension.
+  if (max_q_len >= (1 << 26)) return COMEM_ERR_INVALID_SHAPE;
   if (is_fp8(p.cfg) && !(std::isfinite(1.f / p.cfg.k_scale) && std::isfinite(1.f / p.cfg.v_scale)))
     return COMEM_ERR_UNSUPPORTED;
   comem_status st = check_rope(p, rope);
@@ -121,7 +124,6 @@ comem_status launch_rope(const comem_decode_attn_plan& p, comem::RopeParams& a, 
       comem::select_rope_kernel(p.cfg.head_dim, cache, paged, written > (int64_t{256} << 20));
   if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
   const int64_t blocks = ceil_div(int64_t{a.max_q} * a.parts, comem::kRopeWaves);
-  if (blocks > INT32_MAX / 2) return COMEM_ERR_INVALID_SHAPE;
   void* argv[] = {&a};
   const hipError_t err =
       hipLaunchKernel(reinterpret_cast<const void*>(fn), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(batch)),

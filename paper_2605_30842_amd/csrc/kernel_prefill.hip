@@ -361,14 +361,15 @@ __device__ inline void pipeline_reads() {
 // transpose reads in the output products (measured best of 2/4, 4/8, 6/8).
 constexpr int AHEAD_K = 6, AHEAD_V = 8;
 
-// S^T = K_tile . Q^T for the 32 rows of a wave.
-template <int D, bool FP8>
+// S^T = K_tile . Q^T for the 32 rows of a wave and NSB blocks of 32 keys (the
+// tile's two, or, narrow, one: see the kernel).
+template <int D, bool FP8, int NSB>
 __device__ inline void qk_scores(const char* kt, const LaneOffsets<D, FP8>& lo, const bf16x8 (&qop)[D / 16],
-                                 f32x16 (&s)[2]) {
+                                 f32x16 (&s)[NSB]) {
   constexpr int KS = D / 16;
   constexpr int RB = D * 2;
-  s[0] = f32x16{};
-  s[1] = f32x16{};
+#pragma unroll
+  for (int sb = 0; sb < NSB; ++sb) s[sb] = f32x16{};
   if constexpr (FP8) {
     // The reduction index is a dummy: lane half h takes head_dim 32 kp + 16 h
     // .. + 16 in the steps 2 kp and 2 kp + 1, as its Q operand does.
@@ -376,7 +377,7 @@ __device__ inline void qk_scores(const char* kt, const LaneOffsets<D, FP8>& lo, 
     for (int kp = 0; kp < KS / 2; ++kp) {
       const int off = lo.k ^ (32 * kp);
 #pragma unroll
-      for (int sb = 0; sb < 2; ++sb) {
+      for (int sb = 0; sb < NSB; ++sb) {
         const u32x4 c = *reinterpret_cast<const u32x4*>(kt + off + 32 * sb * D);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -387,36 +388,37 @@ __device__ inline void qk_scores(const char* kt, const LaneOffsets<D, FP8>& lo, 
     }
     // 4 reads ahead of their products; the conversions find their own place
     // (fixing theirs too made the tile 3% slower).
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    constexpr int kReads = NSB * KS / 2, kAhead = kReads < 4 ? kReads : 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-    for (int i = 0; i < KS - 4; ++i) {
+    for (int i = 0; i < kReads - kAhead; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * kAhead, 0);
     return;
   }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int off = lo.k ^ (32 * ks);
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb) {
+    for (int sb = 0; sb < NSB; ++sb) {
       const bf16x8 kop = *reinterpret_cast<const bf16x8*>(kt + off + 32 * sb * RB);
       s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qop[ks], s[sb], 0, 0, 0);
     }
   }
-  pipeline_reads<2 * KS, AHEAD_K>();
+  pipeline_reads<NSB * KS, AHEAD_K>();
 }
 
 // Probabilities of one tile's scores against the reference exponent mb
 // (the running maximum times scale_log2), split into P^T operands; the row's
-// sum goes to psum. hook(part) runs after each quarter of the exponentials
+// sum goes to psum. hook(0 .. 3) runs spread over the parts of the exponentials
 // (tile requests placed there, kept there: requests issued back to back
 // stall the wave while the address unit drains them).
-template <bool FP8, typename Hook>
-__device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2, float& psum, PTile& pt, Hook&& hook) {
+template <bool FP8, int NSB, typename Hook>
+__device__ inline void probs_at(const f32x16 (&s)[NSB], float mb, float scale_log2, float& psum, PTile& pt, Hook&& hook) {
 #pragma unroll
-  for (int sb = 0; sb < 2; ++sb)
+  for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
       uint32_t ph[4], pl[4];
@@ -434,7 +436,12 @@ __device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2
       pt.hi[sb][s2] = u32x4{ph[0], ph[1], ph[2], ph[3]};
       pt.lo[sb][s2] = u32x4{pl[0], pl[1], pl[2], pl[3]};
       __builtin_amdgcn_sched_barrier(0);
-      hook(2 * sb + s2);
+      if constexpr (NSB == 2) {
+        hook(2 * sb + s2);
+      } else {
+        hook(2 * s2);
+        hook(2 * s2 + 1);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -452,14 +459,14 @@ __device__ inline void probs_at(const f32x16 (&s)[2], float mb, float scale_log2
 // says so and takes the probabilities again, the same steps as without the
 // first try. The common case so skips the maximum (32 comparisons, a
 // shuffle and a vote per lane).
-template <int D, bool FP8, typename Hook>
-__device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int limit, int h, float scale_log2,
+template <int D, bool FP8, int NSB, typename Hook>
+__device__ inline void softmax_probs(f32x16 (&s)[NSB], bool masked, int t0, int limit, int h, float scale_log2,
                                      float& m_run, float& l_run, f32x16 (&acc)[D / 32], PTile& pt, Hook&& hook) {
   constexpr int NT = D / 32;
   constexpr float shift = FP8 ? kProbShift : 0.f;
   if (masked) {
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb)
+    for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int t = t0 + 32 * sb + 8 * (r >> 2) + 4 * h + (r & 3);
@@ -468,12 +475,12 @@ __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int li
   }
   // The first try runs in every wave (its hook issues the tile requests).
   float psum = 0.f;
-  probs_at<FP8>(s, m_run == -INFINITY ? 0.f : m_run * scale_log2 - shift, scale_log2, psum, pt, hook);
+  probs_at<FP8, NSB>(s, m_run == -INFINITY ? 0.f : m_run * scale_log2 - shift, scale_log2, psum, pt, hook);
   const bool redo = m_run == -INFINITY || !(psum <= (FP8 ? kLazyMaxProbFp8 : kLazyMaxProb));
   if (__builtin_amdgcn_ballot_w64(redo) != 0) {
     float mt = -INFINITY;
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb)
+    for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[sb][r]);
     mt = fmaxf(mt, __shfl_xor(mt, 32));
@@ -488,7 +495,7 @@ __device__ inline void softmax_probs(f32x16 (&s)[2], bool masked, int t0, int li
     }
     const float mb = m_run == -INFINITY ? 0.f : m_run * scale_log2 - shift;
     psum = 0.f;
-    probs_at<FP8>(s, mb, scale_log2, psum, pt, [](int) {});
+    probs_at<FP8, NSB>(s, mb, scale_log2, psum, pt, [](int) {});
   }
   l_run += psum;
 }
@@ -501,12 +508,12 @@ __device__ inline f32x16 pv_product(bf16x8 v, u32x4 p, f32x16 acc) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p), acc, 0, 0, 0);
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, int NSB>
 __device__ inline void pv_accumulate(const char* vt, const LaneOffsets<D, FP8>& lo, const PTile& pt, f32x16 (&acc)[D / 32]) {
   constexpr int NT = D / 32;
   constexpr int RB = D * 2;
 #pragma unroll
-  for (int sb = 0; sb < 2; ++sb)
+  for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
       const int step = (32 * sb + 16 * s2) * RB;
@@ -519,7 +526,7 @@ __device__ inline void pv_accumulate(const char* vt, const LaneOffsets<D, FP8>& 
         acc[n] = pv_product<FP8>(vop, pt.lo[sb][s2], acc[n]);
       }
     }
-  pipeline_reads<8 * NT, AHEAD_V>();
+  pipeline_reads<4 * NSB * NT, AHEAD_V>();
 }
 
 // s_waitcnt immediate for vmcnt(n) with the other counters left alone (gfx9 encoding).
@@ -571,10 +578,18 @@ constexpr int kXcds = 8;  // XCDs of the GPU; workgroups are dealt to them round
 // SPLIT: the workgroup takes one of p.splits equal shares of the block's keys
 // and leaves a partial result. A form of its own, since the extra scalars
 // spill and cost an unsplit call 0.6%.
-template <int D, PLayout LAYOUT, bool SPLIT, bool FP8>
+//
+// NARROW (FP8 caches): blocks of at most 64 rows, a few new tokens. Waves 0
+// and 1 of a half take their 32 rows over the first 32 keys of every tile,
+// waves 2 and 3 the same rows over the other 32, so a stage is half as long;
+// their states are merged at the end like the halves'. Four sequences of 16
+// new tokens over 12000, G = 4: 50.7 us wide, 42.0 narrow; of 1 to 16 over 2K
+// to 12K 41.0 and 35.6. What is left of a stage is the tile's loads and waits.
+template <int D, PLayout LAYOUT, bool SPLIT, bool FP8, bool NARROW>
 __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const PrefillParams p) {
   constexpr int KS = D / 16;
   constexpr int NT = D / 32;
+  constexpr int NSB = NARROW ? 1 : 2;  // blocks of 32 keys of a tile that a wave takes
   constexpr bool PAGED = LAYOUT != PLayout::kContig;
   constexpr int KB = FP8 ? D : D * 2;  // bytes of a K row in LDS
   using KLoader = TileLoader<KB, LAYOUT, false>;
@@ -633,7 +648,8 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   const int w = wv & 3;   // row group of the wave
   const int kh = wv >> 2; // key half of the wave
   const int j = lane & 31, h = lane >> 5;
-  const int row = 32 * w + j;
+  const int sub = NARROW ? w >> 1 : 0;  // the first of them
+  const int row = 32 * (NARROW ? w & 1 : w) + j;
   const int g = row / TB;
   const int i = i0 + row % TB;  // new-token index of the lane's row
   const int ic = min(i, M - 1);  // padded rows repeat the last token; never stored
@@ -749,11 +765,11 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
   }
   __syncthreads();
 
-  f32x16 s[2];  // scores of a tile between its M and V stages
+  f32x16 s[NSB];  // scores of a tile between its M and V stages
   PTile pt;     // probabilities of a tile between its V stage and the next M stage
   auto m_stage = [&](const LdsTile<KB>& kcur, const LdsTile<D * 2>& vprev, int c) {
-    if (c >= 1 && c <= t_count) pv_accumulate<D, FP8>(vprev.b, lo, pt, acc);
-    if (c < t_count) qk_scores<D, FP8>(kcur.b, lo, qop, s);
+    if (c >= 1 && c <= t_count) pv_accumulate<D, FP8, NSB>(vprev.b + sub * (32 * D * 2), lo, pt, acc);
+    if (c < t_count) qk_scores<D, FP8, NSB>(kcur.b + sub * (32 * KB), lo, qop, s);
     if constexpr (FP8) wait_lds();  // the next stage stores into what this one read
   };
   // Every V stage requests two tiles (past the half's range they are
@@ -781,7 +797,7 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
         const auto kq = kl.tile_req(kl.kbase, TK * (t + 2), kpg);
         pg_v = ld.pages_of(TK * (t + 3));
         kpg = k_pages(TK * (t + 3));
-        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
+        softmax_probs<D, FP8, NSB>(s, t >= nfree, TK * t + 32 * sub, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
 #pragma unroll
           for (int u = part * NI / 4; u < (part + 1) * NI / 4; ++u) {
             put_v(vst.b, u);
@@ -808,10 +824,10 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
           ld.issue(rv, vslot, u);
           ld.issue(rk, kslot, u);
         }
-        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [](int) {});
+        softmax_probs<D, FP8, NSB>(s, t >= nfree, TK * t + 32 * sub, limit, h, p.scale_log2, m_run, l_run, acc, pt, [](int) {});
       } else {
         // Instructions spread over the four parts of the exponentials.
-        softmax_probs<D, FP8>(s, t >= nfree, TK * t, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
+        softmax_probs<D, FP8, NSB>(s, t >= nfree, TK * t + 32 * sub, limit, h, p.scale_log2, m_run, l_run, acc, pt, [&](int part) {
 #pragma unroll
           for (int u = part * NI / 4; u < (part + 1) * NI / 4; ++u) {
             ld.issue(rv, vslot, u);
@@ -850,9 +866,11 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     ml[w * 64 + lane] = m_run;
     ml[256 + w * 64 + lane] = l_run;
   }
-  for (int pass = 0; pass < 2; ++pass) {
+  // The state of the wave `from` (ml[from], accumulators in its slot) goes to
+  // the wave that `takes`.
+  auto merge = [&](bool gives, bool takes, int from) {
     float4* st = reinterpret_cast<float4*>(FP8 ? vs1[w & 1].b : ks0[w & 1].b);  // [4 NT][64 lanes]
-    if (kh == 1 && (w >> 1) == pass) {
+    if (gives) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -860,13 +878,14 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
           st[(4 * n + r4) * 64 + lane] = make_float4(acc[n][4 * r4], acc[n][4 * r4 + 1], acc[n][4 * r4 + 2], acc[n][4 * r4 + 3]);
     }
     __syncthreads();
-    if (kh == 0 && (w >> 1) == pass) {
-      const float m1 = ml[w * 64 + lane];
-      const float l1 = ml[256 + w * 64 + lane];
+    if (takes) {
+      const float m1 = ml[from * 64 + lane];
+      const float l1 = ml[256 + from * 64 + lane];
       // Of an unsplit call half 0 holds key 0, which every row sees; a later
-      // split may hold no key that the row sees at all.
+      // split, or the second keys of a narrow block's tiles, may hold no key
+      // that the row sees at all.
       const float mn = fmaxf(m_run, m1);
-      const float a0 = SPLIT && m_run == -INFINITY ? 0.f : fast_exp2((m_run - mn) * p.scale_log2);
+      const float a0 = (SPLIT || NARROW) && m_run == -INFINITY ? 0.f : fast_exp2((m_run - mn) * p.scale_log2);
       const float a1 = m1 == -INFINITY ? 0.f : fast_exp2((m1 - mn) * p.scale_log2);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -882,8 +901,21 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
       m_run = mn;
     }
     __syncthreads();
+  };
+  for (int pass = 0; pass < 2; ++pass) {
+    const bool now = (w >> 1) == pass;
+    merge(kh == 1 && now, kh == 0 && now, w);
   }
-  if (kh == 1) return;
+  if (kh == 1 && !NARROW) return;
+  if constexpr (NARROW) {
+    // Waves 2 and 3 of half 0 hold the second keys' states.
+    if (kh == 0 && sub == 1) {
+      ml[w * 64 + lane] = m_run;
+      ml[256 + w * 64 + lane] = l_run;
+    }
+    merge(kh == 0 && sub == 1, kh == 0 && sub == 0, w + 2);
+    if (kh == 1 || sub == 1) return;
+  }
   if (i >= M) return;
   float inv = (FP8 ? p.out_scale : 1.f) / l_run;
   const float lse2 = m_run * p.scale_log2 + log2f(l_run) - (FP8 ? kProbShift : 0.f);
@@ -922,6 +954,7 @@ __global__ __launch_bounds__(kPrefillMergeThreads) void prefill_merge_kernel(con
   const int q = blockIdx.x / kGroups, hk = blockIdx.y, b = blockIdx.z;
   const int row0 = (blockIdx.x % kGroups) * kPrefillMergeRows;
   const int TB = p.tokens_per_block;
+  if (row0 >= TB * p.group) return;  // a narrow block has 64 rows
   const int L = min(max(p.ctx_lens[b], 0), p.max_ctx);
   const int M = min(max(p.q_lens[b], 0), min(L, p.max_q));
   const int nblk = (M + TB - 1) / TB;
@@ -974,11 +1007,13 @@ __global__ __launch_bounds__(kPrefillMergeThreads) void prefill_merge_kernel(con
 
 // Every form the host may launch, instantiated explicitly (clang emitted the
 // host launch stubs of only some of the instantiations referenced below).
-#define COMEM_PREFILL_FORMS(D, L)                                                                 \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, false>(const PrefillParams); \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, false>(const PrefillParams);  \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, true>(const PrefillParams);  \
-  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, true>(const PrefillParams);
+#define COMEM_PREFILL_FORMS(D, L)                                                                        \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, false, false>(const PrefillParams); \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, false, false>(const PrefillParams);  \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, true, false>(const PrefillParams);  \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, true, false>(const PrefillParams);   \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, false, true, true>(const PrefillParams);   \
+  template __global__ void prefill_mfma_kernel<D, PLayout::L, true, true, true>(const PrefillParams);
 COMEM_PREFILL_FORMS(128, kContig)
 COMEM_PREFILL_FORMS(128, kPaged)
 COMEM_PREFILL_FORMS(128, kPagedFine)
@@ -991,14 +1026,14 @@ template __global__ void prefill_merge_kernel<64>(const PrefillParams);
 
 }  // namespace
 
-template <int D, bool SPLIT, bool FP8>
+template <int D, bool SPLIT, bool FP8, bool NARROW>
 PrefillKernelFn prefill_by_layout(int page_size) {
   // page_size 0: contiguous cache. A paged cache takes the per-group path when
   // a wave's 16-row group of a tile fits in a page (it starts at a multiple of
   // 16 for either head_dim).
-  PrefillKernelFn fn = prefill_mfma_kernel<D, PLayout::kPagedFine, SPLIT, FP8>;
-  if (page_size == 0) fn = prefill_mfma_kernel<D, PLayout::kContig, SPLIT, FP8>;
-  else if (page_size >= 16) fn = prefill_mfma_kernel<D, PLayout::kPaged, SPLIT, FP8>;
+  PrefillKernelFn fn = prefill_mfma_kernel<D, PLayout::kPagedFine, SPLIT, FP8, NARROW>;
+  if (page_size == 0) fn = prefill_mfma_kernel<D, PLayout::kContig, SPLIT, FP8, NARROW>;
+  else if (page_size >= 16) fn = prefill_mfma_kernel<D, PLayout::kPaged, SPLIT, FP8, NARROW>;
   return fn;
 }
 
@@ -1006,15 +1041,18 @@ PrefillKernelFn select_prefill_merge_kernel(int head_dim) {
   return head_dim == 128 ? prefill_merge_kernel<128> : (head_dim == 64 ? prefill_merge_kernel<64> : nullptr);
 }
 
-template <int D>
-PrefillKernelFn prefill_by_cache(int page_size, bool split, bool fp8) {
-  if (fp8) return split ? prefill_by_layout<D, true, true>(page_size) : prefill_by_layout<D, false, true>(page_size);
-  return split ? prefill_by_layout<D, true, false>(page_size) : prefill_by_layout<D, false, false>(page_size);
+template <int D, bool SPLIT>
+PrefillKernelFn prefill_by_cache(int page_size, bool fp8, bool narrow) {
+  if (!fp8) return prefill_by_layout<D, SPLIT, false, false>(page_size);
+  return narrow ? prefill_by_layout<D, SPLIT, true, true>(page_size)
+                : prefill_by_layout<D, SPLIT, true, false>(page_size);
 }
 
-PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8) {
-  if (head_dim == 128) return prefill_by_cache<128>(page_size, split, fp8);
-  if (head_dim == 64) return prefill_by_cache<64>(page_size, split, fp8);
+PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8, bool narrow) {
+  if (head_dim == 128)
+    return split ? prefill_by_cache<128, true>(page_size, fp8, narrow) : prefill_by_cache<128, false>(page_size, fp8, narrow);
+  if (head_dim == 64)
+    return split ? prefill_by_cache<64, true>(page_size, fp8, narrow) : prefill_by_cache<64, false>(page_size, fp8, narrow);
   return nullptr;
 }
 

@@ -8,6 +8,7 @@ namespace comem {
 
 constexpr int kPrefillThreads = 512;  // 8 waves: two halves of the key tiles, 4 waves each
 constexpr int kPrefillRows = 128;     // (query token, query head) rows per workgroup: 32 per wave
+constexpr int kPrefillNarrowRows = 64;
 constexpr int kPrefillTileKeys = 64;  // keys per K/V tile staged in LDS
 
 // Offsets and strides are in bytes.
@@ -30,7 +31,7 @@ struct PrefillParams {
   int32_t page_mask;
   int32_t num_q_heads;
   int32_t group;               // G = Hq / Hkv
-  int32_t tokens_per_block;    // kPrefillRows / G new tokens per workgroup
+  int32_t tokens_per_block;    // kPrefillRows (narrow: kPrefillNarrowRows) / G new tokens per workgroup
   float scale_log2;            // scale * log2(e), times the K scale of an FP8 cache
   float out_scale;             // FP8 caches: multiplies every output (the V scale)
   int32_t max_ctx;             // ctx_lens[b] is clamped to [0, max_ctx]
@@ -43,8 +44,9 @@ struct PrefillParams {
 };
 
 using PrefillKernelFn = void (*)(PrefillParams);
-// page_size 0 selects the contiguous-cache kernel.
-PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8);
+// page_size 0 selects the contiguous-cache kernel. narrow (FP8 caches): blocks
+// of at most kPrefillNarrowRows rows.
+PrefillKernelFn select_prefill_kernel(int head_dim, int page_size, bool split, bool fp8, bool narrow);
 
 constexpr int kPrefillMergeThreads = 256;
 constexpr int kPrefillMergeRows = 16;  // rows per workgroup of the merge kernel

@@ -155,6 +155,18 @@ def test_keys_shared_by_workgroups(page, lens, new, d):
     assert not torch.equal(split, whole)
 
 
+@pytest.mark.parametrize("most", [0, 1])
+@pytest.mark.parametrize("page", [0, 16, 2])
+@pytest.mark.parametrize("group,d", [(1, 128), (4, 128), (8, 128), (4, 64), (16, 64)])
+def test_few_rows(group, d, page, most):
+    """Blocks of at most 64 rows and, with one more token, of more: contexts whose last tile ends in its first or its
+    second 32 keys, sequences without a new token, single tokens, and rows that see no key of a tile's second part."""
+    m = 64 // group + most
+    lens = [m, 32, 33, 63, 64, 65, 96 + m, 97, 1000, 0, 5, 2048 + m // 2]
+    new = [min(n, k) for n, k in zip(lens, [m, 1, m, m, 2, m, m, 1, m, 0, 1, m])]
+    Case(lens, new, hq=2 * group, d=d, page=page, seed=10 * group + most).check("few rows")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_one_new_token_is_a_decode_step(d):
     c = Case([700, 1, 64, 3000], [1, 1, 1, 1], d=d, page=16, k_scale=0.011, v_scale=0.03, seed=5)

@@ -210,3 +210,10 @@ def test_plain_form_is_a_rotation():
         assert np.array_equal(y[..., 32:], x[..., 32:])
     z, _ = rotated(x, np.ones(64), 0.0, once[:, :0], np.arange(5), False)
     assert np.allclose((z * z).mean(-1), 1.0)
+
+
+def test_most_tokens_of_a_launch():
+    p = _plan(max_ctx_len=1 << 27)
+    for tokens, status in (((1 << 26) - 1, B.ERR_NO_DEVICE), (1 << 26, B.ERR_INVALID_SHAPE)):
+        assert _call(p, max_q_len=tokens, max_ctx_len=1 << 27) == status
+    B.comem_decode_attn_destroy(p)
