@@ -10,6 +10,16 @@
 // Fork and compact calls then edit the tables and move tokens in one more
 // launch: an item's first workgroup the tables, the others the tokens. The
 // counts of given-up pages go down only there, after every look for free ones.
+//
+// Measured. A launch that only edits tables is its round trips to memory:
+// page_release 3 to 4.5 us, page_find 4 to 4.7, page_give 4.8 (reserve), 5.7
+// (fork), 7.2 over five chunks. A release and two reserves of 64 rows over
+// 40960 pages took 38.9 us where one workgroup looked at all of them, 22.6
+// with a workgroup per chunk; of 8 rows over one chunk 28.6 with a separate
+// find, 19.9 without. The copies: fork, the last pages of 32 rows over 4
+// layers (40 MB read and written) 10 us; compact, one row to 5471 tokens (37
+// MB) 10.4 us, eight rows to 6800 over 4 layers (0.79 GB) 154 us, 5.2 TB/s,
+// the rate of a large copy.
 #include "kv_pages.h"
 
 namespace comem {

@@ -10,14 +10,14 @@
 // D / 16 lanes take a head, 16 elements each, 8 and 8, so that both elements
 // of every rotated pair are in one lane and every access is 16 bytes wide
 // (8 bytes for codes). The sum of squares crosses the head's lanes by
-// data-parallel moves. A wave's lanes so hold 8 (16) heads of one token in a pass and keep the position's
-// cosines and sines, which are 2 to 4 times as large as a head, in registers
-// over all passes; kRopeBatch passes' rows are in flight together. The new
-// rows are read past the caches, once and for all (16384 tokens of 32 + 16
-// bf16 heads of 128: 86 -> 71 us, 1024: 9.3 -> 8.2).
+// data-parallel moves. A wave's lanes so hold 8 (16) heads of one token in a
+// pass and keep the position's cosines and sines, which are 2 to 4 times as
+// large as a head, in registers over all passes; kRopeBatch passes' rows are
+// in flight together. The new rows are read past the caches, once and for all
+// (16384 tokens of 32 + 16 bf16 heads of 128: 86 -> 71 us, 1024: 9.3 -> 8.2).
 //
-// Memory bounds it: 5.5-5.8 TB/s of reads and writes from 8192 tokens on,
-// where a copy of the same size reaches 5.1-5.8; below, the launch and the
+// Memory bounds it: 5.5 to 6 TB/s of reads and writes from 8192 tokens on,
+// where a copy of the same size reaches 5.1 to 5.8; below, the launch and the
 // chain of length, block-table entry and rows.
 #include <type_traits>
 
@@ -135,8 +135,10 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
     e0 = p.rot_dim + 8 * (j - turned_lanes);
     e1 = e0 + (D - p.rot_dim) / 2;
   }
-  // Interleaved: 4 angles for each piece that is rotated, else of angle 0.
-  f32x8 c = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, s{};
+  // Interleaved: 4 angles for each piece that is rotated. (A piece that is not
+  // is left out of the rotation: an infinity times a sine of 0 is NaN.)
+  const bool turn0 = p.interleaved != 0 && e0 < p.rot_dim, turn1 = p.interleaved != 0 && e1 < p.rot_dim;
+  f32x8 c{}, s{};
   if (p.rot_dim > 0) {
     const int32_t pos = min(max(p.positions == nullptr ? t : p.positions[row], 0), p.num_positions - 1);
     const float* angles = p.cos_sin + static_cast<int64_t>(pos) * p.rot_dim;
@@ -145,11 +147,11 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
       c = load8(angles + 8 * j);
       s = load8(angles + half + 8 * j);
     } else if (p.interleaved != 0) {
-      if (e0 < p.rot_dim) {
+      if (turn0) {
         c.lo = load4(angles + e0 / 2);
         s.lo = load4(angles + half + e0 / 2);
       }
-      if (e1 < p.rot_dim) {
+      if (turn1) {
         c.hi = load4(angles + e1 / 2);
         s.hi = load4(angles + half + e1 / 2);
       }
@@ -206,10 +208,11 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float a0 = x0[2 * e], a1 = x1[2 * e];
-            x0[2 * e] = a0 * c[e] - x0[2 * e + 1] * s[e];
-            x0[2 * e + 1] = x0[2 * e + 1] * c[e] + a0 * s[e];
-            x1[2 * e] = a1 * c[e + 4] - x1[2 * e + 1] * s[e + 4];
-            x1[2 * e + 1] = x1[2 * e + 1] * c[e + 4] + a1 * s[e + 4];
+            const float b0 = x0[2 * e + 1], b1 = x1[2 * e + 1];
+            x0[2 * e] = turn0 ? a0 * c[e] - b0 * s[e] : a0;
+            x0[2 * e + 1] = turn0 ? b0 * c[e] + a0 * s[e] : b0;
+            x1[2 * e] = turn1 ? a1 * c[e + 4] - b1 * s[e + 4] : a1;
+            x1[2 * e + 1] = turn1 ? b1 * c[e + 4] + a1 * s[e + 4] : b1;
           }
         }
       }

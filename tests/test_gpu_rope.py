@@ -328,6 +328,23 @@ def test_nan_and_infinity_stay_in_their_head():
     assert torch.equal(got[mask.to(DEV)], clean[mask.to(DEV)])
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,d,rot", [("bf16", 128, 32), ("bf16", 64, 16), ("f32", 128, 80), ("bf16", 128, 0)])
+def test_infinity_beside_the_rotation_stays_in_its_place(dtype, d, rot, interleaved):
+    """An element that is not rotated meets no other one: an infinity or a NaN there is passed on alone."""
+    c = Case(dtype=dtype, d=d, lens=(40,), new=[9], rot=rot, norm=(False, False), interleaved=interleaved, page=0)
+    clean = c.call()
+    k = c.k.clone()
+    for at, x in ((rot, float("inf")), (rot + 3, float("nan")), (d - 1, float("-inf"))):
+        c.q[:, :, at] = x
+        c.new_k[:, :, at] = x
+        clean[:9, :, at] = x
+        k[[s for _, s, _ in c.tokens()], :, at] = x
+    got = c.call()
+    for out, want in ((got[:9], clean[:9]), (c.k, k)):
+        assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.nan_to_num(1.0), want.nan_to_num(1.0))
+
+
 def test_zero_rows_and_zero_heads():
     """A head of zeros stays zero (eps > 0)."""
     c = Case("f32", 4, 2, 64, 0, lens=(6,), new=(6,))
