@@ -978,10 +978,10 @@ class DecodeAttention:
 
         tensor, dev, d = torch.Tensor, self._torch_device, self.head_dim
         at = dev.index if dev.type == "cuda" else -1
-        # The call of a decode step in one expression; everything else, and what is wrong, in _check_rope.
+        # The common call in one expression; everything else, and what is wrong, in _check_rope.
         fast, rows_stride = False, None
-        if (q_lens is None and q_start is None and isinstance(q, tensor) and isinstance(new_k, tensor)
-                and isinstance(new_v, tensor) and isinstance(cos_sin, tensor)):
+        if (isinstance(q, tensor) and isinstance(new_k, tensor) and isinstance(new_v, tensor)
+                and isinstance(cos_sin, tensor) and isinstance(ctx_lens, tensor)):
             shape, strides = q.shape, (q.stride(), new_k.stride(), new_v.stride())
             dtype, inner = q.dtype, (d, 1)
             fast = (len(shape) == 3 and shape[1] == self.num_q_heads and shape[2] == d and dtype in self._q_dtypes
@@ -996,6 +996,12 @@ class DecodeAttention:
                     and (k_weight is None or (isinstance(k_weight, tensor) and k_weight.dtype is dtype
                                               and k_weight.get_device() == at and k_weight.shape == (d,)
                                               and k_weight.is_contiguous()))
+                    and (q_lens is q_start is None
+                         or (isinstance(q_lens, tensor) and q_lens.dtype is torch.int32 and q_lens.get_device() == at
+                             and isinstance(q_start, tensor) and q_start.dtype is torch.int64
+                             and q_start.get_device() == at and ctx_lens.dim() == 1
+                             and q_lens.shape == q_start.shape == ctx_lens.shape
+                             and q_lens.is_contiguous() and q_start.is_contiguous()))
                     and (positions is None or _fits(positions, tensor, (torch.int32,), dev, shape[:1]))
                     and (q_out is None or _fits(q_out, tensor, (dtype,), dev, shape)))
             rows_stride = strides[0][:1] + strides[1][:1] + strides[2][:1]

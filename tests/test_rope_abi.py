@@ -190,6 +190,21 @@ def test_wrapper_refuses(op, change):
         op.rope_append(**dict(_good(), **change))
 
 
+@pytest.mark.parametrize("change", [
+    dict(q_start=None), dict(q_lens=None), dict(q_start=torch.zeros(3, dtype=torch.int32)),
+    dict(q_lens=torch.ones(3, dtype=torch.int64)), dict(q_start=torch.zeros(2, dtype=torch.int64)),
+    dict(q_lens=torch.ones(4, dtype=torch.int32)), dict(q_lens=torch.ones(6, dtype=torch.int32)[::2]),
+    dict(q_start=torch.zeros(3, 1, dtype=torch.int64)), dict(q_lens=[1, 1, 1]), dict(ctx_lens=None),
+    dict(ctx_lens=torch.tensor(1, dtype=torch.int32)), dict(ctx_lens=torch.ones(3, 1, dtype=torch.int32)),
+    dict(positions=torch.zeros(3, dtype=torch.int32)), dict(new_k=torch.zeros(3, 2, 64, dtype=torch.bfloat16)),
+    dict(q_out=torch.zeros(3, 8, 64, dtype=torch.bfloat16)),
+], ids=lambda c: next(iter(c)))
+def test_wrapper_refuses_chunks(op, change):
+    chunk = dict(q_start=torch.zeros(3, dtype=torch.int64), q_lens=torch.ones(3, dtype=torch.int32), max_q_len=4)
+    with pytest.raises(ValueError):
+        op.rope_append(**dict(_good(rows=7), **dict(chunk, **change)))
+
+
 # ------------------------------------------------------------ the plain form
 
 
