@@ -910,8 +910,8 @@ class DecodeAttention:
                 int(max_ctx_len), out.data_ptr(), None if lse is None else lse.data_ptr())
         ws = self._prefill_workspace(ctx_lens.shape[0], int(max_q_len), int(max_ctx_len), stream, workspace)
         if self.dtype == "fp8":
-            comem_prefill_fp8_attn(*args, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
-                                   self._stream(stream))
+            _call_on(self, stream, comem_prefill_fp8_attn, *args, None if ws is None else ws.data_ptr(),
+                     0 if ws is None else ws.nbytes)
         elif ws is None:
             comem_prefill_attn(*args, self._stream(stream))
         else:
@@ -931,8 +931,8 @@ class DecodeAttention:
                 ctx_lens.shape[0], int(max_ctx_len), out.data_ptr(), None if lse is None else lse.data_ptr())
         ws = self._prefill_workspace(ctx_lens.shape[0], int(max_q_len), int(max_ctx_len), stream, workspace)
         if self.dtype == "fp8":
-            comem_prefill_fp8_attn_paged(*args, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
-                                         self._stream(stream))
+            _call_on(self, stream, comem_prefill_fp8_attn_paged, *args, None if ws is None else ws.data_ptr(),
+                     0 if ws is None else ws.nbytes)
         elif ws is None:
             comem_prefill_attn_paged(*args, self._stream(stream))
         else:

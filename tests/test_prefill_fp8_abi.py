@@ -113,3 +113,27 @@ def test_wrapper_takes_the_entry_of_its_cache(monkeypatch, dtype, names):
     with pytest.raises(ValueError):
         o.prefill(q.float(), *lens, torch.zeros(9, 2, 64, dtype=cache), torch.zeros(9, 2, 64, dtype=cache),
                   torch.zeros(1, dtype=i64), torch.ones(1, dtype=i32), 9)
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_the_plans_device_is_current_during_a_call(monkeypatch, current):
+    """A call on a plan of another device switches to it (its current stream is asked for there) and back."""
+    now, seen = [current], []
+
+    class On:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.index
+
+        def __exit__(self, *a):
+            now[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 100 + index, raising=False)
+    o = object.__new__(B.DecodeAttention)
+    o.device, o._torch_device = 1, torch.device("cuda:1")
+    B._call_on(o, None, lambda *a: seen.append((now[0], *a)), "x", 7)
+    assert seen == [(1, "x", 7, 101)] and now == [current]
