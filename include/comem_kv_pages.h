@@ -92,9 +92,9 @@ comem_status comem_kv_reserve(const comem_decode_attn_plan* plan, const comem_kv
  * it holds the parent's whole pages too, and of a last, partly filled one a
  * copy in a page of its own (K and V of its tokens, every layer; the rest of
  * that page is left as it was). A parent may be named several times. Children
- * are distinct rows, empty (ctx_lens 0) before the call; a child that is not
- * empty, a row outside [0, num_rows) or a row as its own child leaves that
- * pair out.
+ * are empty (ctx_lens 0) before the call; a child that is not empty or stands
+ * earlier in the list, a row outside [0, num_rows) or a row as its own child
+ * leaves that pair out.
  *   parents, children  device int32 [n], 0 <= n <= num_rows (0: nothing is
  *              enqueued, *missing is not written and no pointer looked at). */
 comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* parents,
@@ -111,11 +111,12 @@ comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pa
  * of later tokens (comem_rope_append) are the caller's to keep. This is also
  * the way to drop a row's last tokens (its list is then the first ones): a
  * ctx_lens entry lowered by hand would leave its pages counted.
- *   rows       device int32 [n], distinct; 0 <= n <= num_rows (0: as above).
+ *   rows       device int32 [n]; 0 <= n <= num_rows (0: as above).
  *   keep       device int32 [keep_total] (NULL with keep_total = 0).
  *   keep_start device int64 [n]; keep_lens device int32 [n].
- * A row outside [0, num_rows), one with more kept tokens than it has, or with
- * a list outside [0, keep_total) is left as it is. A listed position outside
+ * A row outside [0, num_rows), one that stands earlier in rows, one with more
+ * kept tokens than it has, or with a list outside [0, keep_total) is left as
+ * it is (of a row named twice the first list counts). A listed position outside
  * the row's tokens is taken as the nearest one. */
 comem_status comem_kv_compact(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* rows,
                               const int32_t* keep, int64_t keep_total, const int64_t* keep_start,

@@ -1132,7 +1132,8 @@ class KVPages:
         return missing
 
     def fork(self, parents, children, missing=None, stream=None):
-        """Empty rows children[i] become second sequences on the tokens of parents[i] (int32 [n], children distinct)."""
+        """Empty rows children[i] become second sequences on the tokens of parents[i] (int32 [n]; of a child named twice
+        the first pair counts)."""
         src = self._list("parents", parents)
         dst = self._list("children", children, shape=parents.shape)
         missing = self._missing(missing, stream)
@@ -1143,7 +1144,7 @@ class KVPages:
         return missing
 
     def compact(self, rows, keep, keep_start, keep_lens, missing=None, stream=None):
-        """Cut rows[i] (int32 [n], distinct) to the tokens keep[keep_start[i] : keep_start[i] + keep_lens[i]] of it,
+        """Cut rows[i] (int32 [n]; of a row named twice the first counts) to the tokens keep[keep_start[i] : keep_start[i] + keep_lens[i]] of it,
         strictly increasing positions (keep int32, keep_start int64 [n], keep_lens int32 [n])."""
         import torch
 

@@ -28,7 +28,7 @@ comem_status check_state(const comem_decode_attn_plan& p, const comem_kv_pages* 
   if (s->max_pages_per_seq <= 0 || s->max_pages_per_seq < ceil_div(s->max_ctx_len, s->page_size))
     return COMEM_ERR_INVALID_SHAPE;
   if (s->refcounts == nullptr || s->block_table == nullptr || s->ctx_lens == nullptr) return COMEM_ERR_NULL_POINTER;
-  if (!aligned(s->refcounts, 16) || !aligned(s->block_table, 4) || !aligned(s->ctx_lens, 4))
+  if (!aligned(s->refcounts, 4) || !aligned(s->block_table, 4) || !aligned(s->ctx_lens, 4))
     return COMEM_ERR_MISALIGNED;
   return COMEM_OK;
 }

@@ -96,15 +96,19 @@ __device__ inline int64_t block_scan(int64_t x, NeedSums& sums, int64_t& total) 
   return (static_cast<int64_t>(hi_before + hi - high) << kLowBits) + (lo_before + lo - low);
 }
 
-// Free pages of chunk `chunk` as wave masks: bit l of mask k of a wave is page
-// 64 (16 w' + k) + l of the chunk, w' the wave's place. Returns the wave's count.
+// A thread's reference counts of a chunk, and the wave's free pages as masks:
+// bit l of mask k of a wave is page 64 (kMasks w' + k) + l of the chunk, w' the
+// wave's place. (Two steps, so that the counts can be on their way early.)
 constexpr int kMasks = kChunkPages / kPageThreads;
-__device__ inline int free_masks(const PageParams& p, int chunk, uint64_t (&mask)[kMasks]) {
+__device__ inline void load_counts(const PageParams& p, int chunk, int32_t (&x)[kMasks]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t c0 = static_cast<int64_t>(chunk) * kChunkPages + w * (64 * kMasks) + lane;
-  int32_t x[kMasks];
 #pragma unroll
   for (int k = 0; k < kMasks; ++k) x[k] = c0 + 64 * k < p.num_pages ? p.refcounts[c0 + 64 * k] : 1;
+}
+
+// Returns the wave's count.
+__device__ inline int free_masks(const int32_t (&x)[kMasks], uint64_t (&mask)[kMasks]) {
   int count = 0;
 #pragma unroll
   for (int k = 0; k < kMasks; ++k) {
@@ -122,15 +126,33 @@ __device__ inline Item read_item(const PageParams& p, int i) {
   return Item{p.items.row[i], p.items.grown[i], p.items.first[i], p.items.need[i]};
 }
 
-// Item i of a reserve or fork call.
+// Whether a list names x = list[i] at a place before i, for the workgroup's
+// i = i0 + thread together: earlier entries pass through LDS.
+__device__ inline bool named_before(const int32_t* list, int x, int i0, int n) {
+  __shared__ int32_t names[kPageThreads];
+  const int tid = threadIdx.x, i = i0 + tid;
+  bool found = false;
+  for (int j0 = 0; j0 <= i0; j0 += kPageThreads) {
+    const int y = j0 == i0 ? x : list[j0 + tid];
+    __syncthreads();
+    names[tid] = y;
+    __syncthreads();
+    const int end = i >= n ? 0 : j0 == i0 ? tid : kPageThreads;
+#pragma unroll 8
+    for (int k = 0; k < end; ++k) found |= names[k] == x;
+  }
+  return found;
+}
+
+// Item i of a reserve or fork call, all of whose threads come here together
+// with i = i0 + thread.
 template <PageOp OP>
-__device__ inline Item find_item(const PageParams& p, int i) {
+__device__ inline Item find_item(const PageParams& p, int i0) {
+  const int i = i0 + static_cast<int>(threadIdx.x);
   Item item{-1, -1, 0, 0};
-  int from = -1;
-  int64_t len = -1;
   if constexpr (OP == PageOp::kReserve) {
-    const int64_t add = p.add_lens[i];
-    len = p.ctx_lens[i];
+    if (i >= p.n) return Item{};
+    const int64_t add = p.add_lens[i], len = p.ctx_lens[i];
     if (len >= 0 && add >= 0 && len + add <= p.max_ctx) {
       item.row = i;
       item.grown = static_cast<int>(len + add);
@@ -138,18 +160,21 @@ __device__ inline Item find_item(const PageParams& p, int i) {
       item.need = pages_for(len + add, p.page_shift) - item.first;
     }
   } else {
-    const int child = p.children[i];
-    from = p.rows[i];
-    if (from >= 0 && from < p.num_rows && child >= 0 && child < p.num_rows && child != from && p.ctx_lens[child] == 0)
-      len = p.ctx_lens[from];
-    if (len >= 0 && len <= p.max_ctx) {
+    const int child = i < p.n ? p.children[i] : -1, from = i < p.n ? p.rows[i] : -1;
+    const bool rows = from >= 0 && from < p.num_rows && child >= 0 && child < p.num_rows && child != from;
+    // On their way while the list is looked through.
+    const int64_t child_len = p.ctx_lens[rows ? child : 0], from_len = p.ctx_lens[rows ? from : 0];
+    const bool again = named_before(p.children, child, i0, p.n);
+    if (i >= p.n) return Item{};
+    const bool taken = rows && !again && child_len == 0 && from_len >= 0 && from_len <= p.max_ctx;
+    if (taken) {
       item.row = child;
-      item.grown = static_cast<int>(len);
-      item.first = static_cast<int>(len >> p.page_shift);
-      item.need = pages_for(len, p.page_shift) - item.first;
+      item.grown = static_cast<int>(from_len);
+      item.first = static_cast<int>(from_len >> p.page_shift);
+      item.need = pages_for(from_len, p.page_shift) - item.first;
     }
     p.items.from[i] = from;
-    p.items.len[i] = static_cast<int32_t>(len);
+    p.items.len[i] = taken ? static_cast<int32_t>(from_len) : -1;
   }
   p.items.row[i] = item.row;
   p.items.grown[i] = item.grown;
@@ -167,11 +192,13 @@ __device__ inline void find_cut(const PageParams& p, int i) {
   const int r = p.rows[i];
   const int64_t n = p.keep_lens[i], start = p.keep_start[i];
   if (threadIdx.x == 0) first_moved = INT32_MAX;
-  __syncthreads();
+  bool again = false;
+  for (int j = threadIdx.x; j < i; j += kPageThreads) again |= p.rows[j] == r;
+  again = __syncthreads_or(again) != 0;
   // The list, the row's length and its entries (as many as a row can have)
   // are asked for together: none waits for another.
   const bool listed = n >= 0 && n <= p.max_ctx && start >= 0 && start <= p.keep_total - n;
-  const bool has_row = r >= 0 && r < p.num_rows;
+  const bool has_row = !again && r >= 0 && r < p.num_rows;
   const int32_t* entries = p.block_table + static_cast<int64_t>(has_row ? r : 0) * p.max_pages;
   int32_t* old = p.old + static_cast<int64_t>(i) * p.max_pages;
   const int64_t len = has_row ? p.ctx_lens[r] : -1;
@@ -213,8 +240,10 @@ __global__ __launch_bounds__(kPageThreads) void page_find(const PageParams p) {
   const int counted = p.chunks > 1 ? p.chunks : 0;
   if (static_cast<int>(blockIdx.x) < counted) {
     __shared__ int32_t waves[kPageThreads / 64];
+    int32_t x[kMasks];
     uint64_t mask[kMasks];
-    const int count = free_masks(p, blockIdx.x, mask);
+    load_counts(p, blockIdx.x, x);
+    const int count = free_masks(x, mask);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = count;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -225,8 +254,7 @@ __global__ __launch_bounds__(kPageThreads) void page_find(const PageParams p) {
   } else if constexpr (OP == PageOp::kCompact) {
     find_cut(p, blockIdx.x - counted);
   } else {
-    const int64_t i = static_cast<int64_t>(blockIdx.x - counted) * kPageThreads + threadIdx.x;
-    if (i < p.n) find_item<OP>(p, static_cast<int>(i));
+    find_item<OP>(p, static_cast<int>(blockIdx.x - counted) * kPageThreads);
   }
 }
 
@@ -242,12 +270,18 @@ __global__ __launch_bounds__(kPageThreads) void page_give(const PageParams p) {
   __shared__ int32_t pages[kChunkPages];  // the chunk's free pages in order
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int chunk = ALONE ? 0 : blockIdx.x;
+  int32_t counts[kMasks];
+  load_counts(p, chunk, counts);
   // The first tile of items stays in registers: with up to 1024 items no
   // other is looked at.
   Item item{};
-  if (static_cast<int>(threadIdx.x) < p.n) item = ALONE ? find_item<OP>(p, threadIdx.x) : read_item(p, threadIdx.x);
+  if constexpr (ALONE) {
+    item = find_item<OP>(p, 0);
+  } else if (static_cast<int>(threadIdx.x) < p.n) {
+    item = read_item(p, threadIdx.x);
+  }
   uint64_t mask[kMasks];
-  const int mine = free_masks(p, chunk, mask);
+  const int mine = free_masks(counts, mask);
   if (lane == 0) wave_free[w] = mine;
   int64_t need_all, tile;
   int64_t base = block_scan(item.need, sums[0], need_all);
@@ -260,8 +294,14 @@ __global__ __launch_bounds__(kPageThreads) void page_give(const PageParams p) {
   }
   if (p.n > kPageThreads) {
     int64_t more = 0, all;
-    for (int i = threadIdx.x + kPageThreads; i < p.n; i += kPageThreads)
-      more += ALONE ? find_item<OP>(p, i).need : p.items.need[i];
+    for (int i0 = kPageThreads; i0 < p.n; i0 += kPageThreads) {
+      const int i = i0 + static_cast<int>(threadIdx.x);
+      if constexpr (ALONE) {
+        more += find_item<OP>(p, i0).need;
+      } else if (i < p.n) {
+        more += p.items.need[i];
+      }
+    }
     block_scan(more, sums[1], all);
     need_all += all;
     __syncthreads();

@@ -73,8 +73,10 @@ class PagesModel:
 
     def fork(self, parents, children):
         plan = []
-        for f, c in zip(parents, children):
+        for i, (f, c) in enumerate(zip(parents, children)):
             if not (0 <= f < len(self.ctx) and 0 <= c < len(self.ctx)) or f == c or self.ctx[c] != 0:
+                continue
+            if c in children[:i]:
                 continue
             if 0 <= self.ctx[f] <= self.max_ctx:
                 plan.append((f, c))
@@ -100,8 +102,8 @@ class PagesModel:
 
     def compact(self, rows, keeps):
         plan, need = [], 0
-        for r, keep in zip(rows, keeps):
-            if not 0 <= r < len(self.ctx) or len(keep) > self.ctx[r]:
+        for i, (r, keep) in enumerate(zip(rows, keeps)):
+            if not 0 <= r < len(self.ctx) or len(keep) > self.ctx[r] or r in rows[:i]:
                 continue
             same = 0
             while same < len(keep) and keep[same] == same:

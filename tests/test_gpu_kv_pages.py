@@ -221,6 +221,37 @@ def test_fork_pairs_that_are_left_out():
     b.check()
 
 
+def test_of_a_row_named_twice_the_first_counts():
+    b = Both(6, 60, 16, 90)
+    b.reserve([40, 50, 0, 0, 0, 0])
+    b.fork([0, 1, 0], [2, 2, 3])
+    b.check()
+    b.fork([9, 0, 1], [4, 4, 5])  # a pair that is left out names its child all the same
+    b.check()
+    b.compact([2, 2, 0, 5, 2], [[1, 2, 3], [5], [0], [0, 1, 30], []])
+    b.check()
+    b.compact([1, 1], [list(range(60)), [3]])  # also where the first is left out
+    b.check()
+    b.release([0, 1, 2, 3, 4, 5])
+    b.check()
+    assert int(b.counts.abs().sum()) == 0
+
+
+@pytest.mark.parametrize("num_pages", [3000, 9000])
+def test_rows_named_twice_in_long_lists(num_pages):
+    rng = random.Random(num_pages)
+    rows = 2600
+    b = Both(rows, num_pages, 16, 40, layers=1, heads=1)
+    b.reserve([21] + [0] * (rows - 1))
+    children = [rng.randrange(1, rows) for _ in range(2500)]
+    assert len(set(children)) < 2000
+    b.fork([0] * 2500, children)
+    b.check(pools=False)
+    which = [rng.randrange(0, rows) for _ in range(1500)]
+    b.compact(which, [[0, 3, 20] if rng.random() < 0.5 else [0] for _ in which])
+    b.check()
+
+
 @pytest.mark.parametrize("n", [1, 15, 16, 17, 32, 100])
 def test_compact_at_page_borders(n):
     """Everything kept, nothing, and cuts around the ends of pages; the kept whole pages stay where they are."""

@@ -67,7 +67,7 @@ def test_good_calls_stop_at_the_device(plan):
     (dict(num_rows=65536), B.ERR_INVALID_SHAPE), (dict(max_ctx_len=0), B.ERR_INVALID_SHAPE),
     (dict(max_ctx_len=4097), B.ERR_INVALID_SHAPE), (dict(max_pages_per_seq=255), B.ERR_INVALID_SHAPE),
     (dict(refcounts=None), B.ERR_NULL_POINTER), (dict(block_table=None), B.ERR_NULL_POINTER),
-    (dict(ctx_lens=None), B.ERR_NULL_POINTER), (dict(refcounts=A + 4), B.ERR_MISALIGNED),
+    (dict(ctx_lens=None), B.ERR_NULL_POINTER), (dict(refcounts=A + 2), B.ERR_MISALIGNED),
     (dict(block_table=A + 2), B.ERR_MISALIGNED)], ids=str)
 def test_state_refusals(plan, kw, status):
     assert set(_calls(plan, _state(**kw)).values()) == {status}
