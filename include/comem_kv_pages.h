@@ -33,8 +33,9 @@
  * Ownership, errors and streams are as for the decode calls: every argument
  * is checked on the host before any HIP call; the calls enqueue their kernels
  * on the given stream and return, and neither allocate nor synchronise. Calls
- * on one state change it and must be ordered, by one stream or by events; the
- * workspace belongs to the state.
+ * on one state change it and must be ordered, by one stream or by events, and
+ * enqueued one after the other (a call is several kernels); the workspace
+ * belongs to the state.
  *
  * Device-side contract: 0 <= ctx_lens[r] <= max_ctx_len; entries that hold
  * pages lie in [0, num_pages). A row outside the first part is left as it is.

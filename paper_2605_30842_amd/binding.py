@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from typing import Optional, Tuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -561,7 +562,7 @@ def _empty_on(op, stream, shape, dtype):
     """Memory from the allocator of the call's stream, so that it is not handed on while the call still runs."""
     import torch
 
-    if stream is None:
+    if not isinstance(stream, torch.cuda.Stream):
         return torch.empty(shape, dtype=dtype, device=op._torch_device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=op._torch_device)
@@ -849,11 +850,11 @@ class DecodeAttention:
         self._check_bound(max_q_len, "max_q_len")
         self._check_bound(max_ctx_len)
 
-    def _prefill_outputs(self, q, out, lse):
+    def _prefill_outputs(self, q, out, lse, stream=None):
         import torch
 
         if out is None:
-            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+            out = _empty_on(self, stream, q.shape, torch.float32)
         return out, lse
 
     def prefill_workspace_bytes(self, batch: int, max_q_len: int, max_ctx_len: int) -> int:
@@ -904,7 +905,7 @@ class DecodeAttention:
         self._check_prefill(q, q_start, q_lens, max_q_len, ctx_lens, out, lse, max_ctx_len)
         self._check_cache(k, v, paged=False)
         self._check_lengths(ctx_lens, ctx_lens.shape[0], seq_start=seq_start)
-        out, lse = self._prefill_outputs(q, out, lse)
+        out, lse = self._prefill_outputs(q, out, lse, stream)
         args = (self.plan, q.data_ptr(), q_start.data_ptr(), q_lens.data_ptr(), int(max_q_len), k.data_ptr(),
                 v.data_ptr(), k.stride(0), k.stride(1), seq_start.data_ptr(), ctx_lens.data_ptr(), ctx_lens.shape[0],
                 int(max_ctx_len), out.data_ptr(), None if lse is None else lse.data_ptr())
@@ -924,7 +925,7 @@ class DecodeAttention:
         self._check_prefill(q, q_start, q_lens, max_q_len, ctx_lens, out, lse, max_ctx_len)
         self._check_cache(k_pages, v_pages, paged=True)
         self._check_lengths(ctx_lens, ctx_lens.shape[0], block_table=block_table)
-        out, lse = self._prefill_outputs(q, out, lse)
+        out, lse = self._prefill_outputs(q, out, lse, stream)
         args = (self.plan, q.data_ptr(), q_start.data_ptr(), q_lens.data_ptr(), int(max_q_len), k_pages.data_ptr(),
                 v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), k_pages.shape[1],
                 k_pages.shape[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(),
@@ -1065,7 +1066,8 @@ class KVPages:
     op: the DecodeAttention whose plan the cache belongs to. k_pages, v_pages: [P, page_size, Hkv, D], or
     [layers, P, page_size, Hkv, D] where one block table serves several layers. block_table int32 [R, width],
     ctx_lens int32 [R] and refcounts int32 [P] are changed in place (all zero, and any table, to begin with). The object
-    holds these tensors and a workspace; its calls must be ordered, by one stream or by events.
+    holds these tensors and a workspace; its calls must be ordered, by one stream or by events (threads that share a
+    stream may call at any time).
 
     reserve, fork and compact return the pages that were missing, a device int32 tensor of no dimension: 0, or the call
     has changed nothing.
@@ -1101,6 +1103,7 @@ class KVPages:
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
         self._workspace = self.workspace.data_ptr()
         self._rows = ctx_lens.shape
+        self._lock = threading.Lock()  # a call's launches follow one another on the stream
         self._at = dev.index if dev.type == "cuda" else -1
 
     def _list(self, name, t, dtype=None, shape=None):
@@ -1127,8 +1130,9 @@ class KVPages:
         """Room for add_lens[r] (int32 [R]) more tokens in every row: pages where they are needed, ctx_lens grown."""
         add = self._list("add_lens", add_lens, shape=self._rows)
         missing = self._missing(missing, stream)
-        _call_on(self.op, stream, comem_kv_reserve, self.op.plan, self._state, add, missing.data_ptr(),
-                 self._workspace, self.workspace_bytes)
+        with self._lock:
+            _call_on(self.op, stream, comem_kv_reserve, self.op.plan, self._state, add, missing.data_ptr(),
+                     self._workspace, self.workspace_bytes)
         return missing
 
     def fork(self, parents, children, missing=None, stream=None):
@@ -1139,8 +1143,9 @@ class KVPages:
         missing = self._missing(missing, stream)
         if parents.shape[0] == 0:
             return missing.zero_() if stream is None else self._zeroed(missing, stream)
-        _call_on(self.op, stream, comem_kv_fork, self.op.plan, self._state, src, dst, parents.shape[0],
-                 missing.data_ptr(), self._workspace, self.workspace_bytes)
+        with self._lock:
+            _call_on(self.op, stream, comem_kv_fork, self.op.plan, self._state, src, dst, parents.shape[0],
+                     missing.data_ptr(), self._workspace, self.workspace_bytes)
         return missing
 
     def compact(self, rows, keep, keep_start, keep_lens, missing=None, stream=None):
@@ -1155,15 +1160,17 @@ class KVPages:
         missing = self._missing(missing, stream)
         if rows.shape[0] == 0:
             return missing.zero_() if stream is None else self._zeroed(missing, stream)
-        _call_on(self.op, stream, comem_kv_compact, self.op.plan, self._state, at, which, keep.shape[0], start, count,
-                 rows.shape[0], missing.data_ptr(), self._workspace, self.workspace_bytes)
+        with self._lock:
+            _call_on(self.op, stream, comem_kv_compact, self.op.plan, self._state, at, which, keep.shape[0], start,
+                     count, rows.shape[0], missing.data_ptr(), self._workspace, self.workspace_bytes)
         return missing
 
     def release(self, rows, stream=None) -> None:
         """Rows rows[i] (int32 [n]) give up their pages and become empty."""
         at = self._list("rows", rows)
         if rows.shape[0] > 0:
-            _call_on(self.op, stream, comem_kv_release, self.op.plan, self._state, at, rows.shape[0])
+            with self._lock:
+                _call_on(self.op, stream, comem_kv_release, self.op.plan, self._state, at, rows.shape[0])
 
     @staticmethod
     def _zeroed(missing, stream):

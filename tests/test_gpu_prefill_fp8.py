@@ -321,6 +321,11 @@ def test_captured_and_other_stream():
     op.prefill_paged(*args, out=out, stream=side)
     side.synchronize()
     assert torch.equal(out.cpu(), want)
+    got, _ = op.prefill_paged(*args, stream=side)  # its own output: memory of that stream
+    side.synchronize()
+    assert torch.equal(got.cpu(), want)
+    owner = [s["stream"] for s in torch.cuda.memory_snapshot() if 0 <= got.data_ptr() - s["address"] < s["total_size"]]
+    assert owner == [side.cuda_stream]
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         op.prefill_paged(*args, out=out)

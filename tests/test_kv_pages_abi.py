@@ -154,6 +154,31 @@ def _pages(op, layers=0, **kw):
     return B.KVPages(op, **d)
 
 
+def test_threads_enqueue_one_call_after_the_other(op, monkeypatch):
+    import threading
+    import time
+
+    inside, most = [0], [0]
+
+    def entry(*a):
+        inside[0] += 1
+        most[0] = max(most[0], inside[0])
+        time.sleep(0.01)
+        inside[0] -= 1
+
+    for name in B.PAGES_EXPORTED[1:]:
+        monkeypatch.setattr(B, name, entry)
+    p, one, lens = _pages(op), torch.zeros(1, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    calls = [lambda: p.reserve(lens), lambda: p.fork(one, one), lambda: p.compact(one, one, one.long(), one),
+             lambda: p.release(one)]
+    threads = [threading.Thread(target=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert most[0] == 1
+
+
 def test_wrapper_reads_the_pools(op):
     one, two = _pages(op)._state, _pages(op, layers=2)._state
     assert (one.num_layers, one.num_pages, one.page_size, one.stride_page) == (1, 10, 16, 16 * 128)
@@ -228,10 +253,10 @@ def test_model_keeps_counts_true():
         if kind == "reserve":
             m.reserve([rng.choice([0, 1, 5, -1]) for _ in range(6)])
         elif kind == "fork":
-            m.fork([rng.randrange(-1, 7) for _ in range(2)], rng.sample(range(6), 2))
+            m.fork([rng.randrange(-1, 7) for _ in range(3)], [rng.randrange(6) for _ in range(3)])
         elif kind == "compact":
-            r = rng.randrange(6)
-            m.compact([r], [[t for t in range(m.ctx[r]) if rng.random() < 0.7]])
+            which = [rng.randrange(6) for _ in range(2)]
+            m.compact(which, [[t for t in range(m.ctx[r]) if rng.random() < 0.7] for r in which])
         else:
             m.release([rng.randrange(6)])
         held = [0] * 30
