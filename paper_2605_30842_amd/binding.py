@@ -3,7 +3,8 @@
 The functions named like the C entry points pass plain integers (device
 pointers, strides, sizes) straight through and raise ``ComemError`` on a
 non-OK status. ``DecodeAttention`` is a convenience wrapper that takes torch
-tensors, reads their pointers and strides, and owns a zero-filled workspace;
+tensors, reads their pointers and strides, and owns a zero-filled workspace,
+``KVPages`` the same for the calls that keep a paged cache's pages;
 torch is used only for device memory and the current stream. Every step of
 the computation runs in the HIP kernels of the library: when the library has
 not been built this module raises instead of computing anything else.
