@@ -12,8 +12,8 @@
 // counts of given-up pages go down only there, after every look for free ones.
 //
 // Measured. A launch that only edits tables is its round trips to memory:
-// page_release 3 to 4.5 us, page_find 4 to 4.7, page_give 4.8 (reserve), 5.7
-// (fork), 7.2 over five chunks. A release and two reserves of 64 rows over
+// page_release 2 to 4.6 us, page_find 4 to 4.7, page_give 4.8 (reserve), 5.8
+// to 7.4 (fork), 7.2 over five chunks. A release and two reserves of 64 rows over
 // 40960 pages took 38.9 us where one workgroup looked at all of them, 22.6
 // with a workgroup per chunk; of 8 rows over one chunk 28.6 with a separate
 // find, 19.9 without. The copies: fork, the last pages of 32 rows over 4
