@@ -184,17 +184,19 @@ def test_scales(k_scale, v_scale):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("split", [False, True])
-def test_scores_around_the_lazy_bound(d, split):
+@pytest.mark.parametrize("new", [90, 13])  # 13: few rows, a tile's keys shared by waves
+def test_scores_around_the_lazy_bound(d, split, new):
     """Tiles of equal scores: below the running maximum, a little above it (no rescale), far above (rescale), and far
     below, in both halves of a workgroup's tiles and, shared, in every split."""
     steps = [0.0, -3.0, 5.0, 5.5, 30.0, 10.0, 37.9, 38.1, -60.0, 60.0, 59.0, 0.0, 64.0, 60.0, 80.0, 75.0]
     n = 64 * len(steps) - 10
-    c = Case([n], [90], hq=4, hkv=1, d=d, seed=8)
+    c = Case([n], [new], hq=4, hkv=1, d=d, seed=8)
     c.q.zero_()
     c.q[:, :, 0] = 1.0
     kv = c.k.view(torch.float8_e4m3fn)[3:3 + n]
     c.k[3:3 + n] = 0
-    scores = torch.tensor(steps).repeat_interleave(64)[:n] + (torch.arange(n) % 3) * 0.25
+    width = 64 if new == 90 else 32  # few rows: other steps for the two parts of a tile too
+    scores = torch.tensor(steps * (64 // width)).repeat_interleave(width)[:n] + (torch.arange(n) % 3) * 0.25
     codes = (scores / (math.log2(math.e) * c.scale) / 16).clamp(-448, 448).to(torch.float8_e4m3fn)
     c.q[:, :, 0] = 16.0 * c.k_scale ** 0
     c.k_scale = 1.0
@@ -251,10 +253,12 @@ def test_smallest_and_largest_codes():
 
 
 @pytest.mark.parametrize("split", [False, True])
-def test_nan_codes(split):
+@pytest.mark.parametrize("few", [False, True])
+def test_nan_codes(split, few):
     """A NaN key: every row that sees it is NaN, out and lse, and no other. A NaN value in the prefix: the outputs at
     its head_dim entry."""
     n, m = (3000, 40) if split else (200, 120)
+    m = 14 if few else m
     for where in ("k", "v"):
         c = Case([n, n], [m, m], hq=8, hkv=2, seed=11)
         clean, clean_lse = c.run()
