@@ -559,14 +559,15 @@ def _call_on(op, stream, entry, *args) -> None:
         entry(*args, op._stream(stream))
 
 
-def _empty_on(op, stream, shape, dtype):
-    """Memory from the allocator of the call's stream, so that it is not handed on while the call still runs."""
+def _empty_on(stream, like, shape, **dtype):
+    """Memory of like's device, from the allocator of the call's stream, so that it is not handed on while the call
+    still runs."""
     import torch
 
-    if not isinstance(stream, torch.cuda.Stream):
-        return torch.empty(shape, dtype=dtype, device=op._torch_device)
+    if stream is None or not isinstance(stream, torch.cuda.Stream):
+        return like.new_empty(shape, **dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=op._torch_device)
+        return like.new_empty(shape, **dtype)
 
 
 # Placement of V relative to K that the C header recommends
@@ -852,10 +853,10 @@ class DecodeAttention:
         self._check_bound(max_ctx_len)
 
     def _prefill_outputs(self, q, out, lse, stream=None):
-        import torch
-
         if out is None:
-            out = _empty_on(self, stream, q.shape, torch.float32)
+            import torch
+
+            out = _empty_on(stream, q, q.shape, dtype=torch.float32)
         return out, lse
 
     def prefill_workspace_bytes(self, batch: int, max_q_len: int, max_ctx_len: int) -> int:
@@ -1013,10 +1014,7 @@ class DecodeAttention:
         self._check_bound(max_ctx_len)
         rows = q.shape[0]
         if q_out is None:
-            if stream is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-            else:
-                q_out = _empty_on(self, stream, q.shape, q.dtype)
+            q_out = _empty_on(stream, q, q.shape)
         rope = RopeConfig(None if q_weight is None else q_weight.data_ptr(),
                           None if k_weight is None else k_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0],
                           cos_sin.shape[1], eps, ROPE_INTERLEAVED if interleaved else 0)
@@ -1122,7 +1120,7 @@ class KVPages:
         import torch
 
         if missing is None:
-            return _empty_on(self.op, stream, (), torch.int32)
+            return _empty_on(stream, self.ctx_lens, ())
         _need(isinstance(missing, torch.Tensor) and missing.dtype == torch.int32 and missing.numel() == 1
               and missing.device == self.op._torch_device, f"missing must be one int32 on {self.op._torch_device}")
         return missing
