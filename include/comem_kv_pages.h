@@ -9,7 +9,10 @@
  * These calls do it on the block table that the paged attention calls read
  * (comem_decode_attn.h). All state lies in device memory and no call looks at
  * it from the host, so a decode loop that takes pages as it goes can be
- * captured in a graph.
+ * captured in a graph. A row that gets no room keeps its length, and a call
+ * after it that stores new tokens as the row's last ones would write over
+ * tokens it holds, which forks may share: such a loop has to learn on the
+ * device which rows grew (comem_kv_reserve_granted).
  *
  * State, the caller's (comem_kv_pages below): a block table of num_rows rows,
  * one sequence each, ctx_lens[r] tokens long, and refcounts[p], the number of
@@ -82,12 +85,26 @@ comem_status comem_kv_pages_workspace(const comem_decode_attn_plan* plan, const 
 /* Room for add_lens[r] more tokens in every row r: the row gets the pages that
  * ceil((ctx_lens[r] + add_lens[r]) / page_size) asks for besides those it has,
  * and ctx_lens[r] grows by add_lens[r]. A row with add_lens[r] < 0, or that
- * would grow past max_ctx_len, is left as it is.
+ * would grow past max_ctx_len, is left as it is and does not show in *missing.
+ * Neither does *missing reach a call enqueued after this one: unless the
+ * caller has looked at it, and knows that no row passes max_ctx_len, use
+ * comem_kv_reserve_granted.
  *   add_lens   device int32 [num_rows].
  *   missing    device int32 [1]. */
 comem_status comem_kv_reserve(const comem_decode_attn_plan* plan, const comem_kv_pages* pages,
                               const int32_t* add_lens, int32_t* missing, void* workspace,
                               size_t workspace_bytes, void* hip_stream);
+
+/* The same, and granted[r] becomes the number of tokens that row r grew by:
+ * add_lens[r], or 0 for a row that is left as it is (every row, where pages
+ * are missing). It is the q_lens of the calls that follow: comem_rope_append
+ * with q_lens = granted stores nothing for a row without room, prefill writes
+ * nothing. comem_kv_append and the fused append have no such argument: give
+ * them, and the attention, lengths that are 0 for those rows.
+ *   granted    device int32 [num_rows], not overlapping add_lens. */
+comem_status comem_kv_reserve_granted(const comem_decode_attn_plan* plan, const comem_kv_pages* pages,
+                                      const int32_t* add_lens, int32_t* granted, int32_t* missing,
+                                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Row children[i] becomes a second sequence on the tokens of row parents[i]:
  * it holds the parent's whole pages too, and of a last, partly filled one a

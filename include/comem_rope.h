@@ -28,7 +28,10 @@
  * cache token t = L_b - M_b + i. Its position is t, or what `positions` says
  * (after a cut of the context, comem_kv_compact, cache index and position
  * differ). With q_start and q_lens NULL every sequence has one new token, row
- * b, as in a decode step.
+ * b, as in a decode step. A call stores the last M_b tokens of what ctx_lens
+ * says: where a sequence may have been refused room (comem_kv_reserve), its
+ * M_b must be 0, or tokens it holds are overwritten. q_lens may be the
+ * lengths that comem_kv_reserve_granted left on the device.
  *
  * Both calls take a plan from comem_decode_attn_init: its heads, head_dim,
  * dtype (q, new keys and values and weights are float32 for COMEM_F32 plans

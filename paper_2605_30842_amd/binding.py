@@ -38,8 +38,8 @@ EXPORTED = (
 )
 PREFILL_FP8_EXPORTED = ("comem_prefill_fp8_workspace", "comem_prefill_fp8_attn", "comem_prefill_fp8_attn_paged")
 ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
-PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_fork", "comem_kv_compact",
-                  "comem_kv_release")
+PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_reserve_granted", "comem_kv_fork",
+                  "comem_kv_compact", "comem_kv_release")
 ROPE_INTERLEAVED = 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # COMEM_NOALLOC_SCRATCH_BYTES
 FLAG_DEBUG_CHECKS = 1
@@ -204,6 +204,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                             i64, i32, i64, vp, i32, vp, i32, i64, vp]
     lib.comem_kv_pages_workspace.argtypes = [vp, pp, ctypes.POINTER(sz)]
     lib.comem_kv_reserve.argtypes = [vp, pp, vp, vp, vp, sz, vp]
+    lib.comem_kv_reserve_granted.argtypes = [vp, pp, vp, vp, vp, vp, sz, vp]
     lib.comem_kv_fork.argtypes = [vp, pp, vp, vp, i32, vp, vp, sz, vp]
     lib.comem_kv_compact.argtypes = [vp, pp, vp, vp, i64, vp, vp, i32, vp, vp, sz, vp]
     lib.comem_kv_release.argtypes = [vp, pp, vp, i32, vp]
@@ -451,6 +452,12 @@ def comem_kv_pages_workspace(plan, pages: PagesState) -> int:
 def comem_kv_reserve(plan, pages: PagesState, add_lens, missing, workspace, workspace_bytes, stream) -> None:
     _check(load_library().comem_kv_reserve(plan, ctypes.byref(pages), add_lens, missing, workspace, workspace_bytes,
                                            stream), "comem_kv_reserve")
+
+
+def comem_kv_reserve_granted(plan, pages: PagesState, add_lens, granted, missing, workspace, workspace_bytes,
+                             stream) -> None:
+    _check(load_library().comem_kv_reserve_granted(plan, ctypes.byref(pages), add_lens, granted, missing, workspace,
+                                                   workspace_bytes, stream), "comem_kv_reserve_granted")
 
 
 def comem_kv_fork(plan, pages: PagesState, parents, children, n, missing, workspace, workspace_bytes, stream) -> None:
@@ -1125,13 +1132,22 @@ class KVPages:
               and missing.device == self.op._torch_device, f"missing must be one int32 on {self.op._torch_device}")
         return missing
 
-    def reserve(self, add_lens, missing=None, stream=None):
-        """Room for add_lens[r] (int32 [R]) more tokens in every row: pages where they are needed, ctx_lens grown."""
+    def reserve(self, add_lens, missing=None, stream=None, granted=None):
+        """Room for add_lens[r] (int32 [R]) more tokens in every row: pages where they are needed, ctx_lens grown.
+
+        A row that would pass max_ctx_len, and every row where pages are missing, keeps its length. granted (int32 [R])
+        gets the tokens that each row grew by, 0 for those: give it to rope_append and prefill as q_lens wherever the
+        host has not looked at the result, a captured loop above all, or their new tokens replace the row's last ones.
+        """
         add = self._list("add_lens", add_lens, shape=self._rows)
+        entry, lists = comem_kv_reserve, (add,)
+        if granted is not None:
+            entry, lists = comem_kv_reserve_granted, (add, self._list("granted", granted, shape=self._rows))
+            _need(abs(lists[1] - add) >= 4 * self._rows[0], "granted must not overlap add_lens")
         missing = self._missing(missing, stream)
         with self._lock:
-            _call_on(self.op, stream, comem_kv_reserve, self.op.plan, self._state, add, missing.data_ptr(),
-                     self._workspace, self.workspace_bytes)
+            _call_on(self.op, stream, entry, self.op.plan, self._state, *lists, missing.data_ptr(), self._workspace,
+                     self.workspace_bytes)
         return missing
 
     def fork(self, parents, children, missing=None, stream=None):

@@ -153,6 +153,26 @@ comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved,
   return ok ? COMEM_OK : COMEM_ERR_HIP;
 }
 
+// granted: nullptr where the caller does not ask for it.
+comem_status reserve(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* add_lens,
+                     int32_t* granted, int32_t* missing, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const comem_decode_attn_plan* p = checked(plan);
+  if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
+  comem_status st = check_state(*p, pages);
+  if (st != COMEM_OK) return st;
+  if (add_lens == nullptr) return COMEM_ERR_NULL_POINTER;
+  if (!aligned(add_lens, 4) || !aligned(granted, 4)) return COMEM_ERR_MISALIGNED;
+  st = check_workspace(*pages, missing, workspace, workspace_bytes);
+  if (st != COMEM_OK) return st;
+  if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
+  comem::PageParams a = params_of(*p, *pages, pages->num_rows);
+  set_workspace(*pages, workspace, a);
+  a.add_lens = add_lens;
+  a.given = granted;
+  a.missing = missing;
+  return launch_pages(comem::PageOp::kReserve, a, 0, 0, hip_stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -171,20 +191,15 @@ comem_status comem_kv_pages_workspace(const comem_decode_attn_plan* plan, const 
 comem_status comem_kv_reserve(const comem_decode_attn_plan* plan, const comem_kv_pages* pages,
                               const int32_t* add_lens, int32_t* missing, void* workspace,
                               size_t workspace_bytes, void* hip_stream) {
-  const comem_decode_attn_plan* p = checked(plan);
-  if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
-  comem_status st = check_state(*p, pages);
-  if (st != COMEM_OK) return st;
-  if (add_lens == nullptr) return COMEM_ERR_NULL_POINTER;
-  if (!aligned(add_lens, 4)) return COMEM_ERR_MISALIGNED;
-  st = check_workspace(*pages, missing, workspace, workspace_bytes);
-  if (st != COMEM_OK) return st;
-  if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
-  comem::PageParams a = params_of(*p, *pages, pages->num_rows);
-  set_workspace(*pages, workspace, a);
-  a.add_lens = add_lens;
-  a.missing = missing;
-  return launch_pages(comem::PageOp::kReserve, a, 0, 0, hip_stream);
+  return reserve(plan, pages, add_lens, nullptr, missing, workspace, workspace_bytes, hip_stream);
+}
+
+comem_status comem_kv_reserve_granted(const comem_decode_attn_plan* plan, const comem_kv_pages* pages,
+                                      const int32_t* add_lens, int32_t* granted, int32_t* missing,
+                                      void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (checked(plan) == nullptr) return COMEM_ERR_BAD_HANDLE;
+  if (granted == nullptr) return COMEM_ERR_NULL_POINTER;
+  return reserve(plan, pages, add_lens, granted, missing, workspace, workspace_bytes, hip_stream);
 }
 
 comem_status comem_kv_fork(const comem_decode_attn_plan* plan, const comem_kv_pages* pages, const int32_t* parents,

@@ -322,7 +322,13 @@ __global__ __launch_bounds__(kPageThreads) void page_give(const PageParams p) {
     *p.granted = missing == 0 ? 1 : 0;
     *p.missing = static_cast<int32_t>(missing < INT32_MAX ? missing : INT32_MAX);
   }
-  if (missing != 0) return;
+  if (missing != 0) {
+    if constexpr (OP == PageOp::kReserve) {
+      if (blockIdx.x == 0 && p.given != nullptr)
+        for (int i = threadIdx.x; i < p.n; i += kPageThreads) p.given[i] = 0;
+    }
+    return;
+  }
 
 #pragma unroll
   for (int k = 0; k < kMasks; ++k) {
@@ -347,7 +353,10 @@ __global__ __launch_bounds__(kPageThreads) void page_give(const PageParams p) {
       tile_base[threadIdx.x] = base;
       tile_need[threadIdx.x] = item.need;
       tile_first[threadIdx.x] = item.first;
-      if (blockIdx.x == 0 && i < p.n && item.row >= 0) p.ctx_lens[i] = item.grown;
+      if (blockIdx.x == 0 && i < p.n) {
+        if (item.row >= 0) p.ctx_lens[i] = item.grown;
+        if (p.given != nullptr) p.given[i] = item.row >= 0 ? p.add_lens[i] : 0;
+      }
       __syncthreads();
       for (int k = w; k < kPageThreads && i0 + k < p.n; k += kWaves) {
         const int64_t b = tile_base[k];

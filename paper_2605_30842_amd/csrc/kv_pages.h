@@ -47,6 +47,7 @@ struct PageParams {
   const int32_t* rows;        // compact, release; fork: the parents
   const int32_t* children;    // fork
   const int32_t* add_lens;    // reserve
+  int32_t* given;             // reserve: the tokens that each row grew by, or nullptr
   const int32_t* keep;        // compact
   const int64_t* keep_start;
   const int32_t* keep_lens;
