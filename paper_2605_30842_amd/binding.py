@@ -568,13 +568,17 @@ def _call_on(op, stream, entry, *args) -> None:
 
 def _empty_on(stream, like, shape, **dtype):
     """Memory of like's device, from the allocator of the call's stream, so that it is not handed on while the call
-    still runs."""
+    still runs. Nor while the caller's current stream, where the result may be read, still has work from before it was
+    dropped: the allocator is told of that stream too."""
     import torch
 
     if stream is None or not isinstance(stream, torch.cuda.Stream):
         return like.new_empty(shape, **dtype)
+    reader = torch.cuda.current_stream(like.device)
     with torch.cuda.stream(stream):
-        return like.new_empty(shape, **dtype)
+        t = like.new_empty(shape, **dtype)
+    t.record_stream(reader)
+    return t
 
 
 # Placement of V relative to K that the C header recommends
