@@ -85,9 +85,8 @@ typedef struct {
  *   q_start    device int64 [batch]: first row of each sequence's new tokens.
  *   q_lens     device int32 [batch]: M_b. (Both or neither may be NULL.)
  *   max_q_len  host bound >= every q_lens[b], 0 .. max_ctx_len; 1 when q_lens
- *              is NULL; COMEM_ERR_INVALID_SHAPE above 2^26 - 1, what one
- *              launch holds. With max_q_len = 0 or batch = 0 nothing is enqueued
- *              and no pointer is looked at.
+ *              is NULL; COMEM_ERR_INVALID_SHAPE above 2^26 - 1. With max_q_len
+ *              = 0 or batch = 0 nothing is enqueued and no pointer is looked at.
  *   positions  device int32, one for each row, or NULL.
  *   q_out      [rows, h_q, d_h] dense, q's type, 16-byte aligned. May be q
  *              itself where q is dense; no other overlap.

@@ -41,8 +41,6 @@ comem_status prepare_rope(const comem_decode_attn_plan& p, const comem_rope_conf
   if (max_ctx_len < 0 || max_ctx_len > p.cfg.max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
   if (max_q_len < 0 || max_q_len > max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
   if (rope_is_empty(batch, max_q_len)) return COMEM_OK;
-  // A wave takes a token (parts of it only where tokens are few) and a launch
-  // has less than 2^32 threads along a dimension.
   if (max_q_len >= (1 << 26)) return COMEM_ERR_INVALID_SHAPE;
   if (is_fp8(p.cfg) && !(std::isfinite(1.f / p.cfg.k_scale) && std::isfinite(1.f / p.cfg.v_scale)))
     return COMEM_ERR_UNSUPPORTED;
@@ -123,10 +121,15 @@ comem_status launch_rope(const comem_decode_attn_plan& p, comem::RopeParams& a, 
   const comem::RopeKernelFn fn =
       comem::select_rope_kernel(p.cfg.head_dim, cache, paged, written > (int64_t{256} << 20));
   if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
+  // A launch has less than 2^32 threads along a dimension: the last 3 of the
+  // 2^26 - 1 tokens that a call may have take a second slice of the grid.
   const int64_t blocks = ceil_div(int64_t{a.max_q} * a.parts, comem::kRopeWaves);
+  const int64_t slices = ceil_div(blocks, ((int64_t{1} << 32) - 1) / (64 * comem::kRopeWaves));
   void* argv[] = {&a};
   const hipError_t err =
-      hipLaunchKernel(reinterpret_cast<const void*>(fn), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(batch)),
+      hipLaunchKernel(reinterpret_cast<const void*>(fn),
+                      dim3(static_cast<unsigned>(ceil_div(blocks, slices)), static_cast<unsigned>(batch),
+                           static_cast<unsigned>(slices)),
                       dim3(64 * comem::kRopeWaves), argv, 0, static_cast<hipStream_t>(stream));
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }

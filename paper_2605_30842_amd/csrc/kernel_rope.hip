@@ -97,7 +97,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_append_kernel(const Rope
   constexpr int kRow = D * static_cast<int>(sizeof(Elem));
   const int b = blockIdx.y;
   const int lane = threadIdx.x & 63;
-  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kRopeWaves + (threadIdx.x >> 6));
+  const int block = blockIdx.z * gridDim.x + blockIdx.x;
+  const int unit = __builtin_amdgcn_readfirstlane(block * kRopeWaves + (threadIdx.x >> 6));
   const int i = unit / p.parts;  // new token
   const int part = unit - i * p.parts;
   const int L = p.ctx_lens[b];
