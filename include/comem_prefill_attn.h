@@ -59,7 +59,9 @@ extern "C" {
  *              q_lens[b] - 1.
  *   q_start    device int64 [batch].
  *   q_lens     device int32 [batch]: M_b.
- *   max_q_len  host bound >= every q_lens[b], 0 .. max_ctx_len. A call with
+ *   max_q_len  host bound >= every q_lens[b], 0 .. max_ctx_len. In blocks of
+ *              128 / G tokens it makes less than 2^23, and less than 2^31 over
+ *              all sequences and KV heads (else COMEM_ERR_INVALID_SHAPE). A call with
  *              max_q_len = 0 or batch = 0 enqueues nothing and, once batch,
  *              max_ctx_len and max_q_len are in range, returns COMEM_OK
  *              without looking at any pointer (empty buffers may be NULL).

@@ -27,6 +27,11 @@ comem_status check_bounds(const comem_decode_attn_plan& p, int32_t batch, int32_
   if (batch < 0 || batch > p.cfg.max_batch) return COMEM_ERR_INVALID_SHAPE;
   if (max_ctx_len < 0 || max_ctx_len > p.cfg.max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
   if (max_q_len < 0 || max_q_len > max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
+  // A launch has less than 2^32 threads along a dimension, and the kernel
+  // numbers its workgroups in 31 bits. (Calls whose keys are split are small.)
+  const int64_t blocks = ceil_div(max_q_len, comem::kPrefillRows / group_of(p.cfg));
+  if (blocks >= (int64_t{1} << 32) / comem::kPrefillThreads) return COMEM_ERR_INVALID_SHAPE;
+  if (blocks * p.cfg.num_kv_heads > INT32_MAX / std::max(batch, 1)) return COMEM_ERR_INVALID_SHAPE;
   return COMEM_OK;
 }
 
