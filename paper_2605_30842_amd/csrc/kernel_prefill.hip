@@ -917,7 +917,10 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
     if (kh == 1 || sub == 1) return;
   }
   if (i >= M) return;
-  float inv = (FP8 ? p.out_scale : 1.f) / l_run;
+  float inv = 1.f / l_run;
+  // The V scale comes after the division: with the sum, up to 2^15 a key, its
+  // quotient could be subnormal where the output is not.
+  const float scale = FP8 ? p.out_scale : 1.f;
   const float lse2 = m_run * p.scale_log2 + log2f(l_run) - (FP8 ? kProbShift : 0.f);
   const int64_t orow = (qs + i) * p.num_q_heads + qh;
   float* o = p.out + orow * D;
@@ -936,8 +939,8 @@ __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const 
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4)
       *reinterpret_cast<float4*>(o + 32 * n + 8 * r4 + 4 * h) =
-          make_float4(acc[n][4 * r4] * inv, acc[n][4 * r4 + 1] * inv, acc[n][4 * r4 + 2] * inv,
-                      acc[n][4 * r4 + 3] * inv);
+          make_float4(acc[n][4 * r4] * inv * scale, acc[n][4 * r4 + 1] * inv * scale, acc[n][4 * r4 + 2] * inv * scale,
+                      acc[n][4 * r4 + 3] * inv * scale);
   if (h == 0 && p.lse != nullptr && !SPLIT) p.lse[orow] = lse2 * kLn2;
 }
 
