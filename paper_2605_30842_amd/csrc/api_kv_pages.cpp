@@ -134,7 +134,12 @@ bool launched(comem::PageKernelFn fn, dim3 grid, int threads, comem::PageParams&
 // 799 MB 206 and 362 -> 190 and 344; 70 MB 59.3, past the caches 60.3).
 comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved, double bytes, void* stream) {
   using comem::PageOp;
-  const bool compact = op == PageOp::kCompact, alone = a.chunks == 1 && !compact;
+  // A fork's item looks through the list before it, so past what one workgroup
+  // finds at once the lists are looked through side by side (us, a fork and a
+  // release, one workgroup / a find launch: 32 pairs 14.9 / 18.1, 1024 50.8 /
+  // 52.7, 1025 68.5 / 53.9, 4096 305 / 188, 65534 44600 / 2890).
+  const bool compact = op == PageOp::kCompact;
+  const bool alone = a.chunks == 1 && !compact && (op == PageOp::kReserve || a.n <= comem::kPageThreads);
   bool ok = true;
   if (!alone) {
     const int64_t items = compact ? a.n : ceil_div(a.n, comem::kPageThreads);

@@ -66,8 +66,8 @@ using PageKernelFn = void (*)(PageParams);
 // Items and, of more than one chunk, the chunks' free pages: chunk_blocks +
 // (compact: n, else ceil(n / kPageThreads)) workgroups.
 PageKernelFn select_page_find_kernel(PageOp);
-// One workgroup per chunk. ALONE: of one chunk and no compact call, whose
-// items are found here as well.
+// One workgroup per chunk. ALONE: of one chunk, whose items are found here as
+// well (reserve, and fork of at most kPageThreads pairs).
 PageKernelFn select_page_give_kernel(PageOp, bool alone);
 // Fork, compact: grid (1 + movers, n). stream (compact): tokens pass the caches by.
 PageKernelFn select_page_apply_kernel(PageOp, bool stream);
