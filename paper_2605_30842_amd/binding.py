@@ -1195,5 +1195,7 @@ class KVPages:
     def _zeroed(missing, stream):
         import torch
 
+        if not isinstance(stream, torch.cuda.Stream):  # another object with a cuda_stream, as the calls take it
+            stream = torch.cuda.ExternalStream(stream.cuda_stream, device=missing.device)
         with torch.cuda.stream(stream):
             return missing.zero_()
