@@ -65,3 +65,29 @@ def test_a_result_read_on_the_callers_stream_may_be_dropped(dtype, which):
     last = call(side)  # and now it may be taken again
     side.synchronize()
     assert torch.equal(last, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+def test_captured_on_a_second_stream(dtype):
+    """An output made, read and dropped inside a capture, the call on a stream that joins it."""
+    prefill, _ = _setup(dtype)
+    want = prefill()
+    side, res = torch.cuda.Stream(), torch.zeros_like(want)
+    prefill(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(2):
+            side.wait_stream(torch.cuda.current_stream())
+            out = prefill(side)
+            torch.cuda.current_stream().wait_stream(side)
+            res.copy_(out)
+            del out
+    for _ in range(3):
+        res.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(res, want)
+        again = prefill(side)
+        side.synchronize()
+        assert torch.equal(again, want)
