@@ -129,7 +129,8 @@ bool launched(comem::PageKernelFn fn, dim3 grid, int threads, comem::PageParams&
 }
 
 // `moved`: the most tokens of an item that a call may copy; `bytes`: the most
-// that it may store in all. Tokens that the last cache (256 MB) cannot hold for
+// that it may store in all (listed tokens that stay in place count too: the
+// lists are on the device). Tokens that the last cache (256 MB) cannot hold for
 // the attention that follows pass it by (us, compact calls that move 410 and
 // 799 MB 206 and 362 -> 190 and 344; 70 MB 59.3, past the caches 60.3).
 comem_status launch_pages(comem::PageOp op, comem::PageParams& a, int64_t moved, double bytes, void* stream) {

@@ -115,7 +115,8 @@ comem_status launch_rope(const comem_decode_attn_plan& p, comem::RopeParams& a, 
   // fits the last one (256 MB); where it does not, the stores pass them by.
   // Measured (us, bf16 and FP8 caches, 32 + 16 heads of 128): 402 and 335 MB
   // written 166 and 150 -> 149 and 122 us; 201 and 168 MB 71 and 64, past the
-  // caches 78 and 65.
+  // caches 78 and 65. The lengths are on the device, so a ragged batch counts as
+  // if every sequence had max_q_len tokens, and may pass the caches needlessly.
   const int64_t d = p.cfg.head_dim, qe = p.cfg.dtype == COMEM_F32 ? 4 : 2;
   const int64_t written = tokens * d * (p.cfg.num_q_heads * qe + 2 * int64_t{p.cfg.num_kv_heads} * elem_bytes(p.cfg));
   const comem::RopeKernelFn fn =

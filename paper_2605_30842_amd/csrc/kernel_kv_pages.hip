@@ -6,19 +6,20 @@
 // ones, to its items in order. With a pool of one chunk (8192 pages) one
 // workgroup finds the items' needs, ranks the free pages and hands them on.
 // With more, a launch before counts each chunk's free pages and a workgroup
-// per chunk hands out its own: the counts before it give its first rank.
+// per chunk hands out its own: the counts before it give its first rank. (That
+// launch also finds the items of compact and of forks of over 1024 pairs.)
 // Fork and compact calls then edit the tables and move tokens in one more
 // launch: an item's first workgroup the tables, the others the tokens. The
 // counts of given-up pages go down only there, after every look for free ones.
 //
 // Measured. A launch that only edits tables is its round trips to memory:
-// page_release 2 to 4.6 us, page_find 4 to 4.7, page_give 4.8 (reserve), 5.8
-// to 7.4 (fork), 7.2 over five chunks. A release and two reserves of 64 rows over
-// 40960 pages took 38.9 us where one workgroup looked at all of them, 22.6
-// with a workgroup per chunk; of 8 rows over one chunk 28.6 with a separate
-// find, 19.9 without. The copies: fork, the last pages of 32 rows over 4
-// layers (40 MB read and written) 10 us; compact, one row to 5471 tokens (37
-// MB) 10.4 us, eight rows to 6800 over 4 layers (0.79 GB) 154 us, 5.2 TB/s,
+// page_release 2.1 to 4.5 us, page_find 4.6 to 4.8, page_give 4.6 (reserve),
+// 5.1 to 7.7 (fork, compact), 7.1 over five chunks. A release and two reserves
+// of 64 rows over 40960 pages took 38.9 us where one workgroup looked at all of
+// them, 22.6 with a workgroup per chunk; of 8 rows over one chunk 28.6 with a
+// separate find, 19.9 without. The copies: fork, the last pages of 32 rows over
+// 4 layers (40 MB read and written) 10.3 us; compact, one row to 5471 tokens
+// (37 MB) 9.4 us, eight rows to 6800 over 4 layers (0.79 GB) 152 us, 5.2 TB/s,
 // the rate of a large copy.
 #include "kv_pages.h"
 

@@ -584,7 +584,10 @@ constexpr int kXcds = 8;  // XCDs of the GPU; workgroups are dealt to them round
 // waves 2 and 3 the same rows over the other 32, so a stage is half as long;
 // their states are merged at the end like the halves'. Four sequences of 16
 // new tokens over 12000, G = 4: 50.7 us wide, 42.0 narrow; of 1 to 16 over 2K
-// to 12K 41.0 and 35.6. The cache's reads bound what is left: 4.5 TB/s.
+// to 12K 41.0 and 35.6. What is left: start, merges and the second launch,
+// about 12 us, and 3.4 TB/s of cache beyond (24.7 us over 4096 tokens, 32.1
+// over 8192, 71.7 over 24576); in the ragged call also that every sequence has
+// the same number of splits, whatever its length (2.2 TB/s over all).
 template <int D, PLayout LAYOUT, bool SPLIT, bool FP8, bool NARROW>
 __global__ __launch_bounds__(kPrefillThreads, 1) void prefill_mfma_kernel(const PrefillParams p) {
   constexpr int KS = D / 16;
