@@ -1045,7 +1045,8 @@ class DecodeAttention:
 
         q [rows, Hq, D], new_k and new_v [rows, Hkv, D] may be parts of one projection's output (each token's heads
         side by side); cos_sin is float32 [positions, rot_dim], cosines first. Without q_start and q_lens each sequence
-        has one new token, else as in prefill. Give q_out=q to rotate dense queries in place.
+        has one new token, else as in prefill. Give q_out=q to rotate dense queries in place. The new tokens are the
+        last ones of ctx_lens: a row that KVPages.reserve gave no room must have none (its granted as q_lens).
         """
         batch, q_out, head = self._rope_args(q, new_k, new_v, ctx_lens, max_ctx_len, cos_sin, q_weight, k_weight, eps,
                                              q_start, q_lens, max_q_len, positions, interleaved, q_out, stream)
