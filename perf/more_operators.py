@@ -392,7 +392,8 @@ def _own_select(x):
 def _own_attend(x):
     case = x["case"]
     lse = torch.empty(x["q"].shape[:2], dtype=torch.float32, device=DEVICE)
-    return x["op"].block_forward(x["q"], x["k"], x["v"], x["table"], x["lens"], case["budget"] * case["page"], lse=lse)
+    return x["op"].block_forward(x["q"], x["k"], x["v"], x["table"], x["lens"],
+                               x["table"].shape[2] * case["page"], lse=lse)
 
 
 # ------------------------------------------------------------------ the same in elementary operations
