@@ -40,6 +40,8 @@ PREFILL_FP8_EXPORTED = ("comem_prefill_fp8_workspace", "comem_prefill_fp8_attn",
 ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
 PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_reserve_granted", "comem_kv_fork",
                   "comem_kv_compact", "comem_kv_release")
+EVICT_EXPORTED = ("comem_attn_weights", "comem_attn_weights_paged", "comem_keep_tokens")
+BLOCK_EXPORTED = ("comem_block_bounds", "comem_block_scores", "comem_block_select", "comem_block_attn")
 ROPE_INTERLEAVED = 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # COMEM_NOALLOC_SCRATCH_BYTES
 FLAG_DEBUG_CHECKS = 1
@@ -211,7 +213,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comem_prefill_fp8_workspace.argtypes = lib.comem_prefill_attn_workspace.argtypes
     lib.comem_prefill_fp8_attn.argtypes = lib.comem_prefill_attn_split.argtypes
     lib.comem_prefill_fp8_attn_paged.argtypes = lib.comem_prefill_attn_split_paged.argtypes
-    for name in ROPE_EXPORTED + PAGES_EXPORTED + PREFILL_FP8_EXPORTED:
+    f32 = ctypes.c_float
+    lib.comem_attn_weights.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, i32, i64, vp, f32, vp, i64, vp]
+    lib.comem_attn_weights_paged.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, i64, i32, i64, vp, i32, vp, i32, i64,
+                                             vp, f32, vp, i64, vp]
+    lib.comem_keep_tokens.argtypes = [vp, vp, i64, vp, i32, vp, i32, i64, i32, vp, i32, i32, vp, i64, vp, vp, vp, vp]
+    lib.comem_block_bounds.argtypes = [vp, vp, i64, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, vp, vp]
+    lib.comem_block_scores.argtypes = [vp, vp, vp, i32, i64, vp, i32, vp, i32, i64, vp, i64, vp]
+    lib.comem_block_select.argtypes = [vp, vp, i64, i32, vp, i32, vp, i32, i64, i32, i32, i32, vp, i32, vp, vp]
+    lib.comem_block_attn.argtypes = lib.comem_decode_attn_paged.argtypes
+    for name in ROPE_EXPORTED + PAGES_EXPORTED + PREFILL_FP8_EXPORTED + EVICT_EXPORTED + BLOCK_EXPORTED:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -475,6 +486,57 @@ def comem_kv_release(plan, pages: PagesState, rows, n, stream) -> None:
     _check(load_library().comem_kv_release(plan, ctypes.byref(pages), rows, n, stream), "comem_kv_release")
 
 
+def comem_attn_weights(plan, q, lse, q_start, q_lens, max_q_len, k, stride_token, stride_head, seq_start, ctx_lens,
+                       batch, max_ctx_len, prior, decay, weights, weights_stride, stream) -> None:
+    _check(load_library().comem_attn_weights(plan, q, lse, q_start, q_lens, max_q_len, k, stride_token, stride_head,
+                                             seq_start, ctx_lens, batch, max_ctx_len, prior, decay, weights,
+                                             weights_stride, stream), "comem_attn_weights")
+
+
+def comem_attn_weights_paged(plan, q, lse, q_start, q_lens, max_q_len, k_pages, stride_page, stride_token, stride_head,
+                             page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len, prior,
+                             decay, weights, weights_stride, stream) -> None:
+    _check(load_library().comem_attn_weights_paged(plan, q, lse, q_start, q_lens, max_q_len, k_pages, stride_page,
+                                                   stride_token, stride_head, page_size, num_pages, block_table,
+                                                   max_pages_per_seq, ctx_lens, batch, max_ctx_len, prior, decay,
+                                                   weights, weights_stride, stream), "comem_attn_weights_paged")
+
+
+def comem_keep_tokens(plan, weights, weights_stride, ctx_lens, num_rows, rows, n, max_ctx_len, budget, budgets, first,
+                      last, keep, keep_stride, keep_start, keep_lens, kept, stream) -> None:
+    _check(load_library().comem_keep_tokens(plan, weights, weights_stride, ctx_lens, num_rows, rows, n, max_ctx_len,
+                                            budget, budgets, first, last, keep, keep_stride, keep_start, keep_lens,
+                                            kept, stream), "comem_keep_tokens")
+
+
+def comem_block_bounds(plan, k_pages, stride_page, stride_token, stride_head, page_size, num_pages, block_table,
+                       max_pages_per_seq, ctx_lens, q_lens, max_q_len, batch, max_ctx_len, bounds, stream) -> None:
+    _check(load_library().comem_block_bounds(plan, k_pages, stride_page, stride_token, stride_head, page_size, num_pages,
+                                             block_table, max_pages_per_seq, ctx_lens, q_lens, max_q_len, batch,
+                                             max_ctx_len, bounds, stream), "comem_block_bounds")
+
+
+def comem_block_scores(plan, q, bounds, page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch,
+                       max_ctx_len, scores, scores_stride, stream) -> None:
+    _check(load_library().comem_block_scores(plan, q, bounds, page_size, num_pages, block_table, max_pages_per_seq,
+                                             ctx_lens, batch, max_ctx_len, scores, scores_stride, stream),
+           "comem_block_scores")
+
+
+def comem_block_select(plan, scores, scores_stride, page_size, block_table, max_pages_per_seq, ctx_lens, batch,
+                       max_ctx_len, budget, first, last, table, max_blocks, lens, stream) -> None:
+    _check(load_library().comem_block_select(plan, scores, scores_stride, page_size, block_table, max_pages_per_seq,
+                                             ctx_lens, batch, max_ctx_len, budget, first, last, table, max_blocks, lens,
+                                             stream), "comem_block_select")
+
+
+def comem_block_attn(plan, q, k_pages, v_pages, stride_page, stride_token, stride_head, page_size, num_pages, table,
+                     max_blocks, lens, batch, max_len, out, lse, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().comem_block_attn(plan, q, k_pages, v_pages, stride_page, stride_token, stride_head, page_size,
+                                           num_pages, table, max_blocks, lens, batch, max_len, out, lse, workspace,
+                                           workspace_bytes, stream), "comem_block_attn")
+
+
 def _cost_call(name, *args) -> float:
     out = ctypes.c_double()
     _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
@@ -539,6 +601,12 @@ def _check_tensor(name, t, dtypes, device, shape=None, ndim=None, contiguous=Tru
         _need(t.is_contiguous(), f"{name} must be contiguous")
 
 
+def _tensor_type():
+    import torch
+
+    return torch.Tensor
+
+
 def _fits(t, tensor, dtypes, device, shape) -> bool:
     """True only if _check_tensor would pass t as a contiguous tensor of this shape (the common case, in one
     expression: the checks of a call took 20-25 us on the host, several times as long as a short kernel)."""
@@ -579,6 +647,19 @@ def _empty_on(stream, like, shape, **dtype):
         t = like.new_empty(shape, **dtype)
     t.record_stream(reader)
     return t
+
+
+def _zeros_on(stream, like, shape):
+    """float32 zeros, of the call's stream as in _empty_on."""
+    import torch
+
+    t = _empty_on(stream, like, shape, dtype=torch.float32)
+    if stream is None:
+        return t.zero_()
+    if not isinstance(stream, torch.cuda.Stream):  # another object with a cuda_stream, as the calls take it
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=like.device)
+    with torch.cuda.stream(stream):
+        return t.zero_()
 
 
 # Placement of V relative to K that the C header recommends
@@ -1069,6 +1150,206 @@ class DecodeAttention:
                  strides[1], strides[2], pool[1], pool[0], block_table.data_ptr(), block_table.shape[1],
                  ctx_lens.data_ptr(), batch, int(max_ctx_len))
         return q_out
+
+
+    # Which tokens a context keeps: attention weights and the choice by them.
+
+    def _dense(self, name, t, dtype, shape):
+        """The address of a dense tensor of the plan's device."""
+        dev = self._torch_device
+        if not _fits(t, _tensor_type(), (dtype,), dev, shape):
+            _check_tensor(name, t, (dtype,), dev, shape=shape)
+        return t.data_ptr()
+
+    def _rows_of(self, name, t, rows, width):
+        """(address, row stride) of a float32 tensor [rows, width or more] with dense rows (rows None: any)."""
+        import torch
+
+        _check_tensor(name, t, (torch.float32,), self._torch_device, shape=(rows, None), contiguous=False)
+        _need((t.stride(1) == 1 or t.shape[1] <= 1) and t.shape[1] >= width,
+              f"{name} must have dense rows of at least {width} elements, got {tuple(t.shape)}")
+        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        _need(stride >= t.shape[1], f"the rows of {name} must not overlap")
+        return t.data_ptr(), stride
+
+    def _weights_args(self, q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior, decay, out, paged,
+                      stream):
+        import torch
+
+        self._check_q_out(q, None, lse)
+        _need(lse is not None, "lse must be a torch tensor, got NoneType")
+        self._check_cache(k, k, paged=paged)
+        self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_ctx_len)
+        _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
+        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
+        batch = ctx_lens.shape[0]
+        if q_lens is None:
+            _need(q.shape[0] == batch, f"q has {q.shape[0]} rows, expected one for each of {batch} sequences")
+            first = count = None
+        else:
+            first = self._dense("q_start", q_start, torch.int64, (batch,))
+            count = self._dense("q_lens", q_lens, torch.int32, (batch,))
+        if out is None:
+            out = _zeros_on(stream, q, (batch, int(max_ctx_len)))
+        to, stride = self._rows_of("out", out, batch, int(max_ctx_len))
+        old = None
+        if prior is not None:
+            old, prior_stride = self._rows_of("prior", prior, batch, int(max_ctx_len))
+            _need(prior_stride == stride or batch <= 1, "prior and out must have the same row stride")
+        return batch, out, (self.plan, q.data_ptr(), lse.data_ptr(), first, count, int(max_q_len), k.data_ptr()), (
+            ctx_lens.data_ptr(), batch, int(max_ctx_len), old, float(decay), to, stride)
+
+    def attn_weights(self, q, lse, k, seq_start, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
+                     max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None):
+        """What each cached token was paid by the new tokens' queries q [rows, Hq, D], whose attention returned lse
+        [rows, Hq]: out[b, t] = decay * prior[b, t] + the sum of its attention weights over heads and new tokens.
+
+        Without q_start and q_lens each sequence has one new token, else as in prefill. out (float32 [B, >= max_ctx_len])
+        may be prior itself; the new tokens' own prior is 0, and elements past a context stay (0 where out is made here).
+        """
+        batch, out, head, tail = self._weights_args(q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior,
+                                                    decay, out, False, stream)
+        self._check_lengths(ctx_lens, batch, seq_start=seq_start)
+        _call_on(self, stream, comem_attn_weights, *head, k.stride(0), k.stride(1), seq_start.data_ptr(), *tail)
+        return out
+
+    def attn_weights_paged(self, q, lse, k_pages, block_table, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
+                           max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None):
+        """The same over a paged cache."""
+        batch, out, head, tail = self._weights_args(q, lse, k_pages, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len,
+                                                    prior, decay, out, True, stream)
+        self._check_lengths(ctx_lens, batch, block_table=block_table)
+        pool, strides = k_pages.shape, k_pages.stride()
+        _call_on(self, stream, comem_attn_weights_paged, *head, strides[0], strides[1], strides[2], pool[1], pool[0],
+                 block_table.data_ptr(), block_table.shape[1], *tail)
+        return out
+
+    def keep_tokens(self, weights, ctx_lens, max_ctx_len: int, budget: int, first: int = 0, last: int = 0, rows=None,
+                    budgets=None, keep=None, kept=None, stream=None):
+        """The tokens that stay when contexts are cut to `budget`: the first, the last and the most attended ones.
+
+        weights float32 [R, >= max_ctx_len] and ctx_lens int32 [R] are those of all rows; rows (int32 [n]) names the ones
+        to cut (None: all), budgets (int32 [n]) budgets of their own. Returns keep [n, budget], keep_start, keep_lens and
+        kept [n, budget], the weights of the kept tokens. KVPages.compact takes
+        (rows, keep.view(-1), keep_start, keep_lens).
+        """
+        import torch
+
+        self._check_bound(max_ctx_len)
+        for name, v in (("budget", budget), ("first", first), ("last", last)):
+            self._check_bound(v, name)
+        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
+        total = ctx_lens.shape[0]
+        src, stride = self._rows_of("weights", weights, total, int(max_ctx_len))
+        which, n = None, total
+        if rows is not None:
+            _check_tensor("rows", rows, (torch.int32,), self._torch_device, ndim=1)
+            which, n = rows.data_ptr(), rows.shape[0]
+        own = None if budgets is None else self._dense("budgets", budgets, torch.int32, (n,))
+        width = int(budget)
+        if keep is None:
+            keep = _empty_on(stream, ctx_lens, (n, width))
+        else:
+            self._dense("keep", keep, torch.int32, (n, width))
+        if kept is None:
+            kept = _empty_on(stream, weights, (n, width))
+        else:
+            self._dense("kept", kept, torch.float32, (n, width))
+        start, lens = _empty_on(stream, ctx_lens, (n,), dtype=torch.int64), _empty_on(stream, ctx_lens, (n,))
+        _call_on(self, stream, comem_keep_tokens, self.plan, src, stride, ctx_lens.data_ptr(), total, which, n,
+                 int(max_ctx_len), width, own, int(first), int(last), keep.data_ptr(), width, start.data_ptr(),
+                 lens.data_ptr(), kept.data_ptr())
+        return keep, start, lens, kept
+
+    # Attention over chosen blocks (pages) of a paged cache.
+
+    def _blocks_of(self, page_size, block_table, ctx_lens, max_ctx_len):
+        """Checks of what the block calls share; (batch, blocks of the longest context)."""
+        import torch
+
+        self._check_bound(page_size, "page_size")
+        self._check_bound(max_ctx_len)
+        _need(page_size > 0, f"page_size must be positive, got {page_size}")
+        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
+        self._check_lengths(ctx_lens, ctx_lens.shape[0], block_table=block_table)
+        return ctx_lens.shape[0], -(-int(max_ctx_len) // int(page_size))
+
+    def block_bounds(self, k_pages, block_table, ctx_lens, max_ctx_len: int, bounds, q_lens=None, max_q_len: int = 1,
+                     stream=None):
+        """Least and greatest keys of the pages that each sequence's last q_lens[b] tokens (None: one) lie in, into
+        bounds [P, Hkv, 2, D] of the cache's type. Call it after new tokens were stored and after compact and fork."""
+        import torch
+
+        self._check_cache(k_pages, k_pages, paged=True)
+        batch, _ = self._blocks_of(k_pages.shape[1], block_table, ctx_lens, max_ctx_len)
+        self._check_bound(max_q_len, "max_q_len")
+        pool, strides = k_pages.shape, k_pages.stride()
+        to = self._dense("bounds", bounds, k_pages.dtype, (pool[0], self.num_kv_heads, 2, self.head_dim))
+        count = None if q_lens is None else self._dense("q_lens", q_lens, torch.int32, (batch,))
+        _call_on(self, stream, comem_block_bounds, self.plan, k_pages.data_ptr(), strides[0], strides[1], strides[2],
+                 pool[1], pool[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), count,
+                 int(max_q_len), batch, int(max_ctx_len), to)
+        return bounds
+
+    def block_scores(self, q, bounds, page_size: int, block_table, ctx_lens, max_ctx_len: int, scores=None, stream=None):
+        """Bounds of the scores that q [B, Hq, D] reaches in each block: [B, Hkv, blocks of max_ctx_len] (elements past a
+        context's blocks are left as they were)."""
+        import torch
+
+        self._check_q_out(q, None, None)
+        batch, blocks = self._blocks_of(page_size, block_table, ctx_lens, max_ctx_len)
+        _need(q.shape[0] == batch, f"q has {q.shape[0]} rows, expected one for each of {batch} sequences")
+        if not (isinstance(bounds, torch.Tensor) and bounds.dim() == 4 and bounds.dtype in self._kv_dtypes):
+            _check_tensor("bounds", bounds, self._kv_dtypes, self._torch_device, ndim=4)
+        at = self._dense("bounds", bounds, bounds.dtype, (bounds.shape[0], self.num_kv_heads, 2, self.head_dim))
+        if scores is None:
+            scores = _empty_on(stream, q, (batch, self.num_kv_heads, blocks), dtype=torch.float32)
+        to = self._dense("scores", scores, torch.float32, (batch, self.num_kv_heads, blocks))
+        _call_on(self, stream, comem_block_scores, self.plan, q.data_ptr(), at, int(page_size), bounds.shape[0],
+                 block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len), to, blocks)
+        return scores
+
+    def block_select(self, scores, page_size: int, block_table, ctx_lens, max_ctx_len: int, budget: int, first: int = 1,
+                     last: int = 1, table=None, lens=None, stream=None):
+        """The pages of the `budget` blocks that each KV head attends: the first, the last (one at least) and those of
+        the largest scores, in order. Returns table [B, Hkv, budget] and lens [B], the tokens in them."""
+        import torch
+
+        batch, blocks = self._blocks_of(page_size, block_table, ctx_lens, max_ctx_len)
+        for name, v in (("budget", budget), ("first", first), ("last", last)):
+            self._check_bound(v, name)
+        src = self._dense("scores", scores, torch.float32, (batch, self.num_kv_heads, blocks))
+        if table is None:
+            table = _empty_on(stream, ctx_lens, (batch, self.num_kv_heads, int(budget)))
+        if lens is None:
+            lens = _empty_on(stream, ctx_lens, (batch,))
+        to = self._dense("table", table, torch.int32, (batch, self.num_kv_heads, int(budget)))
+        count = self._dense("lens", lens, torch.int32, (batch,))
+        _call_on(self, stream, comem_block_select, self.plan, src, blocks, int(page_size), block_table.data_ptr(),
+                 block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len), int(budget), int(first), int(last),
+                 to, int(budget), count)
+        return table, lens
+
+    def block_forward(self, q, k_pages, v_pages, table, lens, max_len: int, out=None, lse=None, stream=None):
+        """Decode attention with a block table for each KV head: head hk of sequence b attends over the first lens[b]
+        tokens of the pages table[b, hk] (block_select's results; max_len bounds lens)."""
+        import torch
+
+        self._check_q_out(q, out, lse)
+        self._check_cache(k_pages, v_pages, paged=True)
+        self._check_bound(max_len, "max_len")
+        batch = q.shape[0]
+        _need(isinstance(table, torch.Tensor) and table.dim() == 3, "table must be a torch tensor [B, Hkv, blocks]")
+        pages = self._dense("table", table, torch.int32, (batch, self.num_kv_heads, table.shape[2]))
+        count = self._dense("lens", lens, torch.int32, (batch,))
+        out, lse = self._outputs(q, out, lse)
+        pool, strides = k_pages.shape, k_pages.stride()
+        _call_on(self, stream, comem_block_attn, self.plan, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                 strides[0], strides[1], strides[2], pool[1], pool[0], pages, table.shape[2], count, batch, int(max_len),
+                 out.data_ptr(), None if lse is None else lse.data_ptr(), self.workspace.data_ptr(),
+                 self.workspace_bytes)
+        return out, lse
 
 
 class KVPages:

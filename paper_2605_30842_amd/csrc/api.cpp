@@ -9,6 +9,7 @@
 #include <new>
 
 #include "attn_common.h"
+#include "comem_block_attn.h"
 #include "comem_decode_attn.h"
 #include "kv_append.h"
 #include "noalloc.h"
@@ -506,7 +507,7 @@ comem_status decode_paged(const comem_decode_attn_plan* plan, const void* q, con
                           int64_t stride_token, int64_t stride_head, int32_t page_size, int64_t num_pages,
                           const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
                           int32_t batch, int64_t max_ctx_len, float* out, float* lse, void* workspace,
-                          size_t workspace_bytes, void* hip_stream, bool fused) {
+                          size_t workspace_bytes, void* hip_stream, bool fused, bool head_tables = false) {
   const comem_decode_attn_plan* p = checked(plan);
   if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
   comem_status st = validate_common(*p, q, k_pages, v_pages, stride_token, stride_head, ctx_lens, batch,
@@ -537,6 +538,7 @@ comem_status decode_paged(const comem_decode_attn_plan* plan, const void* q, con
   a.block_table = block_table;
   a.stride_page = stride_page * elem_bytes(p->cfg);
   a.max_pages = max_pages_per_seq;
+  a.head_tables = head_tables ? p->cfg.num_kv_heads : 1;
   a.num_pages = num_pages;
   a.page_shift = log2_of(page_size);
   a.page_mask = page_size - 1;
@@ -724,6 +726,16 @@ comem_status comem_decode_attn_paged(const comem_decode_attn_plan* plan, const v
   return decode_paged(plan, q, nullptr, nullptr, k_pages, v_pages, stride_page, stride_token, stride_head,
                       page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len, out, lse,
                       workspace, workspace_bytes, hip_stream, false);
+}
+
+comem_status comem_block_attn(const comem_decode_attn_plan* plan, const void* q, const void* k_pages,
+                              const void* v_pages, int64_t stride_page, int64_t stride_token, int64_t stride_head,
+                              int32_t page_size, int64_t num_pages, const int32_t* table, int32_t max_blocks,
+                              const int32_t* lens, int32_t batch, int64_t max_len, float* out, float* lse,
+                              void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return decode_paged(plan, q, nullptr, nullptr, k_pages, v_pages, stride_page, stride_token, stride_head, page_size,
+                      num_pages, table, max_blocks, lens, batch, max_len, out, lse, workspace, workspace_bytes,
+                      hip_stream, false, true);
 }
 
 comem_status comem_append_decode_attn(const comem_decode_attn_plan* plan, const void* q, const void* new_k,

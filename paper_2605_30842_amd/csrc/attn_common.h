@@ -43,11 +43,12 @@ struct AttnParams {
   float* lse;          // [B, Hq] or nullptr
   const int64_t* seq_start;   // contiguous layout
   const int32_t* ctx_lens;
-  const int32_t* block_table; // paged layout, [B, max_pages]
+  const int32_t* block_table; // paged layout, [B, max_pages], or of each KV head [B, Hkv, max_pages]
   int64_t stride_token;
   int64_t stride_head;
   int64_t stride_page;
-  int32_t max_pages;
+  int32_t max_pages;   // entries of a table row
+  int32_t head_tables; // table rows of a sequence: 1, or Hkv
   int32_t page_shift;  // log2(page_size)
   int32_t page_mask;   // page_size - 1
   int32_t num_q_heads;
@@ -113,12 +114,17 @@ __device__ inline int uniform_i32(int x) {
   return static_cast<int>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)));
 }
 
-// Byte offset of token t of sequence b relative to the (hk-offset) K/V base.
+// Block-table row of KV head hk of sequence b.
+__device__ inline const int32_t* table_row(const AttnParams& p, int b, int hk) {
+  const int64_t row = static_cast<int64_t>(b) * p.head_tables + (p.head_tables > 1 ? hk : 0);
+  return p.block_table + row * p.max_pages;
+}
+
+// Byte offset of token t of a sequence relative to the (hk-offset) K/V base.
 template <bool PAGED>
-__device__ inline int64_t row_offset(const AttnParams& p, int b, int64_t seq0, int t) {
+__device__ inline int64_t row_offset(const AttnParams& p, const int32_t* bt_row, int64_t seq0, int t) {
   if constexpr (PAGED) {
-    const int page = max(0, checked_page(p.block_table[static_cast<int64_t>(b) * p.max_pages + (t >> p.page_shift)],
-                                         p.num_pages, p.errors));
+    const int page = max(0, checked_page(bt_row[t >> p.page_shift], p.num_pages, p.errors));
     return static_cast<int64_t>(page) * p.stride_page +
            static_cast<int64_t>(t & p.page_mask) * p.stride_token;
   } else {

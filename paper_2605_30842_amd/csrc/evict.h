@@ -1,0 +1,82 @@
+// Kernel arguments of the attention-weight and choice kernels (host and device side).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "comem_decode_attn.h"
+
+namespace comem {
+
+enum class CacheType { kF32, kBf16, kFp8 };
+
+inline CacheType cache_type(const comem_decode_attn_config& c) {
+  return c.dtype == COMEM_F32 ? CacheType::kF32 : c.dtype == COMEM_BF16 ? CacheType::kBf16 : CacheType::kFp8;
+}
+
+constexpr int kWeightsWaves = 4;  // waves of a workgroup, on the same tokens
+
+// Offsets and strides are in bytes, but for that of the weights.
+struct WeightsParams {
+  const char* q;               // [rows, Hq, D]
+  const float* lse;            // [rows, Hq]
+  const char* k;               // contiguous: [T, Hkv, D] rows; paged: page pool
+  const int64_t* q_start;      // nullptr: one token per sequence
+  const int32_t* q_lens;
+  const int64_t* seq_start;    // contiguous layout
+  const int32_t* ctx_lens;
+  const int32_t* block_table;  // paged layout, [B, max_pages]
+  const float* prior;          // or nullptr
+  float* weights;
+  int64_t weights_stride;
+  int64_t stride_token;
+  int64_t stride_head;
+  int64_t stride_page;
+  int64_t num_pages;
+  int32_t max_pages;
+  int32_t page_shift;
+  int32_t page_mask;
+  int32_t max_ctx;
+  int32_t max_q;
+  int32_t num_kv_heads;
+  int32_t group_shift;         // log2(G)
+  float scale_log2;            // scale * log2(e), times the K scale of an FP8 cache
+  float decay;
+};
+
+using WeightsKernelFn = void (*)(WeightsParams);
+// sub: 16-token slabs of a workgroup, 1, 2 or 4 (float32: at most 2).
+WeightsKernelFn select_weights_kernel(int head_dim, CacheType cache, bool paged, int sub);
+
+// The largest entries of a row, in ascending order.
+struct ChooseParams {
+  const float* scores;
+  int64_t scores_stride;
+  const int32_t* lens;         // tokens of each row or sequence
+  const int32_t* rows;         // tokens: row of each item, or nullptr
+  const int32_t* budgets;      // tokens: each item's, or nullptr
+  int32_t num_rows;
+  int32_t max_len;             // bound of lens
+  int32_t budget;
+  int32_t first;
+  int32_t last;
+  int32_t* out;                // positions (tokens) or pages (blocks)
+  int64_t out_stride;
+  int64_t* out_start;          // tokens, or nullptr
+  int32_t* out_lens;
+  float* kept;                 // tokens, or nullptr
+  const int32_t* block_table;  // blocks, [B, max_pages]
+  int32_t max_pages;
+  int32_t heads;               // items of a sequence
+  int32_t page_shift;
+};
+
+using ChooseKernelFn = void (*)(ChooseParams);
+struct ChooseForm {
+  ChooseKernelFn fn;
+  int threads;
+};
+// For rows of at most `most` entries; one workgroup per item.
+ChooseForm select_choose_kernel(bool blocks, int64_t most);
+
+}  // namespace comem

@@ -441,7 +441,7 @@ __device__ void attend_split(const AttnParams& p, WaveState<D>& ws, int b, int h
     ld.kbase += seq0;
     ld.vbase += seq0;
   } else {
-    ld.bt_row = p.block_table + static_cast<int64_t>(b) * p.max_pages;
+    ld.bt_row = table_row(p, b, hk);
   }
   ld.pool = static_cast<uint32_t>(min(p.num_pages, int64_t{1} << 31));
   ld.errors = p.errors;

@@ -167,6 +167,7 @@ __global__ __launch_bounds__(kThreads) void decode_valu_kernel(const AttnParams 
   }
   const char* kb = p.k + hk * p.stride_head;
   const char* vb = p.v + hk * p.stride_head;
+  const int32_t* bt_row = PAGED ? table_row(p, b, hk) : nullptr;
 
   float m[G], l[G], acc[G][VEC];
 #pragma unroll
@@ -183,8 +184,7 @@ __global__ __launch_bounds__(kThreads) void decode_valu_kernel(const AttnParams 
   if (p.new_k != nullptr && t_end == L && L > 0 && w == ((L - 1 - t_begin) / TT) % kWaves && p.ctx_lens[b] == L) {
     int64_t row;
     if constexpr (PAGED) {
-      row = checked_page_row(p, p.block_table[static_cast<int64_t>(b) * p.max_pages + ((L - 1) >> p.page_shift)],
-                             L - 1);
+      row = checked_page_row(p, bt_row[(L - 1) >> p.page_shift], L - 1);
     } else {
       row = (seq0 + L - 1) * p.stride_token;
     }
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void decode_valu_kernel(const AttnParams 
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = min(base + u * RPL + rho, t_end - 1);
-      const int64_t off = row_offset<PAGED>(p, b, seq0, t) + ds * 16;
+      const int64_t off = row_offset<PAGED>(p, bt_row, seq0, t) + ds * 16;
       k[u] = *reinterpret_cast<const u32x4*>(kb + off);
       v[u] = *reinterpret_cast<const u32x4*>(vb + off);
     }
