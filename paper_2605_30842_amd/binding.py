@@ -601,12 +601,6 @@ def _check_tensor(name, t, dtypes, device, shape=None, ndim=None, contiguous=Tru
         _need(t.is_contiguous(), f"{name} must be contiguous")
 
 
-def _tensor_type():
-    import torch
-
-    return torch.Tensor
-
-
 def _fits(t, tensor, dtypes, device, shape) -> bool:
     """True only if _check_tensor would pass t as a contiguous tensor of this shape (the common case, in one
     expression: the checks of a call took 20-25 us on the host, several times as long as a short kernel)."""
@@ -729,6 +723,7 @@ class DecodeAttention:
         self.dtype = dtype
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
         self._torch_device = torch.device("cuda", device)
+        self._at = device
         self._q_dtypes, self._kv_dtypes = _torch_dtypes(dtype)
         self.plan, self.workspace_bytes = comem_decode_attn_init(self.cfg, device)
         self.workspace = torch.zeros(max(self.workspace_bytes, 256), dtype=torch.uint8, device=f"cuda:{device}")
@@ -1153,52 +1148,69 @@ class DecodeAttention:
 
 
     # Which tokens a context keeps: attention weights and the choice by them.
+    #
+    # Each call below checks its tensors in one expression first, as those above do; what does not pass is looked at
+    # piece by piece, for what is wrong with it.
+
+    _at = -1  # the plan's device as tensors report it (set with the device)
 
     def _dense(self, name, t, dtype, shape):
-        """The address of a dense tensor of the plan's device."""
-        dev = self._torch_device
-        if not _fits(t, _tensor_type(), (dtype,), dev, shape):
-            _check_tensor(name, t, (dtype,), dev, shape=shape)
-        return t.data_ptr()
+        """A dense tensor of the plan's device, or ValueError."""
+        _check_tensor(name, t, (dtype,), self._torch_device, shape=shape)
 
-    def _rows_of(self, name, t, rows, width):
-        """(address, row stride) of a float32 tensor [rows, width or more] with dense rows (rows None: any)."""
+    def _check_rows_of(self, name, t, rows, width):
+        """A float32 tensor [rows, width or more] with dense rows that do not overlap."""
         import torch
 
         _check_tensor(name, t, (torch.float32,), self._torch_device, shape=(rows, None), contiguous=False)
         _need((t.stride(1) == 1 or t.shape[1] <= 1) and t.shape[1] >= width,
               f"{name} must have dense rows of at least {width} elements, got {tuple(t.shape)}")
-        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-        _need(stride >= t.shape[1], f"the rows of {name} must not overlap")
-        return t.data_ptr(), stride
+        _need(rows <= 1 or t.stride(0) >= t.shape[1], f"the rows of {name} must not overlap")
 
     def _weights_args(self, q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior, decay, out, paged,
                       stream):
         import torch
 
-        self._check_q_out(q, None, lse)
-        _need(lse is not None, "lse must be a torch tensor, got NoneType")
-        self._check_cache(k, k, paged=paged)
+        tensor, at, f32, i32 = torch.Tensor, self._at, torch.float32, torch.int32
+        fast = False
+        if isinstance(q, tensor) and isinstance(lse, tensor) and isinstance(ctx_lens, tensor):
+            shape, lens = q.shape, ctx_lens.shape
+            fast = (len(shape) == 3 and shape[1] == self.num_q_heads and shape[2] == self.head_dim
+                    and q.dtype in self._q_dtypes and q.get_device() == at and q.is_contiguous()
+                    and lse.shape == shape[:2] and lse.dtype is f32 and lse.get_device() == at and lse.is_contiguous()
+                    and len(lens) == 1 and ctx_lens.dtype is i32 and ctx_lens.get_device() == at
+                    and (shape[0] == lens[0] if q_lens is q_start is None else
+                         isinstance(q_lens, tensor) and q_lens.dtype is i32 and q_lens.get_device() == at
+                         and isinstance(q_start, tensor) and q_start.dtype is torch.int64
+                         and q_start.get_device() == at and q_lens.shape == q_start.shape == lens
+                         and q_lens.is_contiguous() and q_start.is_contiguous()))
         self._check_bound(max_q_len, "max_q_len")
         self._check_bound(max_ctx_len)
-        _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
-        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
-        batch = ctx_lens.shape[0]
-        if q_lens is None:
-            _need(q.shape[0] == batch, f"q has {q.shape[0]} rows, expected one for each of {batch} sequences")
-            first = count = None
-        else:
-            first = self._dense("q_start", q_start, torch.int64, (batch,))
-            count = self._dense("q_lens", q_lens, torch.int32, (batch,))
+        if not fast:
+            self._check_q_out(q, None, lse)
+            _need(lse is not None, "lse must be a torch tensor, got NoneType")
+            _need((q_start is None) == (q_lens is None), "q_start and q_lens go together")
+            _check_tensor("ctx_lens", ctx_lens, (i32,), self._torch_device, ndim=1)
+            lens = ctx_lens.shape
+            if q_lens is None:
+                _need(q.shape[0] == lens[0], f"q has {q.shape[0]} rows, expected one for each of {lens[0]} sequences")
+            else:
+                self._dense("q_start", q_start, torch.int64, lens)
+                self._dense("q_lens", q_lens, i32, lens)
+        self._check_cache(k, k, paged=paged)
+        batch, width = lens[0], int(max_ctx_len)
         if out is None:
-            out = _zeros_on(stream, q, (batch, int(max_ctx_len)))
-        to, stride = self._rows_of("out", out, batch, int(max_ctx_len))
-        old = None
-        if prior is not None:
-            old, prior_stride = self._rows_of("prior", prior, batch, int(max_ctx_len))
-            _need(prior_stride == stride or batch <= 1, "prior and out must have the same row stride")
-        return batch, out, (self.plan, q.data_ptr(), lse.data_ptr(), first, count, int(max_q_len), k.data_ptr()), (
-            ctx_lens.data_ptr(), batch, int(max_ctx_len), old, float(decay), to, stride)
+            out = _zeros_on(stream, q, (batch, width))
+        for name, t in (("out", out),) if prior is None else (("out", out), ("prior", prior)):
+            if not (isinstance(t, tensor) and t.dtype is f32 and t.get_device() == at and t.is_contiguous()
+                    and t.dim() == 2 and t.shape[0] == batch and t.shape[1] >= width):
+                self._check_rows_of(name, t, batch, width)
+        stride = out.stride(0) if batch > 1 else out.shape[1]
+        _need(prior is None or batch <= 1 or prior.stride(0) == stride, "prior and out must have the same row stride")
+        return batch, out, (self.plan, q.data_ptr(), lse.data_ptr(), None if q_start is None else q_start.data_ptr(),
+                            None if q_lens is None else q_lens.data_ptr(), int(max_q_len), k.data_ptr()), (
+            ctx_lens.data_ptr(), batch, width, None if prior is None else prior.data_ptr(), float(decay),
+            out.data_ptr(), stride)
 
     def attn_weights(self, q, lse, k, seq_start, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
                      max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None):
@@ -1236,44 +1248,57 @@ class DecodeAttention:
         """
         import torch
 
-        self._check_bound(max_ctx_len)
-        for name, v in (("budget", budget), ("first", first), ("last", last)):
-            self._check_bound(v, name)
-        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
-        total = ctx_lens.shape[0]
-        src, stride = self._rows_of("weights", weights, total, int(max_ctx_len))
-        which, n = None, total
-        if rows is not None:
-            _check_tensor("rows", rows, (torch.int32,), self._torch_device, ndim=1)
-            which, n = rows.data_ptr(), rows.shape[0]
-        own = None if budgets is None else self._dense("budgets", budgets, torch.int32, (n,))
+        tensor, at, i32 = torch.Tensor, self._at, torch.int32
+        for name, v in (("max_ctx_len", max_ctx_len), ("budget", budget), ("first", first), ("last", last)):
+            if type(v) is not int:
+                self._check_bound(v, name)
         width = int(budget)
+        if not (isinstance(weights, tensor) and isinstance(ctx_lens, tensor) and ctx_lens.dtype is i32
+                and ctx_lens.dim() == 1 and ctx_lens.get_device() == at and ctx_lens.is_contiguous()
+                and weights.dtype is torch.float32 and weights.get_device() == at and weights.is_contiguous()
+                and weights.dim() == 2 and weights.shape[0] == ctx_lens.shape[0] and weights.shape[1] >= max_ctx_len):
+            _check_tensor("ctx_lens", ctx_lens, (i32,), self._torch_device, ndim=1)
+            self._check_rows_of("weights", weights, ctx_lens.shape[0], int(max_ctx_len))
+        total = n = ctx_lens.shape[0]
+        if rows is not None:
+            _check_tensor("rows", rows, (i32,), self._torch_device, ndim=1)
+            n = rows.shape[0]
+        if budgets is not None:
+            self._dense("budgets", budgets, i32, (n,))
         if keep is None:
             keep = _empty_on(stream, ctx_lens, (n, width))
-        else:
-            self._dense("keep", keep, torch.int32, (n, width))
+        elif not _fits(keep, tensor, (i32,), self._torch_device, (n, width)):
+            self._dense("keep", keep, i32, (n, width))
         if kept is None:
             kept = _empty_on(stream, weights, (n, width))
-        else:
+        elif not _fits(kept, tensor, (torch.float32,), self._torch_device, (n, width)):
             self._dense("kept", kept, torch.float32, (n, width))
         start, lens = _empty_on(stream, ctx_lens, (n,), dtype=torch.int64), _empty_on(stream, ctx_lens, (n,))
-        _call_on(self, stream, comem_keep_tokens, self.plan, src, stride, ctx_lens.data_ptr(), total, which, n,
-                 int(max_ctx_len), width, own, int(first), int(last), keep.data_ptr(), width, start.data_ptr(),
-                 lens.data_ptr(), kept.data_ptr())
+        _call_on(self, stream, comem_keep_tokens, self.plan, weights.data_ptr(),
+                 weights.stride(0) if total > 1 else weights.shape[1], ctx_lens.data_ptr(), total,
+                 None if rows is None else rows.data_ptr(), n, int(max_ctx_len), width,
+                 None if budgets is None else budgets.data_ptr(), int(first), int(last), keep.data_ptr(), width,
+                 start.data_ptr(), lens.data_ptr(), kept.data_ptr())
         return keep, start, lens, kept
 
     # Attention over chosen blocks (pages) of a paged cache.
 
-    def _blocks_of(self, page_size, block_table, ctx_lens, max_ctx_len):
-        """Checks of what the block calls share; (batch, blocks of the longest context)."""
+    def _check_blocks(self, page_size, block_table, ctx_lens, max_ctx_len):
+        """What the block calls share; returns the batch and the blocks of the longest context."""
         import torch
 
-        self._check_bound(page_size, "page_size")
-        self._check_bound(max_ctx_len)
+        tensor, at, i32 = torch.Tensor, self._at, torch.int32
+        if type(page_size) is not int or type(max_ctx_len) is not int:
+            self._check_bound(page_size, "page_size")
+            self._check_bound(max_ctx_len)
         _need(page_size > 0, f"page_size must be positive, got {page_size}")
-        _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
-        self._check_lengths(ctx_lens, ctx_lens.shape[0], block_table=block_table)
-        return ctx_lens.shape[0], -(-int(max_ctx_len) // int(page_size))
+        if not (isinstance(ctx_lens, tensor) and isinstance(block_table, tensor) and ctx_lens.dtype is i32
+                and block_table.dtype is i32 and ctx_lens.get_device() == at and block_table.get_device() == at
+                and ctx_lens.dim() == 1 and block_table.dim() == 2 and block_table.shape[0] == ctx_lens.shape[0]
+                and ctx_lens.is_contiguous() and block_table.is_contiguous()):
+            _check_tensor("ctx_lens", ctx_lens, (i32,), self._torch_device, ndim=1)
+            self._check_lengths(ctx_lens, ctx_lens.shape[0], block_table=block_table)
+        return ctx_lens.shape[0], -(-max_ctx_len // page_size)
 
     def block_bounds(self, k_pages, block_table, ctx_lens, max_ctx_len: int, bounds, q_lens=None, max_q_len: int = 1,
                      stream=None):
@@ -1282,14 +1307,20 @@ class DecodeAttention:
         import torch
 
         self._check_cache(k_pages, k_pages, paged=True)
-        batch, _ = self._blocks_of(k_pages.shape[1], block_table, ctx_lens, max_ctx_len)
-        self._check_bound(max_q_len, "max_q_len")
         pool, strides = k_pages.shape, k_pages.stride()
-        to = self._dense("bounds", bounds, k_pages.dtype, (pool[0], self.num_kv_heads, 2, self.head_dim))
-        count = None if q_lens is None else self._dense("q_lens", q_lens, torch.int32, (batch,))
+        batch, _ = self._check_blocks(pool[1], block_table, ctx_lens, max_ctx_len)
+        if type(max_q_len) is not int:
+            self._check_bound(max_q_len, "max_q_len")
+        shape = (pool[0], pool[2], 2, pool[3])
+        if not (isinstance(bounds, torch.Tensor) and bounds.dtype is k_pages.dtype and bounds.get_device() == self._at
+                and bounds.shape == shape and bounds.is_contiguous()):
+            self._dense("bounds", bounds, k_pages.dtype, shape)
+        if q_lens is not None:
+            self._dense("q_lens", q_lens, torch.int32, (batch,))
         _call_on(self, stream, comem_block_bounds, self.plan, k_pages.data_ptr(), strides[0], strides[1], strides[2],
-                 pool[1], pool[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), count,
-                 int(max_q_len), batch, int(max_ctx_len), to)
+                 pool[1], pool[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(),
+                 None if q_lens is None else q_lens.data_ptr(), int(max_q_len), batch, int(max_ctx_len),
+                 bounds.data_ptr())
         return bounds
 
     def block_scores(self, q, bounds, page_size: int, block_table, ctx_lens, max_ctx_len: int, scores=None, stream=None):
@@ -1297,17 +1328,22 @@ class DecodeAttention:
         context's blocks are left as they were)."""
         import torch
 
-        self._check_q_out(q, None, None)
-        batch, blocks = self._blocks_of(page_size, block_table, ctx_lens, max_ctx_len)
-        _need(q.shape[0] == batch, f"q has {q.shape[0]} rows, expected one for each of {batch} sequences")
-        if not (isinstance(bounds, torch.Tensor) and bounds.dim() == 4 and bounds.dtype in self._kv_dtypes):
-            _check_tensor("bounds", bounds, self._kv_dtypes, self._torch_device, ndim=4)
-        at = self._dense("bounds", bounds, bounds.dtype, (bounds.shape[0], self.num_kv_heads, 2, self.head_dim))
+        tensor, at, hkv, d = torch.Tensor, self._at, self.num_kv_heads, self.head_dim
+        batch, blocks = self._check_blocks(page_size, block_table, ctx_lens, max_ctx_len)
         if scores is None:
-            scores = _empty_on(stream, q, (batch, self.num_kv_heads, blocks), dtype=torch.float32)
-        to = self._dense("scores", scores, torch.float32, (batch, self.num_kv_heads, blocks))
-        _call_on(self, stream, comem_block_scores, self.plan, q.data_ptr(), at, int(page_size), bounds.shape[0],
-                 block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len), to, blocks)
+            scores = _empty_on(stream, ctx_lens, (batch, hkv, blocks), dtype=torch.float32)
+        if not (isinstance(q, tensor) and isinstance(bounds, tensor) and isinstance(scores, tensor)
+                and q.shape == (batch, self.num_q_heads, d) and q.dtype in self._q_dtypes and q.get_device() == at
+                and q.is_contiguous() and bounds.dim() == 4 and bounds.shape[1:] == (hkv, 2, d)
+                and bounds.dtype in self._kv_dtypes and bounds.get_device() == at and bounds.is_contiguous()
+                and scores.shape == (batch, hkv, blocks) and scores.dtype is torch.float32
+                and scores.get_device() == at and scores.is_contiguous()):
+            self._check_q_out(q, None, None, rows=batch)
+            _check_tensor("bounds", bounds, self._kv_dtypes, self._torch_device, shape=(None, hkv, 2, d))
+            self._dense("scores", scores, torch.float32, (batch, hkv, blocks))
+        _call_on(self, stream, comem_block_scores, self.plan, q.data_ptr(), bounds.data_ptr(), int(page_size),
+                 bounds.shape[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch,
+                 int(max_ctx_len), scores.data_ptr(), blocks)
         return scores
 
     def block_select(self, scores, page_size: int, block_table, ctx_lens, max_ctx_len: int, budget: int, first: int = 1,
@@ -1316,19 +1352,27 @@ class DecodeAttention:
         the largest scores, in order. Returns table [B, Hkv, budget] and lens [B], the tokens in them."""
         import torch
 
-        batch, blocks = self._blocks_of(page_size, block_table, ctx_lens, max_ctx_len)
-        for name, v in (("budget", budget), ("first", first), ("last", last)):
-            self._check_bound(v, name)
-        src = self._dense("scores", scores, torch.float32, (batch, self.num_kv_heads, blocks))
+        tensor, at, hkv, i32 = torch.Tensor, self._at, self.num_kv_heads, torch.int32
+        batch, blocks = self._check_blocks(page_size, block_table, ctx_lens, max_ctx_len)
+        if not type(budget) is type(first) is type(last) is int:
+            for name, v in (("budget", budget), ("first", first), ("last", last)):
+                self._check_bound(v, name)
+        shape = (batch, hkv, int(budget))
         if table is None:
-            table = _empty_on(stream, ctx_lens, (batch, self.num_kv_heads, int(budget)))
+            table = _empty_on(stream, ctx_lens, shape)
         if lens is None:
             lens = _empty_on(stream, ctx_lens, (batch,))
-        to = self._dense("table", table, torch.int32, (batch, self.num_kv_heads, int(budget)))
-        count = self._dense("lens", lens, torch.int32, (batch,))
-        _call_on(self, stream, comem_block_select, self.plan, src, blocks, int(page_size), block_table.data_ptr(),
-                 block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len), int(budget), int(first), int(last),
-                 to, int(budget), count)
+        if not (isinstance(scores, tensor) and isinstance(table, tensor) and isinstance(lens, tensor)
+                and scores.shape == (batch, hkv, blocks) and scores.dtype is torch.float32
+                and scores.get_device() == at and scores.is_contiguous() and table.shape == shape
+                and table.dtype is i32 and table.get_device() == at and table.is_contiguous()
+                and lens.shape == (batch,) and lens.dtype is i32 and lens.get_device() == at and lens.is_contiguous()):
+            self._dense("scores", scores, torch.float32, (batch, hkv, blocks))
+            self._dense("table", table, i32, shape)
+            self._dense("lens", lens, i32, (batch,))
+        _call_on(self, stream, comem_block_select, self.plan, scores.data_ptr(), blocks, int(page_size),
+                 block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), batch, int(max_ctx_len),
+                 shape[2], int(first), int(last), table.data_ptr(), shape[2], lens.data_ptr())
         return table, lens
 
     def block_forward(self, q, k_pages, v_pages, table, lens, max_len: int, out=None, lse=None, stream=None):
@@ -1336,19 +1380,24 @@ class DecodeAttention:
         tokens of the pages table[b, hk] (block_select's results; max_len bounds lens)."""
         import torch
 
+        tensor, at, i32 = torch.Tensor, self._at, torch.int32
         self._check_q_out(q, out, lse)
         self._check_cache(k_pages, v_pages, paged=True)
-        self._check_bound(max_len, "max_len")
+        if type(max_len) is not int:
+            self._check_bound(max_len, "max_len")
         batch = q.shape[0]
-        _need(isinstance(table, torch.Tensor) and table.dim() == 3, "table must be a torch tensor [B, Hkv, blocks]")
-        pages = self._dense("table", table, torch.int32, (batch, self.num_kv_heads, table.shape[2]))
-        count = self._dense("lens", lens, torch.int32, (batch,))
+        if not (isinstance(table, tensor) and isinstance(lens, tensor) and table.dim() == 3 and table.dtype is i32
+                and table.shape[0] == batch and table.shape[1] == self.num_kv_heads and table.get_device() == at
+                and table.is_contiguous() and lens.shape == (batch,) and lens.dtype is i32
+                and lens.get_device() == at and lens.is_contiguous()):
+            self._dense("table", table, i32, (batch, self.num_kv_heads, None))
+            self._dense("lens", lens, i32, (batch,))
         out, lse = self._outputs(q, out, lse)
         pool, strides = k_pages.shape, k_pages.stride()
         _call_on(self, stream, comem_block_attn, self.plan, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                 strides[0], strides[1], strides[2], pool[1], pool[0], pages, table.shape[2], count, batch, int(max_len),
-                 out.data_ptr(), None if lse is None else lse.data_ptr(), self.workspace.data_ptr(),
-                 self.workspace_bytes)
+                 strides[0], strides[1], strides[2], pool[1], pool[0], table.data_ptr(), table.shape[2],
+                 lens.data_ptr(), batch, int(max_len), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                 self.workspace.data_ptr(), self.workspace_bytes)
         return out, lse
 
 

@@ -150,8 +150,8 @@ comem_status comem_block_select(const comem_decode_attn_plan* plan, const float*
   if (scores_stride < blocks || max_blocks < std::min<int64_t>(budget, blocks)) return COMEM_ERR_INVALID_SHAPE;
   if (!aligned(scores, 4) || !aligned(ctx_lens, 4) || !aligned(table, 4) || !aligned(lens, 4))
     return COMEM_ERR_MISALIGNED;
-  const comem::ChooseForm form = comem::select_choose_kernel(true, blocks);
   const int64_t items = int64_t{batch} * p->cfg.num_kv_heads;
+  const comem::ChooseForm form = comem::select_choose_kernel(true, blocks, items, p->num_cus);
   if (items > ((int64_t{1} << 32) - 1) / form.threads) return COMEM_ERR_INVALID_SHAPE;  // more than a launch holds
   if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
   comem::ChooseParams a;
@@ -170,7 +170,7 @@ comem_status comem_block_select(const comem_decode_attn_plan* plan, const float*
   a.max_pages = max_pages_per_seq;
   a.heads = p->cfg.num_kv_heads;
   a.page_shift = log2_of(page_size);
-  return launched(form.fn, dim3(static_cast<unsigned>(items)), form.threads, a, hip_stream);
+  return launched(form.fn, dim3(static_cast<unsigned>(items), static_cast<unsigned>(form.parts)), form.threads, a, hip_stream);
 }
 
 }  // extern "C"

@@ -162,10 +162,10 @@ comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* 
   a.out_start = keep_start;
   a.out_lens = keep_lens;
   a.kept = kept;
-  const comem::ChooseForm form = comem::select_choose_kernel(false, max_ctx_len);
+  const comem::ChooseForm form = comem::select_choose_kernel(false, max_ctx_len, n, p->num_cus);
   void* argv[] = {&a};
   const hipError_t err =
-      hipLaunchKernel(reinterpret_cast<const void*>(form.fn), dim3(static_cast<unsigned>(n)),
+      hipLaunchKernel(reinterpret_cast<const void*>(form.fn), dim3(static_cast<unsigned>(n), static_cast<unsigned>(form.parts)),
                       dim3(static_cast<unsigned>(form.threads)), argv, 0, static_cast<hipStream_t>(hip_stream));
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }

@@ -75,8 +75,9 @@ using ChooseKernelFn = void (*)(ChooseParams);
 struct ChooseForm {
   ChooseKernelFn fn;
   int threads;
+  int parts;  // grid (items, parts)
 };
-// For rows of at most `most` entries; one workgroup per item.
-ChooseForm select_choose_kernel(bool blocks, int64_t most);
+// For `items` rows of at most `most` entries on `cus` compute units.
+ChooseForm select_choose_kernel(bool blocks, int64_t most, int64_t items, int cus);
 
 }  // namespace comem

@@ -11,14 +11,17 @@
 // The histogram is kept 32 times, one copy for each of 32 lanes: score digits
 // cluster (a sign and an exponent have few values), and counts that meet in one
 // word are added one after another.
+#include <algorithm>
+
 #include "attn_common.h"
 #include "evict.h"
 
 namespace comem {
 namespace {
 
+typedef int s32x4 __attribute__((ext_vector_type(4)));
+
 constexpr uint32_t kForced = 0xffffffffu, kNaN = 0xfffffffeu;
-constexpr int kCopies = 32, kBins = 256;
 
 // Keys order as the scores do; 0 is below every score's.
 __device__ inline uint32_t key_of(float x) {
@@ -26,179 +29,382 @@ __device__ inline uint32_t key_of(float x) {
   return x == x ? (static_cast<int32_t>(u) < 0 ? ~u : u | 0x80000000u) : kNaN;
 }
 
-// The digit that holds the need-th entry from the top, the entries above it and
-// those of it; every wave looks for it by itself.
-struct Digit {
-  int digit, above, count;
-};
-__device__ inline Digit find_digit(const int* sums, int need, int lane) {
-  int v[4], total = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[e] = sums[kBins - 1 - 4 * lane - e];
-    total += v[e];
-  }
-  int upto = total;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(upto, o);
-    if (lane >= o) upto += x;
-  }
-  int above = upto - total, digit = -1, count = 0, at = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (above < need && need <= above + v[e]) {
-      digit = kBins - 1 - 4 * lane - e;
-      at = above;
-      count = v[e];
-    }
-    above += v[e];
-  }
-  const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
-  return {__builtin_amdgcn_readlane(digit, from), __builtin_amdgcn_readlane(at, from),
-          __builtin_amdgcn_readlane(count, from)};
-}
+// One item of a call: its row's entries, how many of them stay, where they go.
+template <bool BLOCKS>
+struct Item {
+  const float* scores;
+  const int32_t* table;
+  int32_t* out;
+  float* kept;
+  int n, count, first, last;
 
-// REGS: entries of a lane that are kept in registers; those past them are read again.
-template <bool BLOCKS, int THREADS, int REGS>
-__global__ __launch_bounds__(THREADS) void choose_kernel(const ChooseParams p) {
-  constexpr int kWavesHere = THREADS / 64;
-  __shared__ int hist[kBins * kCopies];
-  __shared__ int sums[kBins];
-  __shared__ int wave_above[kWavesHere], wave_equal[kWavesHere];
-  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6);
-  const int item = blockIdx.x;
-  int n, count, row;
-  if constexpr (BLOCKS) {
-    row = item / p.heads;
-    const int L = min(max(uniform_i32(p.lens[row]), 0), p.max_len);
-    const int page = 1 << p.page_shift;
-    n = static_cast<int>((static_cast<uint32_t>(L) + page - 1) >> p.page_shift);
-    count = min(n, p.budget);
-    if (item - row * p.heads == 0 && tid == 0)
-      p.out_lens[row] = n == 0 ? 0 : (count - 1) * page + L - (n - 1) * page;
-  } else {
-    row = p.rows == nullptr ? item : uniform_i32(p.rows[item]);
-    n = row < 0 || row >= p.num_rows ? -1 : uniform_i32(p.lens[row]);
-    if (n > p.max_len) n = -1;
-    int budget = p.budget;
-    if (p.budgets != nullptr) budget = min(max(uniform_i32(p.budgets[item]), p.first + p.last), p.budget);
-    count = n < 0 ? -1 : min(n, budget);
-    if (tid == 0) {
-      p.out_lens[item] = count;
-      if (p.out_start != nullptr) p.out_start[item] = item * p.out_stride;
+  // The first lane of the first workgroup of an item also writes its length.
+  __device__ Item(const ChooseParams& p, int item, bool writes) : first(p.first), last(p.last) {
+    int row;
+    if constexpr (BLOCKS) {
+      row = item / p.heads;
+      const int L = min(max(uniform_i32(p.lens[row]), 0), p.max_len);
+      const int page = 1 << p.page_shift;
+      n = static_cast<int>((static_cast<uint32_t>(L) + page - 1) >> p.page_shift);
+      count = min(n, p.budget);
+      if (writes && item == row * p.heads) p.out_lens[row] = n == 0 ? 0 : (count - 1) * page + L - (n - 1) * page;
+      table = p.block_table + static_cast<int64_t>(row) * p.max_pages;
+      kept = nullptr;
+    } else {
+      row = p.rows == nullptr ? item : uniform_i32(p.rows[item]);
+      n = row < 0 || row >= p.num_rows ? -1 : uniform_i32(p.lens[row]);
+      if (n > p.max_len) n = -1;
+      int budget = p.budget;
+      if (p.budgets != nullptr) budget = min(max(uniform_i32(p.budgets[item]), p.first + p.last), p.budget);
+      count = n < 0 ? -1 : min(n, budget);
+      if (writes) {
+        p.out_lens[item] = count;
+        if (p.out_start != nullptr) p.out_start[item] = item * p.out_stride;
+      }
+      table = nullptr;
+      kept = p.kept == nullptr ? nullptr : p.kept + item * p.out_stride;
     }
+    scores = p.scores + static_cast<int64_t>(BLOCKS ? item : row) * p.scores_stride;
+    out = p.out + item * p.out_stride;
   }
-  if (count <= 0) return;
-  const float* scores = p.scores + static_cast<int64_t>(BLOCKS ? item : row) * p.scores_stride;
-  int32_t* out = p.out + item * p.out_stride;
-  const int32_t* table = BLOCKS ? p.block_table + static_cast<int64_t>(row) * p.max_pages : nullptr;
-  auto put = [&](int at, int i) {
+  __device__ float score_at(int i) const { return scores[min(i, n - 1)]; }
+  // Of entry i, whose score is x.
+  __device__ uint32_t key(int i, float x) const {
+    const uint32_t k = i < first || i >= n - last ? kForced : key_of(x);
+    return i < n ? k : 0;
+  }
+  __device__ void put(int at, int i) const {
     if constexpr (BLOCKS) {
       out[at] = table[i];
     } else {
       out[at] = i;
-      if (p.kept != nullptr) p.kept[item * p.out_stride + at] = scores[i];
+      if (kept != nullptr) kept[at] = scores[i];
     }
-  };
-  if (count == n) {
-    for (int i = tid; i < n; i += THREADS) put(i, i);
+  }
+};
+
+// What stays: keys from `least` on, and the first `ties` keys that are `tie`.
+struct Limit {
+  uint32_t least, tie;
+  int ties;
+};
+
+// The keys from `found` on stay, where the digits below it were not needed to
+// part them; else those above it and `need` of the equal ones.
+__device__ inline Limit limit_of(uint32_t found, int need, bool all) {
+  return all ? Limit{found, 0, 0} : Limit{found + 1, found, need};
+}
+
+// Entries of one step (64 side by side) before and among those that stay.
+struct Places {
+  int above = 0, equal = 0;
+  // Where the lane's entry goes, -1: it does not stay.
+  __device__ int next(uint32_t k, const Limit& l) {
+    const uint64_t over = __builtin_amdgcn_ballot_w64(k >= l.least);
+    int at = above + lanes_before(over);
+    bool stays = k >= l.least;
+    if (l.ties > 0) {
+      const uint64_t same = __builtin_amdgcn_ballot_w64(k == l.tie);
+      const int e = equal + lanes_before(same);
+      at += min(e, l.ties);
+      stays = stays || (k == l.tie && e < l.ties);
+      equal += __builtin_popcountll(same);
+    }
+    above += __builtin_popcountll(over);
+    return stays ? at : -1;
+  }
+  static __device__ int lanes_before(uint64_t mask) {
+    return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0)));
+  }
+};
+
+// Sum of x over the lanes up to this one.
+template <int CTRL, int ROWS>
+__device__ inline int moved(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ inline int upto_lane(int x) {
+  x += moved<0x111, 0xf>(x);  // 1, 2, 4, 8 lanes before, within a row of 16
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);  // the last of the row before; of the half before
+  x += moved<0x143, 0xc>(x);
+  return x;
+}
+
+// 4 bytes from each lane's address to consecutive places in LDS. (The caller
+// waits for vector memory before it reads them.)
+__device__ inline void load_to_lds(const void* from, uint32_t* to) {
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t*>(
+                                       reinterpret_cast<uintptr_t>(from)),
+                                   (__attribute__((address_space(3))) uint32_t*)to, 4, 0, 0);
+}
+
+// Rows of at most kWaveEntries: one wave each, which needs no barrier. 8 bits
+// at a time, 4 copies of the histogram, 4 bins a lane.
+constexpr int kWaveEntries = 2048, kWaveCopies = 4;
+
+__device__ inline void wave_lds_done() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
+
+template <bool BLOCKS>
+__global__ __launch_bounds__(64) void choose_wave_kernel(const ChooseParams p) {
+  __shared__ s32x4 hist[256];  // the copies of a bin side by side
+  __shared__ uint32_t keys[kWaveEntries];
+  __shared__ uint32_t pages[BLOCKS ? kWaveEntries : 1];
+  const int lane = threadIdx.x;
+  const Item<BLOCKS> item(p, blockIdx.x, lane == 0);
+  if (item.count <= 0) return;
+  if (item.count == item.n) {
+    for (int i = lane; i < item.n; i += 64) item.put(i, i);
     return;
   }
-
-  // The wave's run of the row, 64 entries a step.
-  const int steps = (n + THREADS - 1) / THREADS;
-  const int run = w * steps * 64 + lane;
-  auto key_at = [&](int j) -> uint32_t {
-    const int i = run + 64 * j;
-    if (i >= n) return 0;
-    return i < p.first || i >= n - p.last ? kForced : key_of(scores[i]);
-  };
-  uint32_t key[REGS];
-#pragma unroll
-  for (int j = 0; j < REGS; ++j) key[j] = j < steps ? key_at(j) : 0;
-  auto for_all = [&](auto&& f) {
-#pragma unroll
-    for (int j = 0; j < REGS; ++j)
-      if (j < steps) f(j, key[j]);
-    for (int j = REGS; j < steps; ++j) f(j, key_at(j));
-  };
-
-  for (int i = tid; i < kBins * kCopies; i += THREADS) hist[i] = 0;
-  __syncthreads();
-  uint32_t least = 0;       // the digits found so far
-  int need = count;         // entries still missing among the keys that begin with them
-  bool all = false;         // all of those stay
+  // From memory straight into LDS, all of them in flight together; the first
+  // pass makes keys of the scores.
+#pragma unroll 1
+  for (int g = 0; g < item.n; g += 64) {
+    const int i = min(g + lane, item.n - 1);
+    load_to_lds(item.scores + i, &keys[g]);
+    if constexpr (BLOCKS) load_to_lds(item.table + i, &pages[g]);
+  }
+  wait_stores_done();
+  uint32_t found = 0;
+  int need = item.count;
+  bool all = false;
 #pragma unroll 1
   for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-    const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for_all([&](int, uint32_t k) {
-      if (k != 0 && (k & mask) == least) atomicAdd(&hist[((k >> shift) & 255u) * kCopies + (lane & 31)], 1);
-    });
-    __syncthreads();
-    if (tid < kBins) {
-      int s = 0;
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        int* at = &hist[tid * kCopies + ((i + tid) & 31)];
-        s += *at;
-        *at = 0;
+    for (int i = 0; i < 4; ++i) hist[64 * i + lane] = s32x4{0, 0, 0, 0};
+    wave_lds_done();
+    const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
+#pragma unroll 1
+    for (int g = 0; g < item.n; g += 256) {  // keys past the row are 0, which is in no score's bin
+      uint32_t k[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = keys[g + 64 * e + lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (shift == 24) {
+          k[e] = item.key(g + 64 * e + lane, __uint_as_float(k[e]));
+          keys[g + 64 * e + lane] = k[e];
+        }
+        if ((k[e] & mask) == found)
+          atomicAdd(reinterpret_cast<int*>(&hist[(k[e] >> shift) & 255u]) + (lane & (kWaveCopies - 1)), 1);
       }
-      sums[tid] = s;
+    }
+    wave_lds_done();
+    // The lane's bins from the top down, and the entries of the lanes before it.
+    int v[4], total = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const s32x4 x = hist[255 - 4 * lane - e];
+      v[e] = x[0] + x[1] + x[2] + x[3];
+      total += v[e];
+    }
+    int above = upto_lane(total) - total, digit = -1, at = 0, size = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (above < need && need <= above + v[e]) {
+        digit = 255 - 4 * lane - e;
+        at = above;
+        size = v[e];
+      }
+      above += v[e];
+    }
+    const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
+    found |= static_cast<uint32_t>(__builtin_amdgcn_readlane(digit, from)) << shift;
+    need -= __builtin_amdgcn_readlane(at, from);
+    all = need == __builtin_amdgcn_readlane(size, from);
+  }
+  const Limit limit = limit_of(found, need, all);
+  Places places;
+#pragma unroll 1
+  for (int g = 0; g < item.n; g += 256) {  // keys past the row are 0, which stays nowhere
+    const int i0 = g + lane;
+    uint32_t k[4];
+    int32_t page[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      k[e] = keys[i0 + 64 * e];
+      if constexpr (BLOCKS) page[e] = static_cast<int32_t>(pages[i0 + 64 * e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = places.next(k[e], limit);
+      if constexpr (BLOCKS) {
+        if (at >= 0) item.out[at] = page[e];
+      } else {
+        if (at >= 0) item.put(at, i0 + 64 * e);
+      }
+    }
+  }
+}
+
+// Sum of x[0 .. w - 1], for w < 16.
+__device__ inline int waves_before(const int* x, int w, int lane) {
+  const int upto = upto_lane(x[lane & 15]);
+  return w > 0 ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
+}
+
+// Longer rows: a workgroup of 16 waves, each with a run of the row. 11, 11 and
+// 10 bits at a time, kCopies copies of the histogram. `gridDim.y` workgroups find
+// a row's limit, all the same one, and each puts its part of every run.
+constexpr int kThreadsWide = 1024, kWavesWide = kThreadsWide / 64;
+constexpr int kBins = 2048, kCopies = 4;  // of the histogram
+constexpr int kStep = 8;        // groups of 64 entries that a wave takes at a time
+constexpr int kHeldSteps = 24;  // groups of a run whose keys are kept
+
+template <bool BLOCKS>
+__global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams p) {
+  __shared__ s32x4 hist[kBins];  // the copies of a bin side by side
+  __shared__ uint32_t held[kWavesWide][kHeldSteps * 64];
+  __shared__ int wave_total[kWavesWide], wave_equal[kWavesWide];
+  __shared__ int result[3];
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6);
+  const int part = blockIdx.y, parts = gridDim.y;
+  const Item<BLOCKS> item(p, blockIdx.x, tid == 0 && part == 0);
+  if (item.count <= 0) return;
+  if (item.count == item.n) {
+    for (int i = part * kThreadsWide + tid; i < item.n; i += parts * kThreadsWide) item.put(i, i);
+    return;
+  }
+  // The wave's run, kStep groups at a time.
+  const int steps = (item.n + kStep * kThreadsWide - 1) / (kStep * kThreadsWide) * kStep;
+  const int run = w * steps * 64 + lane;
+  auto scores_at = [&](int j, float (&x)[kStep]) {
+#pragma unroll
+    for (int e = 0; e < kStep; ++e) x[e] = item.score_at(run + 64 * (j + e));
+  };
+  auto keys_of = [&](int j, const float (&x)[kStep], uint32_t (&k)[kStep]) {
+#pragma unroll
+    for (int e = 0; e < kStep; ++e) k[e] = item.key(run + 64 * (j + e), x[e]);
+  };
+  // f(j, keys) for the groups from `from` up to `to`: those that are kept, then
+  // the others, whose scores are asked for one turn ahead.
+  bool raw = true;  // what is kept are scores, not keys yet
+  auto for_groups = [&](int from, int to, auto&& f) {
+    float next[kStep];
+    if (max(from, kHeldSteps) < to) scores_at(max(from, kHeldSteps), next);
+#pragma unroll 1
+    for (int j = from; j < to; j += kStep) {
+      uint32_t k[kStep];
+      if (j < kHeldSteps) {
+#pragma unroll
+        for (int e = 0; e < kStep; ++e) k[e] = held[w][64 * (j + e) + lane];
+        if (raw) {
+#pragma unroll
+          for (int e = 0; e < kStep; ++e) {
+            k[e] = item.key(run + 64 * (j + e), __uint_as_float(k[e]));
+            held[w][64 * (j + e) + lane] = k[e];
+          }
+        }
+      } else {
+        float x[kStep];
+#pragma unroll
+        for (int e = 0; e < kStep; ++e) x[e] = next[e];
+        if (j + kStep < to) scores_at(j + kStep, next);
+        keys_of(j, x, k);
+      }
+      f(j, k);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kBins; i += kThreadsWide) hist[i + tid] = s32x4{0, 0, 0, 0};
+  // The kept groups go from memory straight into LDS, all of them in flight
+  // together; the first pass makes keys of them.
+  const int kept = min(steps, kHeldSteps);
+#pragma unroll 1
+  for (int j = 0; j < kept; ++j) load_to_lds(item.scores + min(run + 64 * j, item.n - 1), &held[w][64 * j]);
+  wait_stores_done();
+  __syncthreads();
+  uint32_t found = 0;       // the digits found so far
+  int need = item.count;    // entries still missing among the keys that begin with them
+  bool all = false;         // all of those stay
+#pragma unroll 1
+  for (int shift = 21; !all;) {
+    const int bits = shift == 0 ? 10 : 11;
+    const uint32_t mask = shift == 21 ? 0u : ~0u << (shift + bits);
+    const uint32_t low = (1u << bits) - 1;
+    for_groups(0, steps, [&](int, const uint32_t (&k)[kStep]) {
+#pragma unroll
+      for (int e = 0; e < kStep; ++e)
+        if ((k[e] & mask) == found) atomicAdd(reinterpret_cast<int*>(&hist[(k[e] >> shift) & low]) + (lane & (kCopies - 1)), 1);
+    });
+    raw = false;
+    __syncthreads();
+    // A thread's two bins from the top down, and the entries of those before.
+    int v[2], total = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      s32x4* bin = &hist[kBins - 1 - 2 * tid - e];
+      const s32x4 x = *bin;
+      *bin = s32x4{0, 0, 0, 0};
+      v[e] = x[0] + x[1] + x[2] + x[3];
+      total += v[e];
+    }
+    const int upto = upto_lane(total);
+    if (lane == 63) wave_total[w] = upto;
+    __syncthreads();
+    int above = upto - total + waves_before(wave_total, w, lane);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (above < need && need <= above + v[e]) {
+        result[0] = kBins - 1 - 2 * tid - e;
+        result[1] = above;
+        result[2] = v[e];
+      }
+      above += v[e];
     }
     __syncthreads();
-    const Digit d = find_digit(sums, need, lane);
-    least |= static_cast<uint32_t>(d.digit) << shift;
-    need -= d.above;
-    all = need == d.count;
+    found |= static_cast<uint32_t>(uniform_i32(result[0])) << shift;
+    need -= uniform_i32(result[1]);
+    all = need == uniform_i32(result[2]);
+    if (shift == 0) break;
+    shift = shift == 21 ? 10 : 0;
   }
-  if (all) need = INT32_MAX;
+  const Limit limit = limit_of(found, need, all);
 
-  int above = 0, equal = 0;
-  const uint32_t top = least;
-  // Keys that begin with the digits found: equal to `top` where all digits were
-  // needed, else all of them stay, as those above do.
-  auto masks = [&](uint32_t k, uint64_t& over, uint64_t& same) {
-    over = __builtin_amdgcn_ballot_w64(all ? k >= top && k != 0 : k > top);
-    same = all ? 0 : __builtin_amdgcn_ballot_w64(k == top);
-  };
-  for_all([&](int, uint32_t k) {
-    uint64_t over, same;
-    masks(k, over, same);
-    above += __builtin_popcountll(over);
-    equal += __builtin_popcountll(same);
+  // This workgroup's part of the run: groups begin .. end - 1.
+  const int begin = static_cast<int>(static_cast<int64_t>(steps / kStep) * part / parts) * kStep;
+  const int end = static_cast<int>(static_cast<int64_t>(steps / kStep) * (part + 1) / parts) * kStep;
+  Places own;
+  int all_above = 0, all_equal = 0;
+  for_groups(0, steps, [&](int j, const uint32_t (&k)[kStep]) {
+    if (j == begin) own = {all_above, all_equal};
+#pragma unroll
+    for (int e = 0; e < kStep; ++e) {
+      all_above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[e] >= limit.least));
+      if (limit.ties > 0) all_equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[e] == limit.tie));
+    }
   });
   if (lane == 0) {
-    wave_above[w] = above;
-    wave_equal[w] = equal;
+    wave_total[w] = all_above;
+    wave_equal[w] = all_equal;
   }
   __syncthreads();
-  above = 0;
-  equal = 0;
-  for (int i = 0; i < w; ++i) {
-    above += wave_above[i];
-    equal += wave_equal[i];
-  }
-  const uint64_t before = (uint64_t{1} << lane) - 1;
-  for_all([&](int j, uint32_t k) {
-    uint64_t over, same;
-    masks(k, over, same);
-    const int a = above + __builtin_popcountll(over & before), e = equal + __builtin_popcountll(same & before);
-    const bool stays = ((over >> lane) & 1) != 0 || (((same >> lane) & 1) != 0 && e < need);
-    if (stays) put(a + min(e, need), run + 64 * j);
-    above += __builtin_popcountll(over);
-    equal += __builtin_popcountll(same);
+  own.above += waves_before(wave_total, w, lane);
+  if (limit.ties > 0) own.equal += waves_before(wave_equal, w, lane);
+  for_groups(begin, end, [&](int j, const uint32_t (&k)[kStep]) {
+#pragma unroll
+    for (int e = 0; e < kStep; ++e) {
+      const int at = own.next(k[e], limit);
+      if (at >= 0) item.put(at, run + 64 * (j + e));
+    }
   });
 }
 
 template <bool BLOCKS>
-ChooseForm form(int64_t most) {
-  if (most <= 2048) return {choose_kernel<BLOCKS, 256, 8>, 256};
-  return {choose_kernel<BLOCKS, 1024, 32>, 1024};
+ChooseForm form(int64_t most, int64_t items, int cus) {
+  if (most <= kWaveEntries) return {choose_wave_kernel<BLOCKS>, 64, 1};
+  const int64_t parts = most <= 8192 ? 1 : std::min<int64_t>(8, std::max<int64_t>(1, cus / items));
+  return {choose_kernel<BLOCKS>, kThreadsWide, static_cast<int>(parts)};
 }
 
 }  // namespace
 
-ChooseForm select_choose_kernel(bool blocks, int64_t most) { return blocks ? form<true>(most) : form<false>(most); }
+ChooseForm select_choose_kernel(bool blocks, int64_t most, int64_t items, int cus) {
+  return blocks ? form<true>(most, items, cus) : form<false>(most, items, cus);
+}
 
 }  // namespace comem
