@@ -73,12 +73,14 @@ struct Item {
     const uint32_t k = i < first || i >= n - last ? kForced : key_of(x);
     return i < n ? k : 0;
   }
-  __device__ void put(int at, int i) const {
+  __device__ void put(int at, int i) const { put(at, i, kept != nullptr ? scores[i] : 0.f); }
+  // x: its score.
+  __device__ void put(int at, int i, float x) const {
     if constexpr (BLOCKS) {
       out[at] = table[i];
     } else {
       out[at] = i;
-      if (kept != nullptr) kept[at] = scores[i];
+      if (kept != nullptr) kept[at] = x;
     }
   }
 };
@@ -95,27 +97,28 @@ __device__ inline Limit limit_of(uint32_t found, int need, bool all) {
   return all ? Limit{found, 0, 0} : Limit{found + 1, found, need};
 }
 
+__device__ inline int lanes_before(uint64_t mask) {
+  return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0)));
+}
+
 // Entries of one step (64 side by side) before and among those that stay.
 struct Places {
   int above = 0, equal = 0;
-  // Where the lane's entry goes, -1: it does not stay.
-  __device__ int next(uint32_t k, const Limit& l) {
-    const uint64_t over = __builtin_amdgcn_ballot_w64(k >= l.least);
+  // Where the lane's entry goes, -1: it does not stay. equals: it is one of
+  // those of which the first `ties` stay.
+  __device__ int next(bool stays, bool equals, int ties) {
+    const uint64_t over = __builtin_amdgcn_ballot_w64(stays);
     int at = above + lanes_before(over);
-    bool stays = k >= l.least;
-    if (l.ties > 0) {
-      const uint64_t same = __builtin_amdgcn_ballot_w64(k == l.tie);
+    if (ties > 0) {
+      const uint64_t same = __builtin_amdgcn_ballot_w64(equals);
       const int e = equal + lanes_before(same);
-      at += min(e, l.ties);
-      stays = stays || (k == l.tie && e < l.ties);
+      at += min(e, ties);
+      stays = stays || (equals && e < ties);
       equal += __builtin_popcountll(same);
     }
     above += __builtin_popcountll(over);
     return stays ? at : -1;
-  }
-  static __device__ int lanes_before(uint64_t mask) {
-    return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
-                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0)));
   }
 };
 
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(64) void choose_wave_kernel(const ChooseParams p) {
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int at = places.next(k[e], limit);
+      const int at = places.next(k[e] >= limit.least, k[e] == limit.tie, limit.ties);
       if constexpr (BLOCKS) {
         if (at >= 0) item.out[at] = page[e];
       } else {
@@ -247,20 +250,49 @@ __device__ inline int waves_before(const int* x, int w, int lane) {
   return w > 0 ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
 }
 
-// Longer rows: a workgroup of 16 waves, each with a run of the row. 11, 11 and
-// 10 bits at a time, kCopies copies of the histogram. `gridDim.y` workgroups find
-// a row's limit, all the same one, and each puts its part of every run.
+// Longer rows: a workgroup of 16 waves, each with a run of the row, which it
+// reads three times, 8 groups of 64 entries a turn and the next turn's scores
+// asked for ahead. The first time it counts the top 11 bits of the scores
+// (4 copies of the histogram, so that lanes with one digit do not all wait for
+// one word), which gives the digit that holds the limit. The second time it
+// counts what lies above that digit and lists the scores that have it, a few
+// percent of the row; the other digits, 11 and 10 bits, follow from the lists
+// (where one overflows, from the row again). The third time it puts what stays.
+// `gridDim.y` workgroups do the first two for a row, with the same results,
+// and share the third.
+//
+// One compute unit's instructions bound it, so turns without NaN between the
+// entries that always stay compare scores as floats, and only the others, and
+// the lists, make keys.
 constexpr int kThreadsWide = 1024, kWavesWide = kThreadsWide / 64;
 constexpr int kBins = 2048, kCopies = 4;  // of the histogram
-constexpr int kStep = 8;        // groups of 64 entries that a wave takes at a time
-constexpr int kHeldSteps = 24;  // groups of a run whose keys are kept
+constexpr int kTurn = 8;                  // groups of a turn
+constexpr int kListed = 1920;             // scores of a wave's list
+
+// The least score whose key is k or more (a NaN, which no comparison holds for,
+// where there is no such number).
+__device__ inline float score_of(uint32_t k) {
+  const uint32_t lowest = 0x007fffffu;  // the key of -inf
+  k = max(k, lowest);
+  return __uint_as_float(static_cast<int32_t>(k) < 0 ? k & 0x7fffffffu : ~k);
+}
+
+// Of a turn: numbers to choose among; entries that all stay; none; anything else.
+enum class Turn { kPlain, kForced, kEmpty, kMixed };
+
+// Orders LDS accesses alone: scores asked for ahead stay in flight.
+__device__ inline void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 
 template <bool BLOCKS>
 __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams p) {
   __shared__ s32x4 hist[kBins];  // the copies of a bin side by side
-  __shared__ uint32_t held[kWavesWide][kHeldSteps * 64];
+  __shared__ float list[kWavesWide][kListed];
   __shared__ int wave_total[kWavesWide], wave_equal[kWavesWide];
-  __shared__ int result[3];
+  __shared__ int result[3], too_long;
   const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6);
   const int part = blockIdx.y, parts = gridDim.y;
   const Item<BLOCKS> item(p, blockIdx.x, tid == 0 && part == 0);
@@ -269,75 +301,92 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
     for (int i = part * kThreadsWide + tid; i < item.n; i += parts * kThreadsWide) item.put(i, i);
     return;
   }
-  // The wave's run, kStep groups at a time.
-  const int steps = (item.n + kStep * kThreadsWide - 1) / (kStep * kThreadsWide) * kStep;
-  const int run = w * steps * 64 + lane;
-  auto scores_at = [&](int j, float (&x)[kStep]) {
+  const int begin = min(item.first, item.n), end = max(item.n - item.last, begin);  // between them it is chosen
+  const int turns = (item.n + kTurn * kThreadsWide - 1) / (kTurn * kThreadsWide);
+  const int run = w * turns * kTurn * 64;  // the wave's first entry
+  auto ask = [&](int at, float (&x)[kTurn]) {
+    if (at + 64 * kTurn <= item.n) {
+      const float* from = item.scores + at + lane;
 #pragma unroll
-    for (int e = 0; e < kStep; ++e) x[e] = item.score_at(run + 64 * (j + e));
-  };
-  auto keys_of = [&](int j, const float (&x)[kStep], uint32_t (&k)[kStep]) {
+      for (int e = 0; e < kTurn; ++e) x[e] = from[64 * e];
+    } else {
 #pragma unroll
-    for (int e = 0; e < kStep; ++e) k[e] = item.key(run + 64 * (j + e), x[e]);
-  };
-  // f(j, keys) for the groups from `from` up to `to`: those that are kept, then
-  // the others, whose scores are asked for one turn ahead.
-  bool raw = true;  // what is kept are scores, not keys yet
-  auto for_groups = [&](int from, int to, auto&& f) {
-    float next[kStep];
-    if (max(from, kHeldSteps) < to) scores_at(max(from, kHeldSteps), next);
-#pragma unroll 1
-    for (int j = from; j < to; j += kStep) {
-      uint32_t k[kStep];
-      if (j < kHeldSteps) {
-#pragma unroll
-        for (int e = 0; e < kStep; ++e) k[e] = held[w][64 * (j + e) + lane];
-        if (raw) {
-#pragma unroll
-          for (int e = 0; e < kStep; ++e) {
-            k[e] = item.key(run + 64 * (j + e), __uint_as_float(k[e]));
-            held[w][64 * (j + e) + lane] = k[e];
-          }
-        }
-      } else {
-        float x[kStep];
-#pragma unroll
-        for (int e = 0; e < kStep; ++e) x[e] = next[e];
-        if (j + kStep < to) scores_at(j + kStep, next);
-        keys_of(j, x, k);
-      }
-      f(j, k);
+      for (int e = 0; e < kTurn; ++e) x[e] = item.score_at(at + 64 * e + lane);
     }
   };
+  // f(first entry of the turn, its scores, what kind it is); `next` holds turn
+  // `from`'s scores, and at the end those of turn `after`.
+  float next[kTurn];
+  auto for_turns = [&](int from, int to, int after, auto&& f) {
+    float x[kTurn];
+#pragma unroll 1
+    for (int j = from; j < to; ++j) {
+      const int at = run + 64 * kTurn * j;
+#pragma unroll
+      for (int e = 0; e < kTurn; ++e) x[e] = next[e];
+      ask(run + 64 * kTurn * (j + 1 < to ? j + 1 : after), next);
+      Turn kind = at >= end || at + 64 * kTurn <= begin ? Turn::kForced : at >= begin && at + 64 * kTurn <= end ? Turn::kPlain : Turn::kMixed;
+      if (at + 64 * kTurn > item.n) kind = at >= item.n ? Turn::kEmpty : Turn::kMixed;
+      if (kind == Turn::kPlain) {
+#pragma unroll
+        for (int e = 0; e < kTurn; e += 2)
+          if (__builtin_amdgcn_ballot_w64(__builtin_isunordered(x[e], x[e + 1])) != 0) kind = Turn::kMixed;
+      }
+      f(at, x, kind);
+    }
+  };
+  auto chosen = [&](int i) { return i >= begin && i < end; };      // not: it stays, or is past the row
+  auto forced = [&](int i) { return i < begin || (i >= end && i < item.n); };
+  auto add = [&](int bin) { atomicAdd(reinterpret_cast<int*>(&hist[bin]) + (lane & (kCopies - 1)), 1); };
+
 #pragma unroll
   for (int i = 0; i < kBins; i += kThreadsWide) hist[i + tid] = s32x4{0, 0, 0, 0};
-  // The kept groups go from memory straight into LDS, all of them in flight
-  // together; the first pass makes keys of them.
-  const int kept = min(steps, kHeldSteps);
+  if (tid == 0) too_long = 0;
+  ask(run, next);
+  lds_barrier();
+  uint32_t found = 0;                                              // the key's digits found so far
+  int need = item.count - begin - (item.n - end);                  // entries still missing among those that have them
+  bool all = need <= 0, overflow = false;                          // all of those stay
+  int above = 0, listed = 0, own_above = 0, own_listed = 0;
+  const int part_begin = turns * part / parts, part_end = turns * (part + 1) / parts;
 #pragma unroll 1
-  for (int j = 0; j < kept; ++j) load_to_lds(item.scores + min(run + 64 * j, item.n - 1), &held[w][64 * j]);
-  wait_stores_done();
-  __syncthreads();
-  uint32_t found = 0;       // the digits found so far
-  int need = item.count;    // entries still missing among the keys that begin with them
-  bool all = false;         // all of those stay
-#pragma unroll 1
-  for (int shift = 21; !all;) {
+  for (int shift = 21;;) {
     const int bits = shift == 0 ? 10 : 11;
-    const uint32_t mask = shift == 21 ? 0u : ~0u << (shift + bits);
     const uint32_t low = (1u << bits) - 1;
-    for_groups(0, steps, [&](int, const uint32_t (&k)[kStep]) {
+    if (shift == 21) {
+      // By the bits as they are; -0 as 0, NaN as one of them.
+      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn kind) {
+        if (kind == Turn::kForced || kind == Turn::kEmpty) return;
+        const bool plain = kind == Turn::kPlain;
 #pragma unroll
-      for (int e = 0; e < kStep; ++e)
-        if ((k[e] & mask) == found) atomicAdd(reinterpret_cast<int*>(&hist[(k[e] >> shift) & low]) + (lane & (kCopies - 1)), 1);
-    });
-    raw = false;
-    __syncthreads();
-    // A thread's two bins from the top down, and the entries of those before.
+        for (int e = 0; e < kTurn; ++e) {
+          uint32_t u = __float_as_uint(x[e] + 0.f);
+          if (!plain) u = x[e] == x[e] ? u : 0x7fffffffu;
+          if (plain || chosen(at + 64 * e + lane)) add(static_cast<int>(u >> 21));
+        }
+      });
+    } else if (overflow) {
+      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn) {
+#pragma unroll
+        for (int e = 0; e < kTurn; ++e) {
+          const uint32_t k = key_of(x[e]);
+          if (chosen(at + 64 * e + lane) && (k ^ found) >> (shift + bits) == 0) add(static_cast<int>((k >> shift) & low));
+        }
+      });
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < listed; i += 64) {
+        const uint32_t k = key_of(list[w][i]);
+        if ((k ^ found) >> (shift + bits) == 0) add(static_cast<int>((k >> shift) & low));
+      }
+    }
+    lds_barrier();
+    // A thread's two digits from the top down, and the entries of those before.
     int v[2], total = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      s32x4* bin = &hist[kBins - 1 - 2 * tid - e];
+      const int digit = kBins - 1 - 2 * tid - e;
+      s32x4* bin = &hist[shift != 21 ? digit : digit >= kBins / 2 ? digit - kBins / 2 : kBins - 1 - digit];
       const s32x4 x = *bin;
       *bin = s32x4{0, 0, 0, 0};
       v[e] = x[0] + x[1] + x[2] + x[3];
@@ -345,51 +394,120 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
     }
     const int upto = upto_lane(total);
     if (lane == 63) wave_total[w] = upto;
-    __syncthreads();
-    int above = upto - total + waves_before(wave_total, w, lane);
+    if (tid == 0) result[0] = result[1] = result[2] = 0;
+    lds_barrier();
+    int before = upto - total + waves_before(wave_total, w, lane);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      if (above < need && need <= above + v[e]) {
+      if (before < need && need <= before + v[e]) {
         result[0] = kBins - 1 - 2 * tid - e;
-        result[1] = above;
+        result[1] = before;
         result[2] = v[e];
       }
-      above += v[e];
+      before += v[e];
     }
-    __syncthreads();
-    found |= static_cast<uint32_t>(uniform_i32(result[0])) << shift;
-    need -= uniform_i32(result[1]);
-    all = need == uniform_i32(result[2]);
-    if (shift == 0) break;
+    lds_barrier();
+    if (!all) {
+      found |= static_cast<uint32_t>(uniform_i32(result[0])) << shift;
+      need -= uniform_i32(result[1]);
+      all = need == uniform_i32(result[2]);
+    } else {
+      found = ~0u;  // only what always stays
+    }
+    if (shift == 21) {
+      const uint32_t top = found >> 21;
+      const float least = score_of(top << 21), over = top == kBins - 1 ? __builtin_nanf("") : score_of((top + 1) << 21);
+      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn kind) {
+        if (at == run + 64 * kTurn * part_begin) {
+          own_above = above;
+          own_listed = listed;
+        }
+        if (kind == Turn::kForced) above += 64 * kTurn;
+        if (kind == Turn::kForced || kind == Turn::kEmpty) return;
+        const bool plain = kind == Turn::kPlain;
+#pragma unroll
+        for (int e = 0; e < kTurn; ++e) {
+          uint64_t more, same;
+          if (plain) {
+            more = __builtin_amdgcn_ballot_w64(x[e] >= over);
+            same = __builtin_amdgcn_ballot_w64(x[e] >= least) & ~more;
+          } else {
+            const int i = at + 64 * e + lane;
+            const uint32_t k = key_of(x[e]) >> 21;
+            more = __builtin_amdgcn_ballot_w64(forced(i) || (chosen(i) && k > top));
+            same = __builtin_amdgcn_ballot_w64(chosen(i) && k == top);
+          }
+          above += __builtin_popcountll(more);
+          if (same != 0) {
+            const int place = listed + lanes_before(same);
+            if (((same >> lane) & 1) != 0 && place < kListed) list[w][place] = x[e];
+            listed += __builtin_popcountll(same);
+          }
+        }
+      });
+      if (listed > kListed) too_long = 1;
+      lds_barrier();
+      overflow = uniform_i32(too_long) != 0;
+    }
+    if (all || shift == 0) break;
     shift = shift == 21 ? 10 : 0;
   }
   const Limit limit = limit_of(found, need, all);
+  const float least = score_of(limit.least), tie = all ? __builtin_nanf("") : score_of(limit.tie);
 
-  // This workgroup's part of the run: groups begin .. end - 1.
-  const int begin = static_cast<int>(static_cast<int64_t>(steps / kStep) * part / parts) * kStep;
-  const int end = static_cast<int>(static_cast<int64_t>(steps / kStep) * (part + 1) / parts) * kStep;
+  // What each run, and this workgroup's part of it, holds of the entries that stay.
   Places own;
-  int all_above = 0, all_equal = 0;
-  for_groups(0, steps, [&](int j, const uint32_t (&k)[kStep]) {
-    if (j == begin) own = {all_above, all_equal};
+  int equal = 0;
+  if (overflow) {
+    above = 0;
+    for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn) {
+      if (at == run + 64 * kTurn * part_begin) own = {above, equal};
 #pragma unroll
-    for (int e = 0; e < kStep; ++e) {
-      all_above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[e] >= limit.least));
-      if (limit.ties > 0) all_equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[e] == limit.tie));
+      for (int e = 0; e < kTurn; ++e) {
+        const int i = at + 64 * e + lane;
+        const uint32_t k = forced(i) ? kForced : chosen(i) ? key_of(x[e]) : 0;
+        above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= limit.least));
+        if (limit.ties > 0) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == limit.tie));
+      }
+    });
+  } else {
+    own.above = own_above;
+#pragma unroll 1
+    for (int i = 0; i < listed; i += 64) {
+      const uint32_t k = i + lane < listed ? key_of(list[w][i + lane]) : 0;
+      const uint64_t mine = own_listed - i >= 64 ? ~uint64_t{0} : own_listed > i ? (uint64_t{1} << (own_listed - i)) - 1 : 0;
+      const uint64_t more = __builtin_amdgcn_ballot_w64(k >= limit.least);
+      above += __builtin_popcountll(more);
+      own.above += __builtin_popcountll(more & mine);
+      if (limit.ties > 0) {
+        const uint64_t same = __builtin_amdgcn_ballot_w64(k == limit.tie);
+        equal += __builtin_popcountll(same);
+        own.equal += __builtin_popcountll(same & mine);
+      }
     }
-  });
-  if (lane == 0) {
-    wave_total[w] = all_above;
-    wave_equal[w] = all_equal;
   }
-  __syncthreads();
+  if (lane == 0) {
+    wave_total[w] = above;
+    wave_equal[w] = equal;
+  }
+  lds_barrier();
   own.above += waves_before(wave_total, w, lane);
   if (limit.ties > 0) own.equal += waves_before(wave_equal, w, lane);
-  for_groups(begin, end, [&](int j, const uint32_t (&k)[kStep]) {
+  if (part_begin != 0) ask(run + 64 * kTurn * part_begin, next);
+  for_turns(part_begin, part_end, part_begin, [&](int at, const float (&x)[kTurn], Turn kind) {
+    if (kind == Turn::kEmpty) return;
+    const bool plain = kind == Turn::kPlain;
 #pragma unroll
-    for (int e = 0; e < kStep; ++e) {
-      const int at = own.next(k[e], limit);
-      if (at >= 0) item.put(at, run + 64 * (j + e));
+    for (int e = 0; e < kTurn; ++e) {
+      const int i = at + 64 * e + lane;
+      bool stays = x[e] >= least, equals = x[e] == tie;
+      if (!plain) {
+        const uint32_t k = forced(i) ? kForced : chosen(i) ? key_of(x[e]) : 0;
+        stays = k >= limit.least;
+        equals = limit.ties > 0 && k == limit.tie;
+      }
+      const int to = own.next(stays, equals, limit.ties);
+      if (to >= 0) item.put(to, i, x[e]);
     }
   });
 }
@@ -397,7 +515,7 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
 template <bool BLOCKS>
 ChooseForm form(int64_t most, int64_t items, int cus) {
   if (most <= kWaveEntries) return {choose_wave_kernel<BLOCKS>, 64, 1};
-  const int64_t parts = most <= 8192 ? 1 : std::min<int64_t>(8, std::max<int64_t>(1, cus / items));
+  const int64_t parts = std::min<int64_t>(8, std::max<int64_t>(1, cus / items));
   return {choose_kernel<BLOCKS>, kThreadsWide, static_cast<int>(parts)};
 }
 
