@@ -20,8 +20,8 @@
  * buffer says, so that it needs no initialisation.
  *
  * Ownership, errors, streams and the device-side contract (lengths, block
- * tables) are those of the decode calls (comem_decode_attn.h). Each call
- * enqueues one kernel and needs no workspace. Same arguments, same bits.
+ * tables) are those of the decode calls (comem_decode_attn.h). Same arguments
+ * (workspaces of the same use among them), same bits.
  */
 #ifndef COMEM_KV_EVICT_H
 #define COMEM_KV_EVICT_H
@@ -31,6 +31,11 @@
 #ifdef __cplusplus
 extern "C" {
 #endif
+
+/* *workspace_bytes_out gets the bytes that a weights call with these bounds can
+ * use (0: none). */
+comem_status comem_attn_weights_workspace(const comem_decode_attn_plan* plan, int32_t batch, int32_t max_q_len,
+                                          int64_t max_ctx_len, size_t* workspace_bytes_out);
 
 /* Attention weights over a contiguous / ragged cache.
  *   q          [rows, h_q, d_h] dense, as in the attention calls; 16-byte aligned.
@@ -49,6 +54,11 @@ extern "C" {
  *   weights    float32 [batch, weights_stride]: element (b, t), t < L_b, is
  *              written, the others are left as they were.
  *   weights_stride >= max_ctx_len.
+ *   workspace  device memory, 256-byte aligned, of any size, or NULL; no
+ *              initialisation, nothing kept between calls. With the bytes that
+ *              comem_attn_weights_workspace says, many query rows over few
+ *              tokens are shared by several workgroups, and a second kernel
+ *              adds up their sums (another order of the same additions).
  * k, strides, seq_start, ctx_lens, batch and max_ctx_len as in
  * comem_decode_attn. A sequence with ctx_lens[b] outside [0, max_ctx_len], or
  * q_lens[b] outside [1, min(ctx_lens[b], max_q_len)], is left as it is. */
@@ -56,7 +66,8 @@ comem_status comem_attn_weights(const comem_decode_attn_plan* plan, const void* 
                                 const int64_t* q_start, const int32_t* q_lens, int32_t max_q_len, const void* k,
                                 int64_t stride_token, int64_t stride_head, const int64_t* seq_start,
                                 const int32_t* ctx_lens, int32_t batch, int64_t max_ctx_len, const float* prior,
-                                float decay, float* weights, int64_t weights_stride, void* hip_stream);
+                                float decay, float* weights, int64_t weights_stride, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
 
 /* Paged cache; pages, strides and block table as in comem_decode_attn_paged. */
 comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const void* q, const float* lse,
@@ -65,7 +76,8 @@ comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const 
                                       int64_t stride_head, int32_t page_size, int64_t num_pages,
                                       const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
                                       int32_t batch, int64_t max_ctx_len, const float* prior, float decay,
-                                      float* weights, int64_t weights_stride, void* hip_stream);
+                                      float* weights, int64_t weights_stride, void* workspace,
+                                      size_t workspace_bytes, void* hip_stream);
 
 /* The tokens of row r = rows[i] (rows NULL: r = i) that stay: of its L =
  * ctx_lens[r] tokens the first `first`, the last `last` and, of those between,
@@ -91,7 +103,7 @@ comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const 
  *   kept       float32 [n, keep_stride] or NULL: the weights of the tokens that
  *              stay, in the places they have after comem_kv_compact.
  * Of the plan only max_ctx_len and the device matter. Outputs may not overlap
- * the inputs. */
+ * the inputs. One kernel, no workspace. */
 comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* weights, int64_t weights_stride,
                                const int32_t* ctx_lens, int32_t num_rows, const int32_t* rows, int32_t n,
                                int64_t max_ctx_len, int32_t budget, const int32_t* budgets, int32_t first,

@@ -40,7 +40,8 @@ PREFILL_FP8_EXPORTED = ("comem_prefill_fp8_workspace", "comem_prefill_fp8_attn",
 ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
 PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_reserve_granted", "comem_kv_fork",
                   "comem_kv_compact", "comem_kv_release")
-EVICT_EXPORTED = ("comem_attn_weights", "comem_attn_weights_paged", "comem_keep_tokens")
+EVICT_EXPORTED = ("comem_attn_weights_workspace", "comem_attn_weights", "comem_attn_weights_paged",
+                  "comem_keep_tokens")
 BLOCK_EXPORTED = ("comem_block_bounds", "comem_block_scores", "comem_block_select", "comem_block_attn")
 ROPE_INTERLEAVED = 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # COMEM_NOALLOC_SCRATCH_BYTES
@@ -214,9 +215,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comem_prefill_fp8_attn.argtypes = lib.comem_prefill_attn_split.argtypes
     lib.comem_prefill_fp8_attn_paged.argtypes = lib.comem_prefill_attn_split_paged.argtypes
     f32 = ctypes.c_float
-    lib.comem_attn_weights.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, i32, i64, vp, f32, vp, i64, vp]
+    lib.comem_attn_weights_workspace.argtypes = lib.comem_prefill_attn_workspace.argtypes
+    lib.comem_attn_weights.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, i32, i64, vp, f32, vp, i64, vp, sz,
+                                       vp]
     lib.comem_attn_weights_paged.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, i64, i32, i64, vp, i32, vp, i32, i64,
-                                             vp, f32, vp, i64, vp]
+                                             vp, f32, vp, i64, vp, sz, vp]
     lib.comem_keep_tokens.argtypes = [vp, vp, i64, vp, i32, vp, i32, i64, i32, vp, i32, i32, vp, i64, vp, vp, vp, vp]
     lib.comem_block_bounds.argtypes = [vp, vp, i64, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, vp, vp]
     lib.comem_block_scores.argtypes = [vp, vp, vp, i32, i64, vp, i32, vp, i32, i64, vp, i64, vp]
@@ -486,20 +489,29 @@ def comem_kv_release(plan, pages: PagesState, rows, n, stream) -> None:
     _check(load_library().comem_kv_release(plan, ctypes.byref(pages), rows, n, stream), "comem_kv_release")
 
 
+def comem_attn_weights_workspace(plan, batch, max_q_len, max_ctx_len) -> int:
+    nbytes = ctypes.c_size_t()
+    _check(load_library().comem_attn_weights_workspace(plan, batch, max_q_len, max_ctx_len, ctypes.byref(nbytes)),
+           "comem_attn_weights_workspace")
+    return nbytes.value
+
+
 def comem_attn_weights(plan, q, lse, q_start, q_lens, max_q_len, k, stride_token, stride_head, seq_start, ctx_lens,
-                       batch, max_ctx_len, prior, decay, weights, weights_stride, stream) -> None:
+                       batch, max_ctx_len, prior, decay, weights, weights_stride, workspace, workspace_bytes,
+                       stream) -> None:
     _check(load_library().comem_attn_weights(plan, q, lse, q_start, q_lens, max_q_len, k, stride_token, stride_head,
                                              seq_start, ctx_lens, batch, max_ctx_len, prior, decay, weights,
-                                             weights_stride, stream), "comem_attn_weights")
+                                             weights_stride, workspace, workspace_bytes, stream), "comem_attn_weights")
 
 
 def comem_attn_weights_paged(plan, q, lse, q_start, q_lens, max_q_len, k_pages, stride_page, stride_token, stride_head,
                              page_size, num_pages, block_table, max_pages_per_seq, ctx_lens, batch, max_ctx_len, prior,
-                             decay, weights, weights_stride, stream) -> None:
+                             decay, weights, weights_stride, workspace, workspace_bytes, stream) -> None:
     _check(load_library().comem_attn_weights_paged(plan, q, lse, q_start, q_lens, max_q_len, k_pages, stride_page,
                                                    stride_token, stride_head, page_size, num_pages, block_table,
                                                    max_pages_per_seq, ctx_lens, batch, max_ctx_len, prior, decay,
-                                                   weights, weights_stride, stream), "comem_attn_weights_paged")
+                                                   weights, weights_stride, workspace, workspace_bytes, stream),
+           "comem_attn_weights_paged")
 
 
 def comem_keep_tokens(plan, weights, weights_stride, ctx_lens, num_rows, rows, n, max_ctx_len, budget, budgets, first,
@@ -953,7 +965,12 @@ class DecodeAttention:
         return comem_prefill_attn_workspace(self.plan, batch, max_q_len, max_ctx_len)
 
     def _prefill_workspace(self, batch, max_q_len, max_ctx_len, stream, given=None):
-        """Scratch of one prefill call, or None when the library would not use any: the caller's, or else from torch's
+        if given is None and max_ctx_len < PREFILL_SPLIT_MIN_CTX:
+            return None
+        return self._scratch(lambda: self.prefill_workspace_bytes(batch, max_q_len, max_ctx_len), stream, given)
+
+    def _scratch(self, needed, stream, given):
+        """Scratch of one call, or None when the library would not use any: the caller's, or else from torch's
         allocator on the call's stream, going back to it when the call has been enqueued. So no two calls share it,
         whatever their streams and threads, and later work on the stream may reuse it. A stream that is being captured
         gets it only from the capture's own pool, which stays the graph's: in a capture that torch did not begin, the
@@ -964,9 +981,7 @@ class DecodeAttention:
             _need(isinstance(given, torch.Tensor) and given.device == self._torch_device and given.is_contiguous(),
                   f"workspace must be a contiguous tensor on {self._torch_device}")
             return given
-        if max_ctx_len < PREFILL_SPLIT_MIN_CTX:
-            return None
-        nbytes = self.prefill_workspace_bytes(batch, max_q_len, max_ctx_len)
+        nbytes = needed()
         if nbytes == 0 or not (stream is None or isinstance(stream, torch.cuda.Stream)):
             return None
 
@@ -1167,8 +1182,12 @@ class DecodeAttention:
               f"{name} must have dense rows of at least {width} elements, got {tuple(t.shape)}")
         _need(rows <= 1 or t.stride(0) >= t.shape[1], f"the rows of {name} must not overlap")
 
+    def attn_weights_workspace_bytes(self, batch: int, max_q_len: int, max_ctx_len: int) -> int:
+        """Bytes of a workspace that a weights call with these bounds can use (0: none)."""
+        return comem_attn_weights_workspace(self.plan, batch, max_q_len, max_ctx_len)
+
     def _weights_args(self, q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior, decay, out, paged,
-                      stream):
+                      stream, workspace):
         import torch
 
         tensor, at, f32, i32 = torch.Tensor, self._at, torch.float32, torch.int32
@@ -1207,30 +1226,34 @@ class DecodeAttention:
                 self._check_rows_of(name, t, batch, width)
         stride = out.stride(0) if batch > 1 else out.shape[1]
         _need(prior is None or batch <= 1 or prior.stride(0) == stride, "prior and out must have the same row stride")
+        ws = workspace
+        if ws is not None or max_q_len > 1:
+            ws = self._scratch(lambda: self.attn_weights_workspace_bytes(batch, int(max_q_len), width), stream, workspace)
         return batch, out, (self.plan, q.data_ptr(), lse.data_ptr(), None if q_start is None else q_start.data_ptr(),
                             None if q_lens is None else q_lens.data_ptr(), int(max_q_len), k.data_ptr()), (
             ctx_lens.data_ptr(), batch, width, None if prior is None else prior.data_ptr(), float(decay),
-            out.data_ptr(), stride)
+            out.data_ptr(), stride, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes), ws
 
     def attn_weights(self, q, lse, k, seq_start, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
-                     max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None):
+                     max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None, workspace=None):
         """What each cached token was paid by the new tokens' queries q [rows, Hq, D], whose attention returned lse
         [rows, Hq]: out[b, t] = decay * prior[b, t] + the sum of its attention weights over heads and new tokens.
 
         Without q_start and q_lens each sequence has one new token, else as in prefill. out (float32 [B, >= max_ctx_len])
         may be prior itself; the new tokens' own prior is 0, and elements past a context stay (0 where out is made here).
+        workspace: as in prefill (attn_weights_workspace_bytes says how much can be used).
         """
-        batch, out, head, tail = self._weights_args(q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior,
-                                                    decay, out, False, stream)
+        batch, out, head, tail, ws = self._weights_args(q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len,
+                                                        prior, decay, out, False, stream, workspace)
         self._check_lengths(ctx_lens, batch, seq_start=seq_start)
         _call_on(self, stream, comem_attn_weights, *head, k.stride(0), k.stride(1), seq_start.data_ptr(), *tail)
         return out
 
     def attn_weights_paged(self, q, lse, k_pages, block_table, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
-                           max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None):
+                           max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None, workspace=None):
         """The same over a paged cache."""
-        batch, out, head, tail = self._weights_args(q, lse, k_pages, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len,
-                                                    prior, decay, out, True, stream)
+        batch, out, head, tail, ws = self._weights_args(q, lse, k_pages, ctx_lens, max_ctx_len, q_start, q_lens,
+                                                        max_q_len, prior, decay, out, True, stream, workspace)
         self._check_lengths(ctx_lens, batch, block_table=block_table)
         pool, strides = k_pages.shape, k_pages.stride()
         _call_on(self, stream, comem_attn_weights_paged, *head, strides[0], strides[1], strides[2], pool[1], pool[0],

@@ -26,11 +26,12 @@ typedef __bf16 dot_bf16x8 __attribute__((ext_vector_type(8)));
 template <int D, CacheType C>
 struct DotPart {
   static constexpr int kLoads = C == CacheType::kF32 ? D / 16 : D / 32;
+  static constexpr int kStep = C == CacheType::kFp8 ? 16 : 64;  // bytes from one load to the next
   dot_u32x4 x[kLoads];
+  static __device__ int lane_offset(int g) { return C == CacheType::kFp8 ? (D / 2) * g : 16 * g; }
   // row: the query row (of the cache's type, bf16 for codes).
   __device__ void load_query(const char* row, int g) {
-    const char* at = row + (C == CacheType::kFp8 ? (D / 2) * g : 16 * g);
-    constexpr int kStep = C == CacheType::kFp8 ? 16 : 64;
+    const char* at = row + lane_offset(g);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) x[i] = *reinterpret_cast<const dot_u32x4*>(at + kStep * i);
   }

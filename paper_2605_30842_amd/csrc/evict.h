@@ -14,7 +14,7 @@ inline CacheType cache_type(const comem_decode_attn_config& c) {
   return c.dtype == COMEM_F32 ? CacheType::kF32 : c.dtype == COMEM_BF16 ? CacheType::kBf16 : CacheType::kFp8;
 }
 
-constexpr int kWeightsWaves = 4;  // waves of a workgroup, on the same tokens
+constexpr int kWeightsWaves = 8;  // most waves of a workgroup, on the same tokens
 
 // Offsets and strides are in bytes, but for that of the weights.
 struct WeightsParams {
@@ -28,6 +28,7 @@ struct WeightsParams {
   const int32_t* block_table;  // paged layout, [B, max_pages]
   const float* prior;          // or nullptr
   float* weights;
+  float* partial;              // [splits, B, max_ctx], or nullptr: one workgroup has a tile's query rows
   int64_t weights_stride;
   int64_t stride_token;
   int64_t stride_head;
@@ -45,8 +46,15 @@ struct WeightsParams {
 };
 
 using WeightsKernelFn = void (*)(WeightsParams);
-// sub: 16-token slabs of a workgroup, 1, 2 or 4 (float32: at most 2).
-WeightsKernelFn select_weights_kernel(int head_dim, CacheType cache, bool paged, int sub);
+struct WeightsForm {
+  WeightsKernelFn fn;
+  int wave_bytes;  // LDS that the launch gives each wave
+};
+// sub: 16-token slabs of a workgroup, 2, 4 or 6 (float32: 2). ring: for many
+// groups of 16 query rows.
+WeightsForm select_weights_kernel(int head_dim, CacheType cache, bool paged, int sub, bool ring);
+using AddWeightsKernelFn = void (*)(WeightsParams, int);
+AddWeightsKernelFn add_weights_kernel_fn();
 
 // The largest entries of a row, in ascending order.
 struct ChooseParams {

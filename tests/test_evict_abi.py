@@ -29,7 +29,7 @@ def plan():
 
 def _weights(plan, **kw):
     a = dict(q=A, lse=A, q_start=A, q_lens=A, max_q_len=7, k=A, stride_token=1024, stride_head=128, seq_start=A,
-             ctx_lens=A, batch=3, max_ctx_len=4096, prior=A, decay=0.5, weights=A, weights_stride=4096)
+             ctx_lens=A, batch=3, max_ctx_len=4096, prior=A, decay=0.5, weights=A, weights_stride=4096, workspace=None, nbytes=0)
     a.update(kw)
     return B.load_library().comem_attn_weights(plan, *a.values(), None)
 
@@ -37,7 +37,7 @@ def _weights(plan, **kw):
 def _paged(plan, **kw):
     a = dict(q=A, lse=A, q_start=A, q_lens=A, max_q_len=7, k=A, stride_page=16 * 1024, stride_token=1024,
              stride_head=128, page_size=16, num_pages=100, block_table=A, max_pages=256, ctx_lens=A, batch=3,
-             max_ctx_len=4096, prior=A, decay=0.5, weights=A, weights_stride=4096)
+             max_ctx_len=4096, prior=A, decay=0.5, weights=A, weights_stride=4096, workspace=None, nbytes=0)
     a.update(kw)
     return B.load_library().comem_attn_weights_paged(plan, *a.values(), None)
 
@@ -83,7 +83,7 @@ def test_empty_calls_look_at_nothing(plan):
     (dict(stride_head=132), B.ERR_MISALIGNED), (dict(q=A + 8), B.ERR_MISALIGNED), (dict(k=A + 8), B.ERR_MISALIGNED),
     (dict(lse=A + 2), B.ERR_MISALIGNED), (dict(q_start=A + 4), B.ERR_MISALIGNED), (dict(q_lens=A + 2), B.ERR_MISALIGNED),
     (dict(ctx_lens=A + 2), B.ERR_MISALIGNED), (dict(prior=A + 2), B.ERR_MISALIGNED),
-    (dict(weights=A + 2), B.ERR_MISALIGNED)], ids=str)
+    (dict(weights=A + 2), B.ERR_MISALIGNED), (dict(workspace=A + 64, nbytes=1 << 20), B.ERR_MISALIGNED)], ids=str)
 def test_weights_refusals(plan, kw, status):
     assert _weights(plan, **kw) == status
     assert _paged(plan, **kw) == status
@@ -97,6 +97,22 @@ def test_weights_refusals(plan, kw, status):
     (dict(block_table=A + 2), B.ERR_MISALIGNED)], ids=str)
 def test_paged_refusals(plan, kw, status):
     assert _paged(plan, **kw) == status
+
+
+def test_workspace(plan):
+    """None for a step and for what fills the chip; a sum for each token and part otherwise; the call's own bounds hold."""
+    size = lambda *a: B.comem_attn_weights_workspace(plan, *a)  # noqa: E731
+    assert size(4, 1, 4096) == size(0, 5, 4096) == size(4, 0, 4096) == 0
+    assert size(1, 300, 4096) >= 2 * 4096 * 4 and size(1, 300, 4096) % 256 == 0
+    for a in ((5, 1, 4096), (-1, 1, 4096), (1, -1, 4096), (1, 5, 4), (1, 1, 4097), (1, 1, -1)):
+        with pytest.raises(B.ComemError) as e:
+            size(*a)
+        assert e.value.status == B.ERR_INVALID_SHAPE
+    with pytest.raises(B.ComemError):
+        B.comem_attn_weights_workspace(None, 1, 1, 1)
+    assert B.load_library().comem_attn_weights_workspace(plan, 1, 1, 1, None) == B.ERR_NULL_POINTER
+    for nbytes in (0, 1, 1 << 30):
+        assert _weights(plan, workspace=A, nbytes=nbytes) == _paged(plan, workspace=A, nbytes=nbytes) == B.ERR_NO_DEVICE
 
 
 def test_contiguous_refusals(plan):
@@ -134,10 +150,11 @@ def op(monkeypatch):
     def sentinel(*a, **k):
         raise Reached()
 
-    for name in B.EVICT_EXPORTED:
+    for name in B.EVICT_EXPORTED[1:]:
         monkeypatch.setattr(B, name, sentinel)
     o = object.__new__(B.DecodeAttention)
-    o.plan = None
+    o.plan, _ = B.comem_decode_attn_init(B.Config(num_q_heads=8, num_kv_heads=2, head_dim=64, dtype=B.BF16, scale=0.1,
+                                                  max_batch=4, max_ctx_len=64), B.NO_DEVICE)
     o.dtype, o.device = "bf16", 0
     o.num_q_heads, o.num_kv_heads, o.head_dim = 8, 2, 64
     o._torch_device = torch.device("cpu")
@@ -160,7 +177,8 @@ def test_wrapper_good_calls(op):
     for kw in ({}, dict(out=None), dict(out=None, prior=None), dict(prior=None),
                dict(q_start=None, q_lens=None, max_q_len=1, q=torch.zeros(3, 8, 64, dtype=torch.bfloat16),
                     lse=torch.zeros(3, 8)),
-               dict(out=torch.zeros(3, 64)[:, :32], prior=torch.zeros(3, 64)[:, 5:37])):
+               dict(out=torch.zeros(3, 64)[:, :32], prior=torch.zeros(3, 64)[:, 5:37]),
+               dict(workspace=torch.zeros(256, dtype=torch.uint8))):
         if kw.get("out", 1) is None and "prior" not in kw:
             kw = dict(kw, prior=torch.zeros(3, 20))
         with pytest.raises(Reached):
@@ -178,7 +196,7 @@ def test_wrapper_good_calls(op):
     dict(seq_start=torch.zeros(3, dtype=torch.int32)), dict(ctx_lens=torch.zeros(3)), dict(max_ctx_len=20.0),
     dict(max_q_len=True), dict(out=torch.zeros(3, 19)), dict(out=torch.zeros(2, 32)),
     dict(out=torch.zeros(32, 3).T), dict(prior=torch.zeros(3, 19)), dict(prior=torch.zeros(3, 31)),
-    dict(prior=torch.zeros(3, 32).half()), dict(out=torch.zeros(1, 32).expand(3, 32))], ids=lambda kw: str(list(kw)))
+    dict(prior=torch.zeros(3, 32).half()), dict(workspace=torch.zeros(64, 64)[:, 1]), dict(workspace=5), dict(out=torch.zeros(1, 32).expand(3, 32))], ids=lambda kw: str(list(kw)))
 def test_wrapper_refusals(op, kw):
     with pytest.raises(ValueError):
         op.attn_weights(**_tensors(**kw))

@@ -59,7 +59,7 @@ class Case:
 
 
 SHAPES = [  # hkv, group, d
-    (8, 4, 128), (2, 8, 64), (1, 1, 128), (3, 16, 64), (5, 2, 128), (1, 16, 128)]
+    (8, 4, 128), (2, 8, 64), (1, 1, 128), (3, 16, 64), (5, 2, 128), (1, 16, 128), (20, 4, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
@@ -125,6 +125,51 @@ def test_many_tiles_and_rows():
         say("weights tiles", lens, new)
         c = Case(lens, new, "bf16", 2, 4, 64, page)
         c.check(c.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("lens,new", [([900], [900]), ([300, 1, 257], [300, 1, 100]), ([60], [3])])
+def test_shared_rows(dtype, lens, new):
+    """Many rows over few tokens: shared by several workgroups with a workspace, and not without a large enough one."""
+    c = Case(lens, new, dtype, 2, 4, 64, 16)
+    most = max(new)
+    nbytes = c.op.attn_weights_workspace_bytes(len(lens), most, c.bound)
+    assert (nbytes > 0) == (most > 8)
+    prior = torch.rand((len(lens), c.bound), generator=c.gen)
+    for ws in (None, torch.empty(1, dtype=torch.uint8, device=DEV), torch.full((nbytes // 4,), float("nan"), device=DEV)):
+        out = torch.full((len(lens), c.bound + 3), -7.0, device=DEV)
+        old = torch.full_like(out, float("nan"))
+        old[:, :c.bound] = prior.to(DEV)
+        c.call(out=out, prior=old, decay=0.5, workspace=ws if ws is None or ws.numel() else None)
+        c.check(out, prior, 0.5, what=str(ws is None))
+        for b, n in enumerate(lens):
+            assert bool((out[b, n:] == -7.0).all())
+
+
+def test_shared_rows_captured():
+    """Scratch of a captured call belongs to its graph."""
+    c = Case([500, 400], [200, 400], "bf16", 2, 4, 64, 0)
+    x, q, lse = c.ctx.to(DEV), c.q.to(DEV), c.lse.to(DEV)
+    rows = dict(q_start=torch.tensor([0, 200], dtype=torch.int64, device=DEV),
+                q_lens=torch.tensor([200, 400], dtype=torch.int32, device=DEV), max_q_len=400)
+
+    def call(**kw):
+        return c.op.attn_weights(q, lse, x["k"], x["seq_start"], x["ctx_lens"], 500, **rows, **kw)
+
+    want = call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        torch.full((1 << 20,), float("nan"), device=DEV)  # the allocator's free memory
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    stream = torch.cuda.Stream()
+    other = call(stream=stream)
+    stream.synchronize()
+    assert torch.equal(other, want)
 
 
 def test_rows_that_saw_nothing():
