@@ -1403,19 +1403,27 @@ class DecodeAttention:
         tokens of the pages table[b, hk] (block_select's results; max_len bounds lens)."""
         import torch
 
-        tensor, at, i32 = torch.Tensor, self._at, torch.int32
-        self._check_q_out(q, out, lse)
+        tensor, at, i32, f32 = torch.Tensor, self._at, torch.int32, torch.float32
+        if not (isinstance(q, tensor) and isinstance(table, tensor) and isinstance(lens, tensor) and q.dim() == 3
+                and q.shape[1] == self.num_q_heads and q.shape[2] == self.head_dim and q.dtype in self._q_dtypes
+                and q.get_device() == at and q.is_contiguous()
+                and (out is None or (isinstance(out, tensor) and out.shape == q.shape and out.dtype is f32
+                                     and out.get_device() == at and out.is_contiguous()))
+                and (lse is None or (isinstance(lse, tensor) and lse.shape == q.shape[:2] and lse.dtype is f32
+                                     and lse.get_device() == at and lse.is_contiguous()))
+                and table.dim() == 3 and table.dtype is i32 and table.shape[0] == q.shape[0]
+                and table.shape[1] == self.num_kv_heads and table.get_device() == at and table.is_contiguous()
+                and lens.shape == q.shape[:1] and lens.dtype is i32 and lens.get_device() == at
+                and lens.is_contiguous()):
+            self._check_q_out(q, out, lse)
+            self._dense("table", table, i32, (q.shape[0], self.num_kv_heads, None))
+            self._dense("lens", lens, i32, (q.shape[0],))
         self._check_cache(k_pages, v_pages, paged=True)
         if type(max_len) is not int:
             self._check_bound(max_len, "max_len")
         batch = q.shape[0]
-        if not (isinstance(table, tensor) and isinstance(lens, tensor) and table.dim() == 3 and table.dtype is i32
-                and table.shape[0] == batch and table.shape[1] == self.num_kv_heads and table.get_device() == at
-                and table.is_contiguous() and lens.shape == (batch,) and lens.dtype is i32
-                and lens.get_device() == at and lens.is_contiguous()):
-            self._dense("table", table, i32, (batch, self.num_kv_heads, None))
-            self._dense("lens", lens, i32, (batch,))
-        out, lse = self._outputs(q, out, lse)
+        if out is None:
+            out = _empty_on(stream, q, q.shape, dtype=f32)
         pool, strides = k_pages.shape, k_pages.stride()
         _call_on(self, stream, comem_block_attn, self.plan, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
                  strides[0], strides[1], strides[2], pool[1], pool[0], table.data_ptr(), table.shape[2],
