@@ -93,8 +93,9 @@ comem_status comem_block_select(const comem_decode_attn_plan* plan, const float*
  *              ceil(max_len / page_size).
  *   lens       device int32 [batch]; max_len the host's bound of them, at most
  *              the plan's max_ctx_len.
- * Other arguments, workspace and results as in comem_decode_attn_paged: with
- * one table for all heads the same bits. */
+ * Other arguments, workspace and results as in comem_decode_attn_paged, but
+ * that the weights enter the matrix cores in three bf16 parts instead of two:
+ * a weight is off by less than 2^-26 of itself. */
 comem_status comem_block_attn(const comem_decode_attn_plan* plan, const void* q, const void* k_pages,
                               const void* v_pages, int64_t stride_page, int64_t stride_token, int64_t stride_head,
                               int32_t page_size, int64_t num_pages, const int32_t* table, int32_t max_blocks,

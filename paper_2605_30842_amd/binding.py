@@ -1338,7 +1338,7 @@ class DecodeAttention:
         if not (isinstance(bounds, torch.Tensor) and bounds.dtype is k_pages.dtype and bounds.get_device() == self._at
                 and bounds.shape == shape and bounds.is_contiguous()):
             self._dense("bounds", bounds, k_pages.dtype, shape)
-        if q_lens is not None:
+        if q_lens is not None and not _fits(q_lens, torch.Tensor, (torch.int32,), self._torch_device, (batch,)):
             self._dense("q_lens", q_lens, torch.int32, (batch,))
         _call_on(self, stream, comem_block_bounds, self.plan, k_pages.data_ptr(), strides[0], strides[1], strides[2],
                  pool[1], pool[0], block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(),

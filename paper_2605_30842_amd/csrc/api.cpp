@@ -18,9 +18,9 @@
 namespace comem {
 using KernelFn = void (*)(AttnParams);
 using QueueKernelFn = void (*)(AttnParams, int);
-KernelFn select_mfma_kernel(int head_dim, bool paged, int page_size, bool fp8);
-QueueKernelFn select_mfma_queue_kernel(int head_dim, bool paged, int page_size, bool fp8);
-QueueKernelFn select_mfma_balanced_kernel(int head_dim, bool paged, int page_size, bool fp8);
+KernelFn select_mfma_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8);
+QueueKernelFn select_mfma_queue_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8);
+QueueKernelFn select_mfma_balanced_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8);
 int mfma_max_queue_batch();
 KernelFn select_valu_kernel(bool bf16, int head_dim, int group, bool paged);
 }  // namespace comem
@@ -325,8 +325,8 @@ bool uses_balanced(const comem_decode_attn_plan& p, const Counters& c, int64_t b
          batch * (ceil_div(max_ctx + 1, 32) + comem::kPieceTilesLight) < kMaxBalancedTiles;
 }
 
-comem_status launch_balanced(const comem_decode_attn_plan& p, bool paged, comem::AttnParams& a, int64_t batch,
-                             void* stream) {
+comem_status launch_balanced(const comem_decode_attn_plan& p, comem::MfmaPages pages, comem::AttnParams& a,
+                             int64_t batch, void* stream) {
   // No more ranges than the call's bound can fill.
   a.ranges = static_cast<int32_t>(
       std::min(max_ranges(p), batch * ceil_div(std::max<int64_t>(a.max_ctx, 1), kMinRangeTokens)));
@@ -335,7 +335,7 @@ comem_status launch_balanced(const comem_decode_attn_plan& p, bool paged, comem:
   const int page = a.page_mask + 1;
   hipError_t err;
   if (batch == 1) {
-    comem::KernelFn fn = comem::select_mfma_kernel(p.cfg.head_dim, paged, page, is_fp8(p.cfg));
+    comem::KernelFn fn = comem::select_mfma_kernel(p.cfg.head_dim, pages, page, is_fp8(p.cfg));
     if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
     a.num_splits = a.ranges;
     a.whole_tiles = static_cast<int32_t>(whole_tokens(p, max_ranges(p)) / 32);
@@ -343,7 +343,7 @@ comem_status launch_balanced(const comem_decode_attn_plan& p, bool paged, comem:
     err = hipLaunchKernel(reinterpret_cast<const void*>(fn), dim3(ranges, heads), dim3(comem::kThreads), args, 0,
                           static_cast<hipStream_t>(stream));
   } else {
-    comem::QueueKernelFn fn = comem::select_mfma_balanced_kernel(p.cfg.head_dim, paged, page, is_fp8(p.cfg));
+    comem::QueueKernelFn fn = comem::select_mfma_balanced_kernel(p.cfg.head_dim, pages, page, is_fp8(p.cfg));
     if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
     int nb = static_cast<int>(batch);
     void* args[] = {&a, &nb};
@@ -353,7 +353,7 @@ comem_status launch_balanced(const comem_decode_attn_plan& p, bool paged, comem:
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }
 
-comem_status launch(const comem_decode_attn_plan& p, bool paged, comem::AttnParams& a, int64_t batch,
+comem_status launch(const comem_decode_attn_plan& p, comem::MfmaPages pages, comem::AttnParams& a, int64_t batch,
                     int64_t splits, bool queue, void* stream) {
   const bool bf16 = p.cfg.dtype == COMEM_BF16;
   const int64_t items = batch * p.cfg.num_kv_heads * splits;
@@ -366,7 +366,7 @@ comem_status launch(const comem_decode_attn_plan& p, bool paged, comem::AttnPara
   const bool whole = p.cfg.chunk_tokens == 0 && !long_call(p, batch, a.max_ctx) &&
                      batch * p.cfg.num_kv_heads >= p.num_cus;
   if (queue && items > resident && !whole) {
-    comem::QueueKernelFn qfn = comem::select_mfma_queue_kernel(p.cfg.head_dim, paged, a.page_mask + 1, is_fp8(p.cfg));
+    comem::QueueKernelFn qfn = comem::select_mfma_queue_kernel(p.cfg.head_dim, pages, a.page_mask + 1, is_fp8(p.cfg));
     if (qfn == nullptr) return COMEM_ERR_UNSUPPORTED;
     dim3 grid(static_cast<unsigned>(items < resident ? items : resident));
     dim3 block(comem::kThreads);
@@ -376,8 +376,9 @@ comem_status launch(const comem_decode_attn_plan& p, bool paged, comem::AttnPara
                                            static_cast<hipStream_t>(stream));
     return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
   }
-  comem::KernelFn fn = uses_mfma(p) ? comem::select_mfma_kernel(p.cfg.head_dim, paged, a.page_mask + 1, is_fp8(p.cfg))
-                                    : comem::select_valu_kernel(bf16, p.cfg.head_dim, group_of(p.cfg), paged);
+  comem::KernelFn fn = uses_mfma(p) ? comem::select_mfma_kernel(p.cfg.head_dim, pages, a.page_mask + 1, is_fp8(p.cfg))
+                                    : comem::select_valu_kernel(bf16, p.cfg.head_dim, group_of(p.cfg),
+                                                                  pages != comem::MfmaPages::kNone);
   if (fn == nullptr) return COMEM_ERR_UNSUPPORTED;
   dim3 grid(static_cast<unsigned>(splits), static_cast<unsigned>(p.cfg.num_kv_heads),
             static_cast<unsigned>(batch));
@@ -498,8 +499,8 @@ comem_status decode_contiguous(const comem_decode_attn_plan* plan, const void* q
     a.new_k = static_cast<const char*>(new_k);
     a.new_v = static_cast<const char*>(new_v);
   }
-  if (balanced) return launch_balanced(*p, false, a, batch, hip_stream);
-  return launch(*p, false, a, batch, splits, queue, hip_stream);
+  if (balanced) return launch_balanced(*p, comem::MfmaPages::kNone, a, batch, hip_stream);
+  return launch(*p, comem::MfmaPages::kNone, a, batch, splits, queue, hip_stream);
 }
 
 comem_status decode_paged(const comem_decode_attn_plan* plan, const void* q, const void* new_k,
@@ -546,8 +547,9 @@ comem_status decode_paged(const comem_decode_attn_plan* plan, const void* q, con
     a.new_k = static_cast<const char*>(new_k);
     a.new_v = static_cast<const char*>(new_v);
   }
-  if (balanced) return launch_balanced(*p, true, a, batch, hip_stream);
-  return launch(*p, true, a, batch, splits, queue, hip_stream);
+  const comem::MfmaPages pages = head_tables ? comem::MfmaPages::kHeads : comem::MfmaPages::kSequence;
+  if (balanced) return launch_balanced(*p, pages, a, batch, hip_stream);
+  return launch(*p, pages, a, batch, splits, queue, hip_stream);
 }
 
 }  // namespace

@@ -22,6 +22,10 @@ namespace comem {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
+// How the matrix-core decode kernels find a token's rows: packed, by the
+// sequence's block table, by one for each KV head.
+enum class MfmaPages { kNone, kSequence, kHeads };
+
 constexpr int kWaves = 4;           // waves per workgroup
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxGroup = 16;       // largest GQA group handled in one workgroup
@@ -43,12 +47,12 @@ struct AttnParams {
   float* lse;          // [B, Hq] or nullptr
   const int64_t* seq_start;   // contiguous layout
   const int32_t* ctx_lens;
-  const int32_t* block_table; // paged layout, [B, max_pages], or of each KV head [B, Hkv, max_pages]
+  const int32_t* block_table; // paged layout, [B, max_pages]; with a table for each KV head [B, Hkv, max_pages]
   int64_t stride_token;
   int64_t stride_head;
   int64_t stride_page;
   int32_t max_pages;   // entries of a table row
-  int32_t head_tables; // table rows of a sequence: 1, or Hkv
+  int32_t head_tables; // vector-ALU kernel: table rows of a sequence, 1 or Hkv
   int32_t page_shift;  // log2(page_size)
   int32_t page_mask;   // page_size - 1
   int32_t num_q_heads;
@@ -114,10 +118,9 @@ __device__ inline int uniform_i32(int x) {
   return static_cast<int>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)));
 }
 
-// Block-table row of KV head hk of sequence b.
-__device__ inline const int32_t* table_row(const AttnParams& p, int b, int hk) {
-  const int64_t row = static_cast<int64_t>(b) * p.head_tables + (p.head_tables > 1 ? hk : 0);
-  return p.block_table + row * p.max_pages;
+// Block-table row of KV head hk of sequence b, which has `tables` rows (1: the heads' common one).
+__device__ inline const int32_t* table_row(const AttnParams& p, int b, int hk, int tables) {
+  return p.block_table + (static_cast<int64_t>(b) * tables + (tables > 1 ? hk : 0)) * p.max_pages;
 }
 
 // Byte offset of token t of a sequence relative to the (hk-offset) K/V base.
@@ -147,6 +150,12 @@ __device__ inline void split_bf16(float p0, float p1, uint32_t& hi, uint32_t& lo
   hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{p0, p1}), bf16x2_t));
   const f32x2_t r = {p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)};
   lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, bf16x2_t));
+}
+
+// The same in three parts, p = hi + mid + lo to less than 2^-26 relative.
+__device__ inline void split_bf16_3(float p0, float p1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{p0, p1}), bf16x2_t));
+  split_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u), mid, lo);
 }
 
 // Fused KV append (paper Sec. 2.2: the new token's key and value join the

@@ -117,8 +117,25 @@ __global__ __launch_bounds__(kBoundsThreads) void block_bounds_kernel(const Boun
     Ends<C> ends;
     ends.clear();
     if (works) {
-#pragma unroll 8
-      for (int t = slot; t < tokens; t += slots) ends.add(*reinterpret_cast<const dot_u32x4*>(k + t * p.stride_token));
+      // Four tokens at a time, the next four asked for ahead; past the last
+      // token it is read again.
+      dot_u32x4 x[4], next[4];
+      auto ask = [&](int t, dot_u32x4 (&y)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          y[e] = *reinterpret_cast<const dot_u32x4*>(k + min(t + e * slots, tokens - 1) * p.stride_token);
+      };
+      ask(slot, x);
+#pragma unroll 1
+      for (int t = slot;;) {
+        t += 4 * slots;
+        if (t < tokens) ask(t, next);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ends.add(x[e]);
+        if (t >= tokens) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = next[e];
+      }
     }
     // Slots with a token: halved until one is left.
     for (int live = min(slots, tokens); live > 1;) {

@@ -153,7 +153,13 @@ __device__ inline void widen_tile(const Tile8<D>& R, Tile<D>& T) {
 // per-sequence offsets live in LDS).
 constexpr int kMaxQueueBatch = 4096;
 
-enum class Layout { kContig, kPaged, kPagedFine };
+// kHeads: paged, with a block table for each KV head (attention over chosen
+// blocks). These forms also take the weights in three parts instead of two, see
+// compute_tile.
+enum class Layout { kContig, kPaged, kPagedFine, kHeads, kHeadsFine };
+constexpr bool pages_by_half(Layout l) { return l == Layout::kPaged || l == Layout::kHeads; }  // 16 tokens and more
+constexpr bool pages_by_lane(Layout l) { return l == Layout::kPagedFine || l == Layout::kHeadsFine; }
+constexpr bool table_per_head(Layout l) { return l == Layout::kHeads || l == Layout::kHeadsFine; }
 
 template <int D, Layout LAYOUT, bool FP8>
 struct Loader {
@@ -201,14 +207,14 @@ struct Loader {
   __device__ int32_t entry_of(int t) const { return bt_row[min(t, t_end - 1) >> page_shift]; }
   // Entries of the wave's tiles n .. n + 31 (n a multiple of 32), or of its tile n.
   __device__ int32_t entries(int n) const {
-    if constexpr (LAYOUT == Layout::kPaged) return entry_of(t_first + t_step * (n + (lane >> 1)) + 16 * (lane & 1));
+    if constexpr (pages_by_half(LAYOUT)) return entry_of(t_first + t_step * (n + (lane >> 1)) + 16 * (lane & 1));
     return entry_of(t_first + t_step * n + (lane & 31));
   }
   __device__ void first_entries() {
-    if constexpr (LAYOUT == Layout::kPaged) {
+    if constexpr (pages_by_half(LAYOUT)) {
       now = in_pool(entries(0));
       next = entries(32);
-    } else if constexpr (LAYOUT == Layout::kPagedFine) {
+    } else if constexpr (pages_by_lane(LAYOUT)) {
       now = in_pool(entries(0));
       next = entries(1);
     }
@@ -220,12 +226,12 @@ struct Loader {
 
   // Before the request of the wave's tile n (n = 1, 2, ...).
   __device__ void next_entries(int n) {
-    if constexpr (LAYOUT == Layout::kPaged) {
+    if constexpr (pages_by_half(LAYOUT)) {
       if ((n & 31) == 0) {
         now = in_pool(next);
         next = entries(n + 32);
       }
-    } else if constexpr (LAYOUT == Layout::kPagedFine) {
+    } else if constexpr (pages_by_lane(LAYOUT)) {
       now = in_pool(next);
       next = entries(n + 1);
     }
@@ -242,7 +248,7 @@ struct Loader {
   __device__ void load(TileT& T, int n, int t0, bool repeat) const {
     constexpr int KB = D / 32;
     const char* vsrc = repeat ? kbase : vbase;
-    if constexpr (LAYOUT == Layout::kPagedFine) {
+    if constexpr (pages_by_lane(LAYOUT)) {
       constexpr int VBYTES = kElemBytes * D / 16;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -323,7 +329,14 @@ __device__ inline float across_groups(float x, Op op) {
 // With one wave on a SIMD (short calls, and the balanced form) a tile's time
 // is this chain's latency: scores, maximum, weights, products. So nothing in
 // it goes through LDS, and the outputs are rescaled only when a maximum moved.
-template <int D>
+//
+// FINE: P = P_hi + P_mid + P_lo, which leaves out less than 2^-26 of a weight (two
+// parts: 2^-18). Over a few thousand chosen tokens that, and not the sums, is
+// what the result is off by: 1.8e-6 of the outputs' norm with two parts,
+// 3e-7 with three (a float32 softmax in torch: 6e-7). A third product for
+// each two costs a call that memory bounds nothing: 64 blocks of 64, one
+// sequence 9.7 / 9.7 us, 128 for 8 sequences 50.3 / 50.3.
+template <int D, bool FINE>
 __device__ inline void compute_tile(const Tile<D>& T, int t0, int t_end, int g,
                                     const bf16x8 (&qop)[D / 32], float scale_log2, float& m_run,
                                     float& l_run, f32x4 (&acc)[D / 16]) {
@@ -358,13 +371,17 @@ __device__ inline void compute_tile(const Tile<D>& T, int t0, int t_end, int g,
     m_run = m_new;
   }
   float psum = 0.f;
-  uint32_t ph[4], pl[4];
+  uint32_t ph[4], pl[4], pm[4];
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const float p0 = fast_exp2(x[e] - m_new);
     const float p1 = fast_exp2(x[e + 1] - m_new);
     psum += p0 + p1;
-    split_bf16(p0, p1, ph[e / 2], pl[e / 2]);
+    if constexpr (FINE) {
+      split_bf16_3(p0, p1, ph[e / 2], pm[e / 2], pl[e / 2]);
+    } else {
+      split_bf16(p0, p1, ph[e / 2], pl[e / 2]);
+    }
   }
   l_run += psum;
   const bf16x8 p_hi = as_bf16x8(u32x4{ph[0], ph[1], ph[2], ph[3]});
@@ -379,21 +396,24 @@ __device__ inline void compute_tile(const Tile<D>& T, int t0, int t_end, int g,
     va[2] = __builtin_amdgcn_perm(T.v[1][1].word(wi), T.v[1][0].word(wi), sel);
     va[3] = __builtin_amdgcn_perm(T.v[1][3].word(wi), T.v[1][2].word(wi), sel);
     acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va), p_hi, acc[n], 0, 0, 0);
+    if constexpr (FINE)
+      acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va), as_bf16x8(u32x4{pm[0], pm[1], pm[2], pm[3]}), acc[n],
+                                                       0, 0, 0);
     acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va), p_lo, acc[n], 0, 0, 0);
   }
 }
 
 // compute_tile on a tile as loaded (FP8 tiles are widened first).
-template <int D, bool FP8>
+template <int D, bool FP8, bool FINE>
 __device__ inline void compute_loaded(const typename TileOf<D, FP8>::type& T, int t0, int t_end, int g,
                                       const bf16x8 (&qop)[D / 32], float scale_log2, float& m_run, float& l_run,
                                       f32x4 (&acc)[D / 16]) {
   if constexpr (FP8) {
     Tile<D> W;
     widen_tile<D>(T, W);
-    compute_tile<D>(W, t0, t_end, g, qop, scale_log2, m_run, l_run, acc);
+    compute_tile<D, FINE>(W, t0, t_end, g, qop, scale_log2, m_run, l_run, acc);
   } else {
-    compute_tile<D>(T, t0, t_end, g, qop, scale_log2, m_run, l_run, acc);
+    compute_tile<D, FINE>(T, t0, t_end, g, qop, scale_log2, m_run, l_run, acc);
   }
 }
 
@@ -441,7 +461,7 @@ __device__ void attend_split(const AttnParams& p, WaveState<D>& ws, int b, int h
     ld.kbase += seq0;
     ld.vbase += seq0;
   } else {
-    ld.bt_row = table_row(p, b, hk);
+    ld.bt_row = table_row(p, b, hk, table_per_head(LAYOUT) ? p.num_kv_heads : 1);
   }
   ld.pool = static_cast<uint32_t>(min(p.num_pages, int64_t{1} << 31));
   ld.errors = p.errors;
@@ -505,14 +525,14 @@ __device__ void attend_split(const AttnParams& p, WaveState<D>& ws, int b, int h
       if (n < last) ld.next_entries(nx);
       ld.load(B, nx, token(nx), n == last);
       __builtin_amdgcn_sched_barrier(0);
-      compute_loaded<D, FP8>(A, token(n), t_end, g, qop, p.scale_log2, m_run, l_run, acc);
+      compute_loaded<D, FP8, table_per_head(LAYOUT)>(A, token(n), t_end, g, qop, p.scale_log2, m_run, l_run, acc);
       if (n == last) break;
       n = nx;
       nx = min(n + 1, last);
       if (n < last) ld.next_entries(nx);
       ld.load(A, nx, token(nx), n == last);
       __builtin_amdgcn_sched_barrier(0);
-      compute_loaded<D, FP8>(B, token(n), t_end, g, qop, p.scale_log2, m_run, l_run, acc);
+      compute_loaded<D, FP8, table_per_head(LAYOUT)>(B, token(n), t_end, g, qop, p.scale_log2, m_run, l_run, acc);
       if (n == last) break;
       n = nx;
     }
@@ -793,44 +813,47 @@ using KernelFn = void (*)(AttnParams);
 using QueueKernelFn = void (*)(AttnParams, int);
 
 template <int D, bool FP8>
-KernelFn pick_layout(bool paged, int page_size) {
-  if (!paged) return decode_mfma_kernel<D, Layout::kContig, FP8>;
-  return page_size >= 16 ? decode_mfma_kernel<D, Layout::kPaged, FP8> : decode_mfma_kernel<D, Layout::kPagedFine, FP8>;
+KernelFn pick_layout(MfmaPages pages, int page_size) {
+  const bool fine = page_size < 16;
+  if (pages == MfmaPages::kNone) return decode_mfma_kernel<D, Layout::kContig, FP8>;
+  if (pages == MfmaPages::kHeads)
+    return fine ? decode_mfma_kernel<D, Layout::kHeadsFine, FP8> : decode_mfma_kernel<D, Layout::kHeads, FP8>;
+  return fine ? decode_mfma_kernel<D, Layout::kPagedFine, FP8> : decode_mfma_kernel<D, Layout::kPaged, FP8>;
 }
 
 template <int D, bool FP8>
-QueueKernelFn pick_queue_layout(bool paged, int page_size) {
-  if (!paged) return decode_mfma_queue_kernel<D, Layout::kContig, FP8>;
-  return page_size >= 16 ? decode_mfma_queue_kernel<D, Layout::kPaged, FP8>
-                         : decode_mfma_queue_kernel<D, Layout::kPagedFine, FP8>;
+QueueKernelFn pick_queue_layout(MfmaPages pages, int page_size) {
+  const bool fine = page_size < 16;
+  if (pages == MfmaPages::kNone) return decode_mfma_queue_kernel<D, Layout::kContig, FP8>;
+  if (pages == MfmaPages::kHeads)
+    return fine ? decode_mfma_queue_kernel<D, Layout::kHeadsFine, FP8> : decode_mfma_queue_kernel<D, Layout::kHeads, FP8>;
+  return fine ? decode_mfma_queue_kernel<D, Layout::kPagedFine, FP8> : decode_mfma_queue_kernel<D, Layout::kPaged, FP8>;
 }
 
 template <int D, bool FP8>
-QueueKernelFn pick_balanced_layout(bool paged, int page_size) {
-  if (!paged) return decode_mfma_balanced_kernel<D, Layout::kContig, FP8>;
-  return page_size >= 16 ? decode_mfma_balanced_kernel<D, Layout::kPaged, FP8>
-                         : decode_mfma_balanced_kernel<D, Layout::kPagedFine, FP8>;
+QueueKernelFn pick_balanced_layout(MfmaPages pages, int page_size) {
+  const bool fine = page_size < 16;
+  if (pages == MfmaPages::kNone) return decode_mfma_balanced_kernel<D, Layout::kContig, FP8>;
+  if (pages == MfmaPages::kHeads)
+    return fine ? decode_mfma_balanced_kernel<D, Layout::kHeadsFine, FP8> : decode_mfma_balanced_kernel<D, Layout::kHeads, FP8>;
+  return fine ? decode_mfma_balanced_kernel<D, Layout::kPagedFine, FP8> : decode_mfma_balanced_kernel<D, Layout::kPaged, FP8>;
 }
 
-KernelFn select_mfma_kernel(int head_dim, bool paged, int page_size, bool fp8) {
-  if (head_dim == 128) return fp8 ? pick_layout<128, true>(paged, page_size) : pick_layout<128, false>(paged, page_size);
-  if (head_dim == 64) return fp8 ? pick_layout<64, true>(paged, page_size) : pick_layout<64, false>(paged, page_size);
+KernelFn select_mfma_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8) {
+  if (head_dim == 128) return fp8 ? pick_layout<128, true>(pages, page_size) : pick_layout<128, false>(pages, page_size);
+  if (head_dim == 64) return fp8 ? pick_layout<64, true>(pages, page_size) : pick_layout<64, false>(pages, page_size);
   return nullptr;
 }
 
-QueueKernelFn select_mfma_queue_kernel(int head_dim, bool paged, int page_size, bool fp8) {
-  if (head_dim == 128)
-    return fp8 ? pick_queue_layout<128, true>(paged, page_size) : pick_queue_layout<128, false>(paged, page_size);
-  if (head_dim == 64)
-    return fp8 ? pick_queue_layout<64, true>(paged, page_size) : pick_queue_layout<64, false>(paged, page_size);
+QueueKernelFn select_mfma_queue_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8) {
+  if (head_dim == 128) return fp8 ? pick_queue_layout<128, true>(pages, page_size) : pick_queue_layout<128, false>(pages, page_size);
+  if (head_dim == 64) return fp8 ? pick_queue_layout<64, true>(pages, page_size) : pick_queue_layout<64, false>(pages, page_size);
   return nullptr;
 }
 
-QueueKernelFn select_mfma_balanced_kernel(int head_dim, bool paged, int page_size, bool fp8) {
-  if (head_dim == 128)
-    return fp8 ? pick_balanced_layout<128, true>(paged, page_size) : pick_balanced_layout<128, false>(paged, page_size);
-  if (head_dim == 64)
-    return fp8 ? pick_balanced_layout<64, true>(paged, page_size) : pick_balanced_layout<64, false>(paged, page_size);
+QueueKernelFn select_mfma_balanced_kernel(int head_dim, MfmaPages pages, int page_size, bool fp8) {
+  if (head_dim == 128) return fp8 ? pick_balanced_layout<128, true>(pages, page_size) : pick_balanced_layout<128, false>(pages, page_size);
+  if (head_dim == 64) return fp8 ? pick_balanced_layout<64, true>(pages, page_size) : pick_balanced_layout<64, false>(pages, page_size);
   return nullptr;
 }
 

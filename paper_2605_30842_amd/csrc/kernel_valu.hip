@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void decode_valu_kernel(const AttnParams 
   }
   const char* kb = p.k + hk * p.stride_head;
   const char* vb = p.v + hk * p.stride_head;
-  const int32_t* bt_row = PAGED ? table_row(p, b, hk) : nullptr;
+  const int32_t* bt_row = PAGED ? table_row(p, b, hk, p.head_tables) : nullptr;
 
   float m[G], l[G], acc[G][VEC];
 #pragma unroll

@@ -257,10 +257,19 @@ def test_attention_over_blocks(dtype, hkv, group, d, page):
     check(out.cpu().numpy(), lse.cpu().numpy(), np.stack([w[0] for w in want]), np.stack([w[1] for w in want]), dtype)
 
 
+def near_decode(got, want, v, exact):
+    """The decode call's results: its bits where both take the weights in float32; else within what its weights are off by
+    (two bf16 parts, 2^-17 of a weight, so 2^-17 of the largest value; as much again for the float32 sums)."""
+    if exact:
+        assert torch.equal(got, want)
+    else:
+        assert float((got - want).abs().max()) <= 2.0 ** -16 * max(1.0, v)
+
+
 @pytest.mark.parametrize("dtype,variant,chunk", [("bf16", "auto", 0), ("fp8", "auto", 0), ("f32", "auto", 0), ("bf16", "valu", 0),
                                                  ("bf16", "mfma_grid", 0), ("bf16", "mfma", 64)])
 @pytest.mark.parametrize("page", [1, 16])
-def test_one_table_for_all_heads_gives_the_decode_bits(dtype, variant, chunk, page):
+def test_one_table_for_all_heads_is_the_decode_call(dtype, variant, chunk, page):
     """... in every form of the kernels: split, balanced (long calls), queue, vector."""
     g = torch.Generator().manual_seed(7)
     for lens in ([700], [3000, 1, 0, 2500], [4000] * 6 if dtype != "f32" else [400] * 6):
@@ -272,12 +281,33 @@ def test_one_table_for_all_heads_gives_the_decode_bits(dtype, variant, chunk, pa
         table = x["block_table"][:, None].expand(-1, 2, -1).contiguous()
         got, _ = op.block_forward(q, x["k"], x["v"], table, x["ctx_lens"], max(lens), lse=b)
         torch.cuda.synchronize()
-        assert torch.equal(got, want) and torch.equal(a, b), (lens, variant)
+        near_decode(got, want, 5.0, dtype == "f32" or variant == "valu")
+        assert torch.equal(a, b), (lens, variant)
+        again, _ = op.block_forward(q, x["k"], x["v"], table, x["ctx_lens"], max(lens))
+        assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("page", [4, 64])
+def test_the_weights_keep_float32s_precision(dtype, page):
+    """Errors against 64 bits stay below 2^-20 of the outputs' norm: weights in three bf16 parts (2^-26), products exact,
+    float32 sums of at most 128 products in a row (a few 2^-24 of the norm, at random signs), lse likewise."""
+    g = torch.Generator().manual_seed(3)
+    c = Context([4096, 1000], dtype, 2, 128, page, g, both=True)
+    x, op = c.to(DEV), make_op(dtype, 8, 2, 128, 2, 4096)
+    q = torch.randn((2, 8, 128), generator=g).to(query_dtype(dtype))
+    table = x["block_table"][:, None].expand(-1, 2, -1).contiguous()
+    got, _ = op.block_forward(q.to(DEV), x["k"], x["v"], table, x["ctx_lens"], 4096)
+    scale = float(np.float32(1.0 / math.sqrt(128)))
+    for b, n in enumerate([4096, 1000]):
+        want, _ = attended(c, b, q[b], [c.table[b, :-(-n // page)]] * 2, n, scale)
+        off = np.linalg.norm(got[b].cpu().double().numpy() - want) / np.linalg.norm(want)
+        assert off <= 2.0 ** -20, off
 
 
 def test_heads_tables_are_their_own():
-    """A head's result is that of a decode call with its table, whatever the other heads' say; bad entries read page 0 and
-    are reported."""
+    """A head's result is that of a call with its table for all heads, whatever the other heads' say; bad entries read
+    page 0 and are reported."""
     g = torch.Generator().manual_seed(8)
     c = Context([640, 500], "bf16", 4, 64, 16, g, both=True)
     x, op = c.to(DEV), make_op("bf16", 16, 4, 64, 2, 640, debug_checks=True)
@@ -287,7 +317,7 @@ def test_heads_tables_are_their_own():
     table = torch.stack([torch.stack([c.table[b, torch.randperm(30, generator=g)[:10]] for _ in range(4)]) for b in range(2)])
     got, _ = op.block_forward(q, x["k"], x["v"], table.to(DEV), lens, 160)
     for h in range(4):
-        one, _ = op.forward_paged(q, x["k"], x["v"], table[:, h].contiguous().to(DEV), lens, 160)
+        one, _ = op.block_forward(q, x["k"], x["v"], table[:, h:h + 1].expand(-1, 4, -1).contiguous().to(DEV), lens, 160)
         assert torch.equal(got[:, 4 * h:4 * h + 4], one[:, 4 * h:4 * h + 4]), h
     assert op.device_errors() == 0
     bad = table.clone()
@@ -302,7 +332,7 @@ def test_heads_tables_are_their_own():
 
 
 def test_all_blocks_selected_is_dense_attention():
-    """With a budget for every block the step is the dense one, bit for bit."""
+    """With a budget for every block the step is the dense one."""
     g = torch.Generator().manual_seed(9)
     lens = [1000, 16, 333]
     c = Context(lens, "bf16", 2, 128, 16, g, both=True)
@@ -315,7 +345,7 @@ def test_all_blocks_selected_is_dense_attention():
     assert torch.equal(count, x["ctx_lens"])
     got, _ = op.block_forward(q, x["k"], x["v"], table, count, 1000)
     want, _ = op.forward_paged(q, x["k"], x["v"], x["block_table"], x["ctx_lens"], 1000)
-    assert torch.equal(got, want)
+    near_decode(got, want, 5.0, False)
 
 
 def test_a_needle_is_found():
