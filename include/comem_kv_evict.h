@@ -79,6 +79,11 @@ comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const 
                                       float* weights, int64_t weights_stride, void* workspace,
                                       size_t workspace_bytes, void* hip_stream);
 
+/* *workspace_bytes_out gets the bytes that a keep call for n rows can use (0:
+ * none). */
+comem_status comem_keep_tokens_workspace(const comem_decode_attn_plan* plan, int32_t n, int64_t max_ctx_len,
+                                         size_t* workspace_bytes_out);
+
 /* The tokens of row r = rows[i] (rows NULL: r = i) that stay: of its L =
  * ctx_lens[r] tokens the first `first`, the last `last` and, of those between,
  * the ones with the largest weights, min(L, budget) in all. Of equal weights
@@ -102,13 +107,18 @@ comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const 
  *              (comem_kv_compact leaves such an entry out).
  *   kept       float32 [n, keep_stride] or NULL: the weights of the tokens that
  *              stay, in the places they have after comem_kv_compact.
+ *   workspace  device memory, 256-byte aligned, of any size, or NULL; no
+ *              initialisation, nothing kept between calls. With the bytes that
+ *              comem_keep_tokens_workspace says, long rows are shared by several
+ *              workgroups (three kernels instead of one; the same results).
  * Of the plan only max_ctx_len and the device matter. Outputs may not overlap
- * the inputs. One kernel, no workspace. */
+ * the inputs. */
 comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* weights, int64_t weights_stride,
                                const int32_t* ctx_lens, int32_t num_rows, const int32_t* rows, int32_t n,
                                int64_t max_ctx_len, int32_t budget, const int32_t* budgets, int32_t first,
                                int32_t last, int32_t* keep, int64_t keep_stride, int64_t* keep_start,
-                               int32_t* keep_lens, float* kept, void* hip_stream);
+                               int32_t* keep_lens, float* kept, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
 
 #ifdef __cplusplus
 }

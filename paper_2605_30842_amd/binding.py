@@ -41,7 +41,7 @@ ROPE_EXPORTED = ("comem_rope_append", "comem_rope_append_paged")
 PAGES_EXPORTED = ("comem_kv_pages_workspace", "comem_kv_reserve", "comem_kv_reserve_granted", "comem_kv_fork",
                   "comem_kv_compact", "comem_kv_release")
 EVICT_EXPORTED = ("comem_attn_weights_workspace", "comem_attn_weights", "comem_attn_weights_paged",
-                  "comem_keep_tokens")
+                  "comem_keep_tokens_workspace", "comem_keep_tokens")
 BLOCK_EXPORTED = ("comem_block_bounds", "comem_block_scores", "comem_block_select", "comem_block_attn")
 ROPE_INTERLEAVED = 1
 NOALLOC_SCRATCH_BYTES = 32 << 20  # COMEM_NOALLOC_SCRATCH_BYTES
@@ -220,7 +220,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                        vp]
     lib.comem_attn_weights_paged.argtypes = [vp, vp, vp, vp, vp, i32, vp, i64, i64, i64, i32, i64, vp, i32, vp, i32, i64,
                                              vp, f32, vp, i64, vp, sz, vp]
-    lib.comem_keep_tokens.argtypes = [vp, vp, i64, vp, i32, vp, i32, i64, i32, vp, i32, i32, vp, i64, vp, vp, vp, vp]
+    lib.comem_keep_tokens_workspace.argtypes = [vp, i32, i64, ctypes.POINTER(sz)]
+    lib.comem_keep_tokens.argtypes = [vp, vp, i64, vp, i32, vp, i32, i64, i32, vp, i32, i32, vp, i64, vp, vp, vp, vp, sz,
+                                      vp]
     lib.comem_block_bounds.argtypes = [vp, vp, i64, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, vp, vp]
     lib.comem_block_scores.argtypes = [vp, vp, vp, i32, i64, vp, i32, vp, i32, i64, vp, i64, vp]
     lib.comem_block_select.argtypes = [vp, vp, i64, i32, vp, i32, vp, i32, i64, i32, i32, i32, vp, i32, vp, vp]
@@ -514,11 +516,18 @@ def comem_attn_weights_paged(plan, q, lse, q_start, q_lens, max_q_len, k_pages, 
            "comem_attn_weights_paged")
 
 
+def comem_keep_tokens_workspace(plan, n, max_ctx_len) -> int:
+    nbytes = ctypes.c_size_t()
+    _check(load_library().comem_keep_tokens_workspace(plan, n, max_ctx_len, ctypes.byref(nbytes)),
+           "comem_keep_tokens_workspace")
+    return nbytes.value
+
+
 def comem_keep_tokens(plan, weights, weights_stride, ctx_lens, num_rows, rows, n, max_ctx_len, budget, budgets, first,
-                      last, keep, keep_stride, keep_start, keep_lens, kept, stream) -> None:
+                      last, keep, keep_stride, keep_start, keep_lens, kept, workspace, workspace_bytes, stream) -> None:
     _check(load_library().comem_keep_tokens(plan, weights, weights_stride, ctx_lens, num_rows, rows, n, max_ctx_len,
                                             budget, budgets, first, last, keep, keep_stride, keep_start, keep_lens,
-                                            kept, stream), "comem_keep_tokens")
+                                            kept, workspace, workspace_bytes, stream), "comem_keep_tokens")
 
 
 def comem_block_bounds(plan, k_pages, stride_page, stride_token, stride_head, page_size, num_pages, block_table,
@@ -710,6 +719,8 @@ def _in_private_pool(t) -> bool:
 
 # Shorter contexts hold fewer than two splits' worth of keys: not worth asking for a prefill workspace.
 PREFILL_SPLIT_MIN_CTX = 1024
+# Up to so many tokens a keep call never uses a workspace: not worth asking.
+KEEP_CHUNKS_MIN_CTX = 40960
 
 
 class DecodeAttention:
@@ -1260,14 +1271,19 @@ class DecodeAttention:
                  block_table.data_ptr(), block_table.shape[1], *tail)
         return out
 
+    def keep_tokens_workspace_bytes(self, n: int, max_ctx_len: int) -> int:
+        """Bytes of a workspace that a call for n rows can use (0: none)."""
+        return comem_keep_tokens_workspace(self.plan, n, max_ctx_len)
+
     def keep_tokens(self, weights, ctx_lens, max_ctx_len: int, budget: int, first: int = 0, last: int = 0, rows=None,
-                    budgets=None, keep=None, kept=None, stream=None):
+                    budgets=None, keep=None, kept=None, stream=None, workspace=None):
         """The tokens that stay when contexts are cut to `budget`: the first, the last and the most attended ones.
 
         weights float32 [R, >= max_ctx_len] and ctx_lens int32 [R] are those of all rows; rows (int32 [n]) names the ones
         to cut (None: all), budgets (int32 [n]) budgets of their own. Returns keep [n, budget], keep_start, keep_lens and
         kept [n, budget], the weights of the kept tokens. KVPages.compact takes
-        (rows, keep.view(-1), keep_start, keep_lens).
+        (rows, keep.view(-1), keep_start, keep_lens). workspace: as in prefill (keep_tokens_workspace_bytes says how much
+        can be used).
         """
         import torch
 
@@ -1297,11 +1313,15 @@ class DecodeAttention:
         elif not _fits(kept, tensor, (torch.float32,), self._torch_device, (n, width)):
             self._dense("kept", kept, torch.float32, (n, width))
         start, lens = _empty_on(stream, ctx_lens, (n,), dtype=torch.int64), _empty_on(stream, ctx_lens, (n,))
+        ws = workspace
+        if ws is not None or max_ctx_len > KEEP_CHUNKS_MIN_CTX:
+            ws = self._scratch(lambda: self.keep_tokens_workspace_bytes(n, int(max_ctx_len)), stream, workspace)
         _call_on(self, stream, comem_keep_tokens, self.plan, weights.data_ptr(),
                  weights.stride(0) if total > 1 else weights.shape[1], ctx_lens.data_ptr(), total,
                  None if rows is None else rows.data_ptr(), n, int(max_ctx_len), width,
                  None if budgets is None else budgets.data_ptr(), int(first), int(last), keep.data_ptr(), width,
-                 start.data_ptr(), lens.data_ptr(), kept.data_ptr())
+                 start.data_ptr(), lens.data_ptr(), kept.data_ptr(), None if ws is None else ws.data_ptr(),
+                 0 if ws is None else ws.nbytes)
         return keep, start, lens, kept
 
     # Attention over chosen blocks (pages) of a paged cache.

@@ -150,6 +150,23 @@ comem_status launch_weights(const comem_decode_attn_plan& p, comem::WeightsParam
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }
 
+// Rows of a keep call in chunks (comem_keep_tokens_workspace), or 0. us, a
+// quarter kept, one workgroup a row / chunks: one row of 40000 entries 19 / 17,
+// of 65536 27 / 18, of 262144 84 / 24; 32 rows of 131072 49 / 29, of 262144
+// 88 / 64, of 524288 168 / 156; 128 of 65536 36 / 48. Every chunk adds up the
+// counts of all of its row's, so many chunks of many rows lose; up to 40960
+// entries an eager call's host time (three launches 19, one 11) would show.
+int64_t keep_chunks(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {
+  const int64_t chunks = ceil_div(max_ctx, comem::kChunkEntries);
+  const bool few = 4 * n <= p.num_cus && n * chunks <= 4 * p.num_cus;
+  return max_ctx > 40960 && chunks <= comem::kMostChunks && few ? chunks : 0;
+}
+
+size_t keep_bytes(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {
+  const int64_t chunks = keep_chunks(p, n, max_ctx);
+  return chunks > 0 ? static_cast<size_t>(n * comem::choose_item_bytes(chunks)) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -214,11 +231,24 @@ comem_status comem_attn_weights_paged(const comem_decode_attn_plan* plan, const 
   return launch_weights(*p, a, true, batch, workspace, workspace_bytes, hip_stream);
 }
 
+comem_status comem_keep_tokens_workspace(const comem_decode_attn_plan* plan, int32_t n, int64_t max_ctx_len,
+                                         size_t* workspace_bytes_out) {
+  const comem_decode_attn_plan* p = checked(plan);
+  if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
+  if (workspace_bytes_out == nullptr) return COMEM_ERR_NULL_POINTER;
+  *workspace_bytes_out = 0;
+  if (n < 0 || n > kGridYZLimit) return COMEM_ERR_INVALID_SHAPE;
+  if (max_ctx_len < 0 || max_ctx_len > p->cfg.max_ctx_len) return COMEM_ERR_INVALID_SHAPE;
+  *workspace_bytes_out = keep_bytes(*p, n, max_ctx_len);
+  return COMEM_OK;
+}
+
 comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* weights, int64_t weights_stride,
                                const int32_t* ctx_lens, int32_t num_rows, const int32_t* rows, int32_t n,
                                int64_t max_ctx_len, int32_t budget, const int32_t* budgets, int32_t first,
                                int32_t last, int32_t* keep, int64_t keep_stride, int64_t* keep_start,
-                               int32_t* keep_lens, float* kept, void* hip_stream) {
+                               int32_t* keep_lens, float* kept, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
   const comem_decode_attn_plan* p = checked(plan);
   if (p == nullptr) return COMEM_ERR_BAD_HANDLE;
   if (num_rows < 1 || num_rows > kGridYZLimit || n < 0 || n > num_rows) return COMEM_ERR_INVALID_SHAPE;
@@ -231,7 +261,8 @@ comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* 
       keep_lens == nullptr)
     return COMEM_ERR_NULL_POINTER;
   if (!aligned(weights, 4) || !aligned(ctx_lens, 4) || !aligned(rows, 4) || !aligned(budgets, 4) ||
-      !aligned(keep, 4) || !aligned(keep_start, 8) || !aligned(keep_lens, 4) || !aligned(kept, 4))
+      !aligned(keep, 4) || !aligned(keep_start, 8) || !aligned(keep_lens, 4) || !aligned(kept, 4) ||
+      !aligned(workspace, 256))
     return COMEM_ERR_MISALIGNED;
   if (p->device == COMEM_NO_DEVICE) return COMEM_ERR_NO_DEVICE;
   comem::ChooseParams a;
@@ -251,12 +282,25 @@ comem_status comem_keep_tokens(const comem_decode_attn_plan* plan, const float* 
   a.out_start = keep_start;
   a.out_lens = keep_lens;
   a.kept = kept;
-  const comem::ChooseForm form = comem::select_choose_kernel(false, max_ctx_len, n, p->num_cus);
   void* argv[] = {&a};
-  const hipError_t err =
-      hipLaunchKernel(reinterpret_cast<const void*>(form.fn), dim3(static_cast<unsigned>(n), static_cast<unsigned>(form.parts)),
-                      dim3(static_cast<unsigned>(form.threads)), argv, 0, static_cast<hipStream_t>(hip_stream));
-  return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
+  auto launched = [&](comem::ChooseKernelFn fn, int64_t parts, int threads) {
+    return hipLaunchKernel(reinterpret_cast<const void*>(fn),
+                           dim3(static_cast<unsigned>(n), static_cast<unsigned>(parts)),
+                           dim3(static_cast<unsigned>(threads)), argv, 0,
+                           static_cast<hipStream_t>(hip_stream)) == hipSuccess;
+  };
+  const int64_t chunks = keep_chunks(*p, n, max_ctx_len);
+  bool ok;
+  if (chunks > 0 && workspace != nullptr && workspace_bytes >= keep_bytes(*p, n, max_ctx_len)) {
+    a.workspace = static_cast<char*>(workspace);
+    const comem::ChunkKernels k = comem::select_chunk_kernels();
+    ok = launched(k.count, chunks, k.threads) && launched(k.list, chunks, k.threads) &&
+         launched(k.put, chunks, k.threads);
+  } else {
+    const comem::ChooseForm form = comem::select_choose_kernel(false, max_ctx_len, n, p->num_cus);
+    ok = launched(form.fn, form.parts, form.threads);
+  }
+  return ok ? COMEM_OK : COMEM_ERR_HIP;
 }
 
 }  // extern "C"

@@ -77,7 +77,17 @@ struct ChooseParams {
   int32_t max_pages;
   int32_t heads;               // items of a sequence
   int32_t page_shift;
+  char* workspace;             // choose_item_bytes for each item of long rows in chunks
 };
+
+// Rows in chunks.
+constexpr int kMostChunks = 64, kChunkEntries = 8192;
+
+// Workspace of an item: 2048 counts a chunk; a header of 4 words; two counts and
+// a list for each chunk.
+__host__ __device__ inline int64_t choose_item_bytes(int64_t chunks) {
+  return (4 * (2048 * chunks + 4 + 2 * chunks + kChunkEntries * chunks) + 255) / 256 * 256;
+}
 
 using ChooseKernelFn = void (*)(ChooseParams);
 struct ChooseForm {
@@ -87,5 +97,12 @@ struct ChooseForm {
 };
 // For `items` rows of at most `most` entries on `cus` compute units.
 ChooseForm select_choose_kernel(bool blocks, int64_t most, int64_t items, int cus);
+
+// Tokens of long rows, one launch after the other, grid (items, chunks).
+struct ChunkKernels {
+  ChooseKernelFn count, list, put;
+  int threads;
+};
+ChunkKernels select_chunk_kernels();
 
 }  // namespace comem

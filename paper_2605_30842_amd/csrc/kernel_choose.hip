@@ -20,6 +20,7 @@ namespace comem {
 namespace {
 
 typedef int s32x4 __attribute__((ext_vector_type(4)));
+typedef int s32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t kForced = 0xffffffffu, kNaN = 0xfffffffeu;
 
@@ -287,24 +288,20 @@ __device__ inline void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// A row as the kernels for long rows read it. Between `begin` and `end` it is
+// chosen; what lies outside, and in the row, stays.
 template <bool BLOCKS>
-__global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams p) {
-  __shared__ s32x4 hist[kBins];  // the copies of a bin side by side
-  __shared__ float list[kWavesWide][kListed];
-  __shared__ int wave_total[kWavesWide], wave_equal[kWavesWide];
-  __shared__ int result[3], too_long;
-  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6);
-  const int part = blockIdx.y, parts = gridDim.y;
-  const Item<BLOCKS> item(p, blockIdx.x, tid == 0 && part == 0);
-  if (item.count <= 0) return;
-  if (item.count == item.n) {
-    for (int i = part * kThreadsWide + tid; i < item.n; i += parts * kThreadsWide) item.put(i, i);
-    return;
-  }
-  const int begin = min(item.first, item.n), end = max(item.n - item.last, begin);  // between them it is chosen
-  const int turns = (item.n + kTurn * kThreadsWide - 1) / (kTurn * kThreadsWide);
-  const int run = w * turns * kTurn * 64;  // the wave's first entry
-  auto ask = [&](int at, float (&x)[kTurn]) {
+struct Row {
+  const Item<BLOCKS>& item;
+  int begin, end, lane;
+  __device__ Row(const Item<BLOCKS>& it, int l)
+      : item(it), begin(min(it.first, it.n)), end(max(it.n - it.last, begin)), lane(l) {}
+  __device__ int missing() const { return item.count - begin - (item.n - end); }  // entries to choose
+  __device__ bool chosen(int i) const { return i >= begin && i < end; }
+  __device__ bool forced(int i) const { return i < begin || (i >= end && i < item.n); }
+  __device__ uint32_t key(int i, float x) const { return forced(i) ? kForced : chosen(i) ? key_of(x) : 0; }
+
+  __device__ void ask(int at, float (&x)[kTurn]) const {
     if (at + 64 * kTurn <= item.n) {
       const float* from = item.scores + at + lane;
 #pragma unroll
@@ -313,11 +310,23 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
 #pragma unroll
       for (int e = 0; e < kTurn; ++e) x[e] = item.score_at(at + 64 * e + lane);
     }
-  };
-  // f(first entry of the turn, its scores, what kind it is); `next` holds turn
-  // `from`'s scores, and at the end those of turn `after`.
-  float next[kTurn];
-  auto for_turns = [&](int from, int to, int after, auto&& f) {
+  }
+  __device__ Turn kind(int at, const float (&x)[kTurn]) const {
+    const int to = at + 64 * kTurn;
+    if (at >= item.n) return Turn::kEmpty;
+    if (to > item.n) return Turn::kMixed;
+    if (at >= end || to <= begin) return Turn::kForced;
+    if (at < begin || to > end) return Turn::kMixed;
+#pragma unroll
+    for (int e = 0; e < kTurn; e += 2)
+      if (__builtin_amdgcn_ballot_w64(__builtin_isunordered(x[e], x[e + 1])) != 0) return Turn::kMixed;
+    return Turn::kPlain;
+  }
+  // f(first entry of the turn, its scores, its kind) for the turns from .. to - 1
+  // of the run that starts at entry `run`. `next` holds turn `from`'s scores, and
+  // at the end those of turn `after`.
+  template <typename F>
+  __device__ void for_turns(int run, int from, int to, int after, float (&next)[kTurn], F&& f) const {
     float x[kTurn];
 #pragma unroll 1
     for (int j = from; j < to; ++j) {
@@ -325,147 +334,219 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
 #pragma unroll
       for (int e = 0; e < kTurn; ++e) x[e] = next[e];
       ask(run + 64 * kTurn * (j + 1 < to ? j + 1 : after), next);
-      Turn kind = at >= end || at + 64 * kTurn <= begin ? Turn::kForced : at >= begin && at + 64 * kTurn <= end ? Turn::kPlain : Turn::kMixed;
-      if (at + 64 * kTurn > item.n) kind = at >= item.n ? Turn::kEmpty : Turn::kMixed;
-      if (kind == Turn::kPlain) {
-#pragma unroll
-        for (int e = 0; e < kTurn; e += 2)
-          if (__builtin_amdgcn_ballot_w64(__builtin_isunordered(x[e], x[e + 1])) != 0) kind = Turn::kMixed;
-      }
-      f(at, x, kind);
+      f(at, x, kind(at, x));
     }
-  };
-  auto chosen = [&](int i) { return i >= begin && i < end; };      // not: it stays, or is past the row
-  auto forced = [&](int i) { return i < begin || (i >= end && i < item.n); };
-  auto add = [&](int bin) { atomicAdd(reinterpret_cast<int*>(&hist[bin]) + (lane & (kCopies - 1)), 1); };
+  }
 
+  // Counts a turn's first digits, by the bits as they are; -0 as 0, NaN as one of them.
+  template <typename Add>
+  __device__ void count(int at, const float (&x)[kTurn], Turn kind, Add&& add) const {
+    if (kind == Turn::kForced || kind == Turn::kEmpty) return;
+    const bool plain = kind == Turn::kPlain;
+#pragma unroll
+    for (int e = 0; e < kTurn; ++e) {
+      uint32_t u = __float_as_uint(x[e] + 0.f);
+      if (!plain) u = x[e] == x[e] ? u : 0x7fffffffu;
+      if (plain || chosen(at + 64 * e + lane)) add(static_cast<int>(u >> 21));
+    }
+  }
+  // Adds a turn's entries above digit `top` to `above`, and lists those that have it.
+  template <typename Store>
+  __device__ void list(int at, const float (&x)[kTurn], Turn kind, uint32_t top, float least, float over, int& above,
+                       int& listed, Store&& store) const {
+    if (kind == Turn::kForced) above += 64 * kTurn;
+    if (kind == Turn::kForced || kind == Turn::kEmpty) return;
+    const bool plain = kind == Turn::kPlain;
+#pragma unroll
+    for (int e = 0; e < kTurn; ++e) {
+      uint64_t more, same;
+      if (plain) {
+        more = __builtin_amdgcn_ballot_w64(x[e] >= over);
+        same = __builtin_amdgcn_ballot_w64(x[e] >= least) & ~more;
+      } else {
+        const int i = at + 64 * e + lane;
+        const uint32_t digit = key_of(x[e]) >> 21;
+        more = __builtin_amdgcn_ballot_w64(forced(i) || (chosen(i) && digit > top));
+        same = __builtin_amdgcn_ballot_w64(chosen(i) && digit == top);
+      }
+      above += __builtin_popcountll(more);
+      if (same != 0) {
+        if (((same >> lane) & 1) != 0) store(listed + lanes_before(same), x[e]);
+        listed += __builtin_popcountll(same);
+      }
+    }
+  }
+  // Puts a turn's entries that stay.
+  __device__ void put(int at, const float (&x)[kTurn], Turn kind, const Limit& limit, float least, float tie,
+                      Places& places) const {
+    if (kind == Turn::kEmpty) return;
+    const bool plain = kind == Turn::kPlain;
+#pragma unroll
+    for (int e = 0; e < kTurn; ++e) {
+      const int i = at + 64 * e + lane;
+      bool stays = x[e] >= least, equals = x[e] == tie;
+      if (!plain) {
+        const uint32_t k = key(i, x[e]);
+        stays = k >= limit.least;
+        equals = limit.ties > 0 && k == limit.tie;
+      }
+      const int to = places.next(stays, equals, limit.ties);
+      if (to >= 0) item.put(to, i, x[e]);
+    }
+  }
+};
+
+// Where the first digit's counts lie: digits in the order of the scores, bins by
+// their bits.
+__device__ inline int first_bin(int digit) { return digit >= kBins / 2 ? digit - kBins / 2 : kBins - 1 - digit; }
+
+// The limit as the digits are found.
+struct Search {
+  uint32_t found = 0;  // the digits found so far
+  int need;            // entries still missing among the keys that begin with them
+  bool all;            // all of those stay
+  __device__ explicit Search(int missing) : need(missing), all(missing <= 0) {}
+  // One more digit: it holds the need-th entry from the top, `above` lie above it, `size` have it.
+  __device__ void add(int digit, int above, int size, int shift) {
+    if (all) {
+      found = ~0u;  // only what always stays
+      return;
+    }
+    found |= static_cast<uint32_t>(digit) << shift;
+    need -= above;
+    all = need == size;
+  }
+  __device__ Limit limit() const { return limit_of(found, need, all); }
+  __device__ float tie() const { return all ? __builtin_nanf("") : score_of(found); }
+};
+
+// What a workgroup of 16 waves finds with.
+struct Found {
+  int wave_total[kWavesWide];
+  int result[3];
+};
+// Adds the digit that holds the need-th entry from the top: thread tid has the
+// counts v of the digits kBins - 1 - 2 tid and the one below. The barriers of
+// two calls have one between them.
+__device__ inline void find_digit(Search& search, int shift, const int (&v)[2], Found& f, int tid, int lane, int w) {
+  const int upto = upto_lane(v[0] + v[1]);
+  if (lane == 63) f.wave_total[w] = upto;
+  if (tid == 0) f.result[0] = f.result[1] = f.result[2] = 0;
+  lds_barrier();
+  int before = upto - v[0] - v[1] + waves_before(f.wave_total, w, lane);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (before < search.need && search.need <= before + v[e]) {
+      f.result[0] = kBins - 1 - 2 * tid - e;
+      f.result[1] = before;
+      f.result[2] = v[e];
+    }
+    before += v[e];
+  }
+  lds_barrier();
+  search.add(uniform_i32(f.result[0]), uniform_i32(f.result[1]), uniform_i32(f.result[2]), shift);
+}
+
+// The histogram: the copies of a bin side by side.
+__device__ inline void count_one(s32x4* hist, int bin, int lane) {
+  atomicAdd(reinterpret_cast<int*>(&hist[bin]) + (lane & (kCopies - 1)), 1);
+}
+__device__ inline int taken(s32x4* bin) {
+  const s32x4 x = *bin;
+  *bin = s32x4{0, 0, 0, 0};
+  return x[0] + x[1] + x[2] + x[3];
+}
+
+template <bool BLOCKS>
+__global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams p) {
+  __shared__ s32x4 hist[kBins];
+  __shared__ float list[kWavesWide][kListed];
+  __shared__ Found found;
+  __shared__ int wave_above[kWavesWide], wave_equal[kWavesWide];
+  __shared__ int too_long;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6);
+  const int part = blockIdx.y, parts = gridDim.y;
+  const Item<BLOCKS> item(p, blockIdx.x, tid == 0 && part == 0);
+  if (item.count <= 0) return;
+  if (item.count == item.n) {
+    for (int i = part * kThreadsWide + tid; i < item.n; i += parts * kThreadsWide) item.put(i, i);
+    return;
+  }
+  const Row<BLOCKS> row(item, lane);
+  const int turns = (item.n + kTurn * kThreadsWide - 1) / (kTurn * kThreadsWide);
+  const int run = w * turns * kTurn * 64;  // the wave's first entry
+  auto add = [&](int bin) { count_one(hist, bin, lane); };
+
+  float next[kTurn];
+  row.ask(run, next);
 #pragma unroll
   for (int i = 0; i < kBins; i += kThreadsWide) hist[i + tid] = s32x4{0, 0, 0, 0};
   if (tid == 0) too_long = 0;
-  ask(run, next);
   lds_barrier();
-  uint32_t found = 0;                                              // the key's digits found so far
-  int need = item.count - begin - (item.n - end);                  // entries still missing among those that have them
-  bool all = need <= 0, overflow = false;                          // all of those stay
+  Search search(row.missing());
+  bool overflow = false;
   int above = 0, listed = 0, own_above = 0, own_listed = 0;
   const int part_begin = turns * part / parts, part_end = turns * (part + 1) / parts;
 #pragma unroll 1
   for (int shift = 21;;) {
     const int bits = shift == 0 ? 10 : 11;
     const uint32_t low = (1u << bits) - 1;
+    auto add_key = [&](uint32_t k) {
+      if ((k ^ search.found) >> (shift + bits) == 0) add(static_cast<int>((k >> shift) & low));
+    };
     if (shift == 21) {
-      // By the bits as they are; -0 as 0, NaN as one of them.
-      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn kind) {
-        if (kind == Turn::kForced || kind == Turn::kEmpty) return;
-        const bool plain = kind == Turn::kPlain;
-#pragma unroll
-        for (int e = 0; e < kTurn; ++e) {
-          uint32_t u = __float_as_uint(x[e] + 0.f);
-          if (!plain) u = x[e] == x[e] ? u : 0x7fffffffu;
-          if (plain || chosen(at + 64 * e + lane)) add(static_cast<int>(u >> 21));
-        }
-      });
+      row.for_turns(run, 0, turns, 0, next,
+                    [&](int at, const float (&x)[kTurn], Turn kind) { row.count(at, x, kind, add); });
     } else if (overflow) {
-      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn) {
+      row.for_turns(run, 0, turns, 0, next, [&](int at, const float (&x)[kTurn], Turn) {
 #pragma unroll
-        for (int e = 0; e < kTurn; ++e) {
-          const uint32_t k = key_of(x[e]);
-          if (chosen(at + 64 * e + lane) && (k ^ found) >> (shift + bits) == 0) add(static_cast<int>((k >> shift) & low));
-        }
+        for (int e = 0; e < kTurn; ++e)
+          if (row.chosen(at + 64 * e + lane)) add_key(key_of(x[e]));
       });
     } else {
 #pragma unroll 1
-      for (int i = lane; i < listed; i += 64) {
-        const uint32_t k = key_of(list[w][i]);
-        if ((k ^ found) >> (shift + bits) == 0) add(static_cast<int>((k >> shift) & low));
-      }
+      for (int i = lane; i < listed; i += 64) add_key(key_of(list[w][i]));
     }
     lds_barrier();
-    // A thread's two digits from the top down, and the entries of those before.
-    int v[2], total = 0;
+    int v[2];  // of a thread's two digits, from the top down
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int digit = kBins - 1 - 2 * tid - e;
-      s32x4* bin = &hist[shift != 21 ? digit : digit >= kBins / 2 ? digit - kBins / 2 : kBins - 1 - digit];
-      const s32x4 x = *bin;
-      *bin = s32x4{0, 0, 0, 0};
-      v[e] = x[0] + x[1] + x[2] + x[3];
-      total += v[e];
+      v[e] = taken(&hist[shift != 21 ? digit : first_bin(digit)]);
     }
-    const int upto = upto_lane(total);
-    if (lane == 63) wave_total[w] = upto;
-    if (tid == 0) result[0] = result[1] = result[2] = 0;
-    lds_barrier();
-    int before = upto - total + waves_before(wave_total, w, lane);
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      if (before < need && need <= before + v[e]) {
-        result[0] = kBins - 1 - 2 * tid - e;
-        result[1] = before;
-        result[2] = v[e];
-      }
-      before += v[e];
-    }
-    lds_barrier();
-    if (!all) {
-      found |= static_cast<uint32_t>(uniform_i32(result[0])) << shift;
-      need -= uniform_i32(result[1]);
-      all = need == uniform_i32(result[2]);
-    } else {
-      found = ~0u;  // only what always stays
-    }
+    find_digit(search, shift, v, found, tid, lane, w);
     if (shift == 21) {
-      const uint32_t top = found >> 21;
+      const uint32_t top = search.found >> 21;
       const float least = score_of(top << 21), over = top == kBins - 1 ? __builtin_nanf("") : score_of((top + 1) << 21);
-      for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn kind) {
+      row.for_turns(run, 0, turns, 0, next, [&](int at, const float (&x)[kTurn], Turn kind) {
         if (at == run + 64 * kTurn * part_begin) {
           own_above = above;
           own_listed = listed;
         }
-        if (kind == Turn::kForced) above += 64 * kTurn;
-        if (kind == Turn::kForced || kind == Turn::kEmpty) return;
-        const bool plain = kind == Turn::kPlain;
-#pragma unroll
-        for (int e = 0; e < kTurn; ++e) {
-          uint64_t more, same;
-          if (plain) {
-            more = __builtin_amdgcn_ballot_w64(x[e] >= over);
-            same = __builtin_amdgcn_ballot_w64(x[e] >= least) & ~more;
-          } else {
-            const int i = at + 64 * e + lane;
-            const uint32_t k = key_of(x[e]) >> 21;
-            more = __builtin_amdgcn_ballot_w64(forced(i) || (chosen(i) && k > top));
-            same = __builtin_amdgcn_ballot_w64(chosen(i) && k == top);
-          }
-          above += __builtin_popcountll(more);
-          if (same != 0) {
-            const int place = listed + lanes_before(same);
-            if (((same >> lane) & 1) != 0 && place < kListed) list[w][place] = x[e];
-            listed += __builtin_popcountll(same);
-          }
-        }
+        row.list(at, x, kind, top, least, over, above, listed, [&](int place, float score) {
+          if (place < kListed) list[w][place] = score;
+        });
       });
       if (listed > kListed) too_long = 1;
       lds_barrier();
       overflow = uniform_i32(too_long) != 0;
     }
-    if (all || shift == 0) break;
+    if (search.all || shift == 0) break;
     shift = shift == 21 ? 10 : 0;
   }
-  const Limit limit = limit_of(found, need, all);
-  const float least = score_of(limit.least), tie = all ? __builtin_nanf("") : score_of(limit.tie);
+  const Limit limit = search.limit();
+  const float least = score_of(limit.least), tie = search.tie();
 
-  // What each run, and this workgroup's part of it, holds of the entries that stay.
+  // What each run, and this workgroup's part of it, holds of what stays.
   Places own;
   int equal = 0;
   if (overflow) {
     above = 0;
-    for_turns(0, turns, 0, [&](int at, const float (&x)[kTurn], Turn) {
+    row.for_turns(run, 0, turns, 0, next, [&](int at, const float (&x)[kTurn], Turn) {
       if (at == run + 64 * kTurn * part_begin) own = {above, equal};
 #pragma unroll
       for (int e = 0; e < kTurn; ++e) {
-        const int i = at + 64 * e + lane;
-        const uint32_t k = forced(i) ? kForced : chosen(i) ? key_of(x[e]) : 0;
+        const uint32_t k = row.key(at + 64 * e + lane, x[e]);
         above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= limit.least));
         if (limit.ties > 0) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == limit.tie));
       }
@@ -487,29 +568,206 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
     }
   }
   if (lane == 0) {
-    wave_total[w] = above;
+    wave_above[w] = above;
     wave_equal[w] = equal;
   }
   lds_barrier();
-  own.above += waves_before(wave_total, w, lane);
+  own.above += waves_before(wave_above, w, lane);
   if (limit.ties > 0) own.equal += waves_before(wave_equal, w, lane);
-  if (part_begin != 0) ask(run + 64 * kTurn * part_begin, next);
-  for_turns(part_begin, part_end, part_begin, [&](int at, const float (&x)[kTurn], Turn kind) {
-    if (kind == Turn::kEmpty) return;
-    const bool plain = kind == Turn::kPlain;
+  if (part_begin != 0) row.ask(run + 64 * kTurn * part_begin, next);
+  row.for_turns(run, part_begin, part_end, part_begin, next, [&](int at, const float (&x)[kTurn], Turn kind) {
+    row.put(at, x, kind, limit, least, tie, own);
+  });
+}
+
+// The longest rows, with a workspace: the same three readings as three
+// launches, each with a workgroup for every chunk of a row, a turn for each of
+// its waves. The first leaves the chunk's counts; in the second every workgroup
+// adds up those of the row's chunks, finds the digit and lists its chunk's
+// scores that have it; in the third every workgroup goes through the lists for
+// the other digits and for what stays before its chunk, and puts the chunk's.
+// Latency bounds them: 8 rows of 32768-131072, 4.1 MB in and out, 4 + 6 + 7 us,
+// where one workgroup a row takes 42. (A workgroup of 4 waves for a chunk, each
+// wave with four turns and a list of its own, took 31: too few instructions at
+// once in the lists.)
+static_assert(kChunkEntries == kThreadsWide * kTurn);
+
+// An item's part of the workspace.
+struct ChunkSpace {
+  int32_t* counts;  // [chunks][kBins]
+  int32_t* header;  // first digit, entries missing among those that have it, whether all of them stay
+  int32_t* above;   // [chunks]: entries above the digit
+  int32_t* listed;  // [chunks]
+  float* lists;     // [chunks][kChunkEntries]
+  __device__ ChunkSpace(const ChooseParams& p, int item, int chunks)
+      : counts(reinterpret_cast<int32_t*>(p.workspace + item * choose_item_bytes(chunks))),
+        header(counts + chunks * kBins),
+        above(header + 4),
+        listed(above + chunks),
+        lists(reinterpret_cast<float*>(listed + chunks)) {}
+};
+
+__global__ __launch_bounds__(kThreadsWide) void chunk_count_kernel(const ChooseParams p) {
+  __shared__ s32x4 hist[kBins];
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6), chunk = blockIdx.y;
+  const Item<false> item(p, blockIdx.x, tid == 0 && chunk == 0);
+  const int at = chunk * kChunkEntries + w * 64 * kTurn;
+  if (item.count <= 0 || item.count == item.n || chunk * kChunkEntries >= item.n) return;
+  const Row<false> row(item, lane);
+  float x[kTurn];
+  row.ask(at, x);
 #pragma unroll
-    for (int e = 0; e < kTurn; ++e) {
-      const int i = at + 64 * e + lane;
-      bool stays = x[e] >= least, equals = x[e] == tie;
-      if (!plain) {
-        const uint32_t k = forced(i) ? kForced : chosen(i) ? key_of(x[e]) : 0;
-        stays = k >= limit.least;
-        equals = limit.ties > 0 && k == limit.tie;
+  for (int i = 0; i < kBins; i += kThreadsWide) hist[i + tid] = s32x4{0, 0, 0, 0};
+  lds_barrier();
+  row.count(at, x, row.kind(at, x), [&](int bin) { count_one(hist, bin, lane); });
+  lds_barrier();
+  int32_t* counts = ChunkSpace(p, blockIdx.x, gridDim.y).counts + chunk * kBins;
+  *reinterpret_cast<s32x2*>(counts + 2 * tid) = s32x2{taken(&hist[2 * tid]), taken(&hist[2 * tid + 1])};
+}
+
+__global__ __launch_bounds__(kThreadsWide) void chunk_list_kernel(const ChooseParams p) {
+  __shared__ Found found;
+  __shared__ int wave_above[kWavesWide], wave_listed[kWavesWide];
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6), chunk = blockIdx.y;
+  const Item<false> item(p, blockIdx.x, false);
+  const int at = chunk * kChunkEntries + w * 64 * kTurn;
+  if (item.count <= 0 || item.count == item.n || chunk * kChunkEntries >= item.n) return;
+  const Row<false> row(item, lane);
+  float x[kTurn];
+  row.ask(at, x);
+  const ChunkSpace space(p, blockIdx.x, gridDim.y);
+  const int chunks = (item.n + kChunkEntries - 1) / kChunkEntries;
+  // The thread's two digits, side by side, upwards above 0 and downwards below.
+  const int digit = kBins - 1 - 2 * tid;
+  const bool up = digit >= kBins / 2;
+  const int32_t* from = space.counts + (up ? first_bin(digit - 1) : first_bin(digit));
+  s32x2 sum = {0, 0};
+#pragma unroll 8
+  for (int i = 0; i < chunks; ++i) sum += *reinterpret_cast<const s32x2*>(from + i * kBins);
+  const int v[2] = {up ? sum[1] : sum[0], up ? sum[0] : sum[1]};
+  Search search(row.missing());
+  find_digit(search, 21, v, found, tid, lane, w);
+  const uint32_t top = search.found >> 21;
+  const float least = score_of(top << 21), over = top == kBins - 1 ? __builtin_nanf("") : score_of((top + 1) << 21);
+  const Turn kind = row.kind(at, x);
+  int above = 0, listed = 0;
+  row.list(at, x, kind, top, least, over, above, listed, [](int, float) {});
+  if (lane == 0) {
+    wave_above[w] = above;
+    wave_listed[w] = listed;
+  }
+  lds_barrier();
+  if (tid == 0) {
+    if (chunk == 0) {
+      space.header[0] = static_cast<int32_t>(search.found);
+      space.header[1] = search.need;
+      space.header[2] = search.all ? 1 : 0;
+    }
+  }
+  if (w == 0) {
+    const int all_above = waves_before(wave_above, kWavesWide, lane);
+    const int all_listed = waves_before(wave_listed, kWavesWide, lane);
+    if (lane == 0) {
+      space.above[chunk] = all_above;
+      space.listed[chunk] = all_listed;
+    }
+  }
+  listed = waves_before(wave_listed, w, lane);
+  float* list = space.lists + static_cast<int64_t>(chunk) * kChunkEntries;
+  row.list(at, x, kind, top, least, over, above, listed, [&](int place, float score) { list[place] = score; });
+}
+
+__global__ __launch_bounds__(kThreadsWide) void chunk_put_kernel(const ChooseParams p) {
+  __shared__ s32x4 hist[kBins];
+  __shared__ Found found;
+  __shared__ int listed_of[kMostChunks], above_of[kMostChunks], equal_of[kMostChunks];  // what stays, of each chunk
+  __shared__ int wave_above[kWavesWide], wave_equal[kWavesWide];
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform_i32(tid >> 6), chunk = blockIdx.y;
+  const Item<false> item(p, blockIdx.x, false);
+  const int at = chunk * kChunkEntries + w * 64 * kTurn;
+  if (item.count <= 0 || chunk * kChunkEntries >= item.n) return;
+  if (item.count == item.n) {
+    for (int i = chunk * kChunkEntries + tid; i < min(item.n, (chunk + 1) * kChunkEntries); i += kThreadsWide)
+      item.put(i, i);
+    return;
+  }
+  const Row<false> row(item, lane);
+  float x[kTurn];
+  row.ask(at, x);
+  const ChunkSpace space(p, blockIdx.x, gridDim.y);
+  const int chunks = (item.n + kChunkEntries - 1) / kChunkEntries;
+  Search search(0);
+  search.found = static_cast<uint32_t>(uniform_i32(space.header[0]));
+  search.need = uniform_i32(space.header[1]);
+  search.all = uniform_i32(space.header[2]) != 0;
+#pragma unroll
+  for (int i = 0; i < kBins; i += kThreadsWide) hist[i + tid] = s32x4{0, 0, 0, 0};
+  if (tid < chunks) {
+    listed_of[tid] = space.listed[tid];
+    above_of[tid] = space.above[tid];
+    equal_of[tid] = 0;
+  }
+  lds_barrier();
+  // f(chunk, key or 0 past the end): a chunk's list is one wave's.
+  auto for_lists = [&](auto&& f) {
+#pragma unroll 1
+    for (int c = w; c < chunks; c += kWavesWide) {
+      const int n = uniform_i32(listed_of[c]);
+      const float* list = space.lists + static_cast<int64_t>(c) * kChunkEntries;
+#pragma unroll 1
+      for (int i = lane; i - lane < n; i += 256) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = i + 64 * e < n ? list[i + 64 * e] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(c, i + 64 * e < n ? key_of(y[e]) : 0);
       }
-      const int to = own.next(stays, equals, limit.ties);
-      if (to >= 0) item.put(to, i, x[e]);
+    }
+  };
+#pragma unroll 1
+  for (int shift = 10; !search.all; shift = 0) {
+    const int bits = shift == 0 ? 10 : 11;
+    for_lists([&](int, uint32_t k) {
+      if (k != 0 && (k ^ search.found) >> (shift + bits) == 0)
+        count_one(hist, static_cast<int>((k >> shift) & ((1u << bits) - 1)), lane);
+    });
+    lds_barrier();
+    const int v[2] = {taken(&hist[kBins - 1 - 2 * tid]), taken(&hist[kBins - 2 - 2 * tid])};
+    find_digit(search, shift, v, found, tid, lane, w);
+    if (shift == 0) break;
+  }
+  const Limit limit = search.limit();
+  const float least = score_of(limit.least), tie = search.tie();
+  for_lists([&](int c, uint32_t k) {
+    const uint64_t more = __builtin_amdgcn_ballot_w64(k >= limit.least);
+    const uint64_t same = limit.ties > 0 ? __builtin_amdgcn_ballot_w64(k == limit.tie) : 0;
+    if (lane == 0) {
+      above_of[c] += __builtin_popcountll(more);
+      equal_of[c] += __builtin_popcountll(same);
     }
   });
+  // The wave's own turn, and what stays before it in the chunk and in the row.
+  const Turn kind = row.kind(at, x);
+  int above = 0, equal = 0;
+  if (kind != Turn::kEmpty) {
+#pragma unroll
+    for (int e = 0; e < kTurn; ++e) {
+      const uint32_t k = row.key(at + 64 * e + lane, x[e]);
+      above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= limit.least));
+      if (limit.ties > 0) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == limit.tie));
+    }
+  }
+  if (lane == 0) {
+    wave_above[w] = above;
+    wave_equal[w] = equal;
+  }
+  lds_barrier();
+  Places own;
+  own.above = waves_before(wave_above, w, lane) +
+              __builtin_amdgcn_readlane(upto_lane(lane < chunk ? above_of[lane] : 0), 63);
+  own.equal = waves_before(wave_equal, w, lane) +
+              __builtin_amdgcn_readlane(upto_lane(lane < chunk ? equal_of[lane] : 0), 63);
+  row.put(at, x, kind, limit, least, tie, own);
 }
 
 template <bool BLOCKS>
@@ -523,6 +781,10 @@ ChooseForm form(int64_t most, int64_t items, int cus) {
 
 ChooseForm select_choose_kernel(bool blocks, int64_t most, int64_t items, int cus) {
   return blocks ? form<true>(most, items, cus) : form<false>(most, items, cus);
+}
+
+ChunkKernels select_chunk_kernels() {
+  return {chunk_count_kernel, chunk_list_kernel, chunk_put_kernel, kThreadsWide};
 }
 
 }  // namespace comem

@@ -44,7 +44,8 @@ def _paged(plan, **kw):
 
 def _keep(plan, **kw):
     a = dict(weights=A, weights_stride=4096, ctx_lens=A, num_rows=8, rows=A, n=5, max_ctx_len=4096, budget=100,
-             budgets=A, first=10, last=20, keep=A, keep_stride=100, keep_start=A, keep_lens=A, kept=A)
+             budgets=A, first=10, last=20, keep=A, keep_stride=100, keep_start=A, keep_lens=A, kept=A,
+             workspace=None, nbytes=0)
     a.update(kw)
     return B.load_library().comem_keep_tokens(plan, *a.values(), None)
 
@@ -133,9 +134,28 @@ def test_contiguous_refusals(plan):
     (dict(weights=A + 2), B.ERR_MISALIGNED), (dict(ctx_lens=A + 2), B.ERR_MISALIGNED), (dict(rows=A + 2), B.ERR_MISALIGNED),
     (dict(budgets=A + 2), B.ERR_MISALIGNED), (dict(keep=A + 2), B.ERR_MISALIGNED),
     (dict(keep_start=A + 4), B.ERR_MISALIGNED), (dict(keep_lens=A + 2), B.ERR_MISALIGNED),
-    (dict(kept=A + 2), B.ERR_MISALIGNED)], ids=str)
+    (dict(kept=A + 2), B.ERR_MISALIGNED), (dict(workspace=A + 64, nbytes=1 << 20), B.ERR_MISALIGNED)], ids=str)
 def test_keep_refusals(plan, kw, status):
     assert _keep(plan, **kw) == status
+
+
+def test_keep_workspace():
+    """None for rows that one workgroup takes, and for too many rows or chunks; else counts and lists of every entry."""
+    p, _ = B.comem_decode_attn_init(B.Config(num_q_heads=8, num_kv_heads=8, head_dim=64, dtype=B.BF16, scale=0.1,
+                                             max_batch=4, max_ctx_len=1 << 30), B.NO_DEVICE)
+    size = lambda *a: B.comem_keep_tokens_workspace(p, *a)  # noqa: E731
+    assert size(0, 100000) == size(5, 40960) == size(5, 0) == size(5, 1 << 30) == 0
+    assert size(65, 50000) == size(33, 500000) == 0
+    assert size(1, 40961) >= 4 * 40961 and size(3, 131072) == 3 * size(1, 131072) and size(1, 131072) % 256 == 0
+    for a in ((-1, 5), (65536, 5), (1, -1), (1, (1 << 30) + 1)):
+        with pytest.raises(B.ComemError) as e:
+            size(*a)
+        assert e.value.status == B.ERR_INVALID_SHAPE
+    assert B.load_library().comem_keep_tokens_workspace(p, 1, 1, None) == B.ERR_NULL_POINTER
+    assert B.load_library().comem_keep_tokens_workspace(None, 1, 1, None) == B.ERR_BAD_HANDLE
+    for nbytes in (0, 5, 1 << 30):
+        assert _keep(p, max_ctx_len=100000, weights_stride=100000, workspace=A, nbytes=nbytes) == B.ERR_NO_DEVICE
+    B.comem_decode_attn_destroy(p)
 
 
 # ------------------------------------------------------------ the wrapper
@@ -150,7 +170,7 @@ def op(monkeypatch):
     def sentinel(*a, **k):
         raise Reached()
 
-    for name in B.EVICT_EXPORTED[1:]:
+    for name in ("comem_attn_weights", "comem_attn_weights_paged", "comem_keep_tokens"):
         monkeypatch.setattr(B, name, sentinel)
     o = object.__new__(B.DecodeAttention)
     o.plan, _ = B.comem_decode_attn_init(B.Config(num_q_heads=8, num_kv_heads=2, head_dim=64, dtype=B.BF16, scale=0.1,

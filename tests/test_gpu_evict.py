@@ -306,7 +306,7 @@ def test_keep_sizes(part):
         check_keep(w, lens, budget, bound=bound)
 
 
-@pytest.mark.parametrize("n", [32767, 32768, 32769, 65536, 65537, 100001, 150000])
+@pytest.mark.parametrize("n", [32767, 32769, 65536, 65537, 100001, 150000])
 def test_keep_long(n):
     say("keep", n)
     g = torch.Generator().manual_seed(n)
@@ -316,7 +316,59 @@ def test_keep_long(n):
     check_keep(w, [n, n // 2], n - 1)
 
 
-@pytest.mark.parametrize("n", [50, 3000, 40000])
+@pytest.mark.parametrize("n", [40960, 40961, 49152, 49153, 131073, 524288, 524289])
+def test_keep_with_and_without_a_workspace(n):
+    """Long rows in chunks give what one workgroup a row gives: rows that end before, in and at the end of a chunk, one
+    that stays whole, one whose bound it passes, one that is forced throughout."""
+    say("keep", n)
+    g = torch.Generator().manual_seed(n)
+    w = (torch.randn((6, n), generator=g) * 3).exp()
+    w[2] = w[2].round()
+    w[3] = 1.0
+    lens = [n, 8193, n - 1, n - 8192, 100, n]
+    full = 2 * (n // 5)
+    for budget, first, last, budgets in ((n // 3, 5, 70, None), (full, n // 5, n // 5, None),
+                                         (n // 2, 0, 9000, [0, 8200, 9000, 9001, 101, n // 2])):
+        got = keep(w, lens, budget, first, last, budgets=budgets)
+        one = keep(w, lens, budget, first, last, budgets=budgets, workspace=torch.empty(0, device=DEV))
+        for i, count in enumerate(got[2].tolist()):
+            assert count == int(one[2][i]) and torch.equal(got[0][i, :count], one[0][i, :count]), i
+            assert torch.equal(got[3][i, :count], one[3][i, :count]), i
+    check_keep(w, lens, n // 3, 5, 70)
+    check_keep(w, lens, n // 4, n // 4, 0, rows=[5, 5, 1, -1, 6, 0])
+
+
+def test_keep_long_captured_and_on_another_stream():
+    """A graph's workspace is its own: two of them, and eager calls between."""
+    n = 100000
+    g = torch.Generator().manual_seed(5)
+    w = [torch.randn((2, n), generator=g).to(DEV) for _ in range(2)]
+    lens = torch.tensor([n, n - 9000], dtype=torch.int32, device=DEV)
+    op = make_op("f32", 1, 1, 64, 1, n)
+    want = [op.keep_tokens(x, lens, n, 4000, 3, 3) for x in w]
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in w]
+    got = []
+    for graph, x in zip(graphs, w):
+        with torch.cuda.graph(graph):
+            got.append(op.keep_tokens(x, lens, n, 4000, 3, 3))
+    for i in range(3):
+        for graph, out in zip(graphs, got):
+            for t in out:
+                t.fill_(-7)
+            torch.full((1 << 20,), -1, dtype=torch.int32, device=DEV)  # the allocator's free memory
+            graph.replay()
+        op.keep_tokens(w[0], lens, n, 100)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b)), i
+    stream = torch.cuda.Stream()
+    other = op.keep_tokens(w[1], lens, n, 4000, 3, 3, stream=stream)
+    stream.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(other, want[1]))
+
+
+@pytest.mark.parametrize("n", [50, 3000, 40000, 60001])
 def test_keep_equal_and_special_values(n):
     rows = [torch.zeros(n), torch.ones(n), torch.full((n,), math.inf), torch.full((n,), -math.inf), torch.full((n,), math.nan)]
     rows[0][::3] = -0.0
