@@ -48,7 +48,9 @@ extern "C" {
  *              head. Other pages' bounds are left as they were.
  * A sequence with ctx_lens[b] outside [0, max_ctx_len], or q_lens[b] outside
  * [1, min(ctx_lens[b], max_q_len)], is skipped, and so is a page outside
- * [0, num_pages). */
+ * [0, num_pages). Sequences that share a page hold the same tokens of it (as
+ * after comem_kv_fork, which shares whole pages alone): each of them writes its
+ * bounds. */
 comem_status comem_block_bounds(const comem_decode_attn_plan* plan, const void* k_pages, int64_t stride_page,
                                 int64_t stride_token, int64_t stride_head, int32_t page_size, int64_t num_pages,
                                 const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,

@@ -196,3 +196,69 @@ def test_a_context_run(dtype, page):
     s.sparse_steps(5, 3)
     s.release([0, 1, 2])
     assert int(s.counts.abs().sum()) == 0
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 4), ("fp8", 16)])
+def test_pools_past_32_bits(dtype, page):
+    """Every call over pages whose bytes, and whose bounds' bytes, lie past 2^32 gives what it gives over a small pool."""
+    from tests.test_gpu_block_attn import make_op
+
+    say("pools past 32 bits", dtype, page)
+    hkv, d, lens = 8, 128, [203, 64, 1]
+    g = torch.Generator().manual_seed(12)
+    width = -(-max(lens) // page)
+    few = 3 * width
+    kind = torch.float8_e4m3fn if dtype == "fp8" else torch.bfloat16
+    size = 1 if dtype == "fp8" else 2
+    small = torch.randn((few, page, hkv, d), generator=g).to(kind).to(DEV)
+    base = 2 ** 32 // (2 * hkv * d * size) + 100  # bounds of a page: 2 hkv d elements
+    assert base * 2 * hkv * d * size > 2 ** 32 and base * page * hkv * d * size > 2 ** 32
+    big = torch.empty((base + few, page, hkv, d), dtype=torch.uint8 if dtype == "fp8" else kind, device=DEV).view(kind)
+    big[base:] = small
+    ends = {0: torch.empty((few, hkv, 2, d), dtype=kind, device=DEV)}
+    ends[base] = torch.empty((base + few, hkv, 2, d), dtype=torch.uint8 if dtype == "fp8" else kind, device=DEV).view(kind)
+    table = torch.randperm(few, generator=g).view(3, width).to(torch.int32).to(DEV)
+    ctx = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    op = make_op(dtype, 32, hkv, d, 3, 203)
+    q = torch.randn((3, 32, d), generator=g).to(torch.bfloat16).to(DEV)
+    got = {}
+    for shift, pool in ((0, small), (base, big)):
+        at, e = table + shift, ends[shift]
+        op.block_bounds(pool, at, ctx, 203, e, q_lens=ctx, max_q_len=203)
+        scores = op.block_scores(q, e, page, at, ctx, 203, scores=torch.zeros((3, hkv, width), device=DEV))
+        chosen, count = op.block_select(scores, page, at, ctx, 203, 5, table=torch.full((3, hkv, 5), shift, dtype=torch.int32,
+                                                                                       device=DEV))
+        out, lse = op.block_forward(q, pool, pool, chosen, count, 5 * page, lse=torch.empty((3, 32), device=DEV))
+        _, all_lse = op.forward_paged(q, pool, pool, at, ctx, 203, lse=torch.empty((3, 32), device=DEV))
+        paid = op.attn_weights_paged(q, all_lse, pool, at, ctx, 203)
+        got[shift] = (e[shift:][table[0].long()].view(torch.uint8), scores, chosen - shift, count, out, lse, paid)
+    for i, (a, b) in enumerate(zip(got[0], got[base])):
+        assert torch.equal(a, b), i
+    # One long cache without pages: the sequence begins past 2^32 bytes.
+    flat, start = big.view(-1, hkv, d), (base + few - width) * page
+    begin = torch.tensor([start], dtype=torch.int64, device=DEV)
+    own = flat[start:start + 203].view(torch.uint8).clone().view(kind)
+    a, b = (op.attn_weights(q[:1], all_lse[:1], k, s, ctx[:1], 203) for k, s in ((flat, begin), (own, begin * 0)))
+    assert torch.equal(a, b)
+
+
+def test_rows_of_weights_past_32_bits():
+    """Rows of weights further apart than 2^32 bytes."""
+    say("weights past 32 bits")
+    from tests.test_gpu_evict import make_op
+
+    g = torch.Generator().manual_seed(13)
+    n, stride = 3000, 2 ** 30 + 64
+    wide = torch.empty((2 * stride,), device=DEV).view(2, stride)
+    near = torch.rand((2, n), generator=g).to(DEV)
+    wide[:, :n] = near
+    ctx = torch.tensor([n, n - 1], dtype=torch.int32, device=DEV)
+    op = make_op("bf16", 8, 2, 64, 2, n)
+    got = [op.keep_tokens(w, ctx, n, 700, 3, 5) for w in (wide, near)]
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][3], got[1][3])
+    k = torch.randn((2 * n, 2, 64), generator=g).to(torch.bfloat16).to(DEV)
+    q = torch.randn((2, 8, 64), generator=g).to(torch.bfloat16).to(DEV)
+    lse, start = torch.full((2, 8), 9.0, device=DEV), torch.tensor([0, n], dtype=torch.int64, device=DEV)
+    for w in (wide, near):
+        op.attn_weights(q, lse, k, start, ctx, n, prior=w, decay=0.5, out=w)
+    assert torch.equal(wide[:, :n], near)

@@ -424,3 +424,38 @@ def test_keep_empty_call_and_capture():
         torch.cuda.synchronize()
         a, _, n, v = op.keep_tokens(w, lens, 300, 10, 1, 1)
         assert torch.equal(a, keep_g) and torch.equal(n, lens_g) and torch.equal(v, kept_g), i
+
+
+def test_two_graphs_and_eager_calls_of_shared_rows():
+    """Graphs of one plan have a workspace each; a caller's own serves calls that follow each other."""
+    c = Case([500, 400], [200, 400], "bf16", 2, 4, 64, 0)
+    x, q = c.ctx.to(DEV), c.q.to(DEV)
+    lse = [c.lse.to(DEV), (c.lse + 1).to(DEV)]
+    rows = dict(q_start=torch.tensor([0, 200], dtype=torch.int64, device=DEV),
+                q_lens=torch.tensor([200, 400], dtype=torch.int32, device=DEV), max_q_len=400)
+    nbytes = c.op.attn_weights_workspace_bytes(2, 400, 500)
+    assert nbytes > 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+
+    def call(i, **kw):
+        return c.op.attn_weights(q, lse[i], x["k"], x["seq_start"], x["ctx_lens"], 500, **rows, **kw)
+
+    want = [call(0), call(1)]
+    torch.cuda.synchronize()
+    for given in ({}, {"workspace": ws}):
+        graphs, got = [torch.cuda.CUDAGraph() for _ in lse], []
+        for i, graph in enumerate(graphs):
+            with torch.cuda.graph(graph):
+                got.append(call(i, **given))
+        for _ in range(3):
+            ws.fill_(255)
+            for graph in graphs:
+                graph.replay()
+            eager = call(0, **given)
+            torch.cuda.synchronize()
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(eager, want[0])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[call(i, stream=s) for i, s in enumerate(streams)] for _ in range(4)]
+    torch.cuda.synchronize()
+    for pair in got:
+        assert torch.equal(pair[0], want[0]) and torch.equal(pair[1], want[1])
