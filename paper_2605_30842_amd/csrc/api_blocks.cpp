@@ -88,8 +88,14 @@ comem_status comem_block_bounds(const comem_decode_attn_plan* plan, const void* 
   a.pieces = static_cast<int32_t>(p->cfg.num_kv_heads * head_pieces);
   // Pages that max_q_len tokens can lie in.
   const int64_t pages = std::min({ceil_div(max_q_len - 1, page_size) + 1, ceil_div(max_ctx_len, page_size), kMostBlocks});
+  // A workgroup takes whole tokens; of few and long pages 512 bytes of each, so
+  // that more workgroups share a page (us, 512 bytes / whole tokens of 2 KiB and,
+  // FP8, 1 KiB: 64 pages of 64 tokens 4.2 / 6.0 and 6.1 / 6.9, of 128 5.1 / 9.0
+  // and 7.6 / 9.8, of 16 4.2 / 3.6 and 6.1 / 5.5; 1024 of 64 25 / 23 and 26 / 20).
+  const bool few = page_size >= 64 && pages * batch <= p->num_cus;
+  a.width = std::min(a.pieces, few ? 32 : comem::kBoundsThreads);
   const dim3 grid(static_cast<unsigned>(pages), static_cast<unsigned>(batch),
-                  static_cast<unsigned>(ceil_div(a.pieces, comem::kBoundsThreads)));
+                  static_cast<unsigned>(ceil_div(a.pieces, a.width)));
   return launched(comem::select_bounds_kernel(comem::cache_type(p->cfg)), grid, comem::kBoundsThreads, a, hip_stream);
 }
 

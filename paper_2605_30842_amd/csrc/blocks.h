@@ -28,6 +28,7 @@ struct BoundsParams {
   int32_t max_ctx;
   int32_t max_q;
   int32_t pieces;              // 16-byte pieces of a token's heads
+  int32_t width;               // of them, a workgroup's
   int32_t piece_shift;         // log2 of those of one head
 };
 

@@ -102,10 +102,10 @@ __global__ __launch_bounds__(kBoundsThreads) void block_bounds_kernel(const Boun
   const int L = uniform_i32(p.ctx_lens[b]);
   const int M = p.q_lens == nullptr ? 1 : uniform_i32(p.q_lens[b]);
   if (L > p.max_ctx || M < 1 || M > L || M > p.max_q) return;
-  const int width = min(p.pieces, kBoundsThreads);
+  const int width = p.width;
   const int slots = kBoundsThreads / width;
   const int slot = tid / width;
-  const int piece = blockIdx.z * kBoundsThreads + tid % width;
+  const int piece = blockIdx.z * width + tid % width;
   const bool works = slot < slots && piece < p.pieces;
   const int head = piece >> p.piece_shift, part = piece & ((1 << p.piece_shift) - 1);
   const int last = (L - 1) >> p.page_shift;
