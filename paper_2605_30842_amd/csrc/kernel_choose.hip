@@ -1,14 +1,17 @@
 // The largest entries of a row of scores, in the row's order (gfx950).
 //
-// One workgroup per row. Scores become 32-bit keys of the same order (NaN above
-// all, and entries that always stay above NaN), and the K-th largest key is
-// found 8 bits at a time from the top: a histogram of the digit over the keys
-// that share the digits found so far, then the digit at which the counts from
-// the top reach K. Keys above it stay, and as many of the equal ones as are
-// still missing, the first ones. Every wave has a run of the row, so an entry's
-// place is what the runs before hold plus a count of lane masks within its own.
+// Scores become 32-bit keys of the same order (NaN above all, and entries that
+// always stay above NaN), and the K-th largest key is found some bits at a time
+// from the top: a histogram of the digit over the keys that share the digits
+// found so far, then the digit at which the counts from the top reach K. Keys
+// above it stay, and as many of the equal ones as are still missing, the first
+// ones. Every wave has a run of the row, so an entry's place is what the runs
+// before hold plus a count of lane masks within its own: nothing depends on the
+// order of atomics, which only count.
 //
-// The histogram is kept 32 times, one copy for each of 32 lanes: score digits
+// Three forms, by the longest row: one wave, one workgroup, and three launches
+// with a workgroup for each 8192 entries (which asks for a workspace).
+// Histograms are kept 4 times, for a quarter of the lanes each: score digits
 // cluster (a sign and an exponent have few values), and counts that meet in one
 // word are added one after another.
 #include <algorithm>
@@ -147,7 +150,9 @@ __device__ inline void load_to_lds(const void* from, uint32_t* to) {
 }
 
 // Rows of at most kWaveEntries: one wave each, which needs no barrier. 8 bits
-// at a time, 4 copies of the histogram, 4 bins a lane.
+// at a time, 4 copies of the histogram, 4 bins a lane. The loops are rolled:
+// the code is cold at every launch. 8 rows of 512 blocks 5.5 us, 512 rows of
+// 128-1024 9.5 us; latency.
 constexpr int kWaveEntries = 2048, kWaveCopies = 4;
 
 __device__ inline void wave_lds_done() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
@@ -262,9 +267,9 @@ __device__ inline int waves_before(const int* x, int w, int lane) {
 // `gridDim.y` workgroups do the first two for a row, with the same results,
 // and share the third.
 //
-// One compute unit's instructions bound it, so turns without NaN between the
-// entries that always stay compare scores as floats, and only the others, and
-// the lists, make keys.
+// One compute unit's instructions bound it (24300 entries 14.3 us, 131072 45),
+// so turns without NaN between the entries that always stay compare scores as
+// floats, and only the others, and the lists, make keys.
 constexpr int kThreadsWide = 1024, kWavesWide = kThreadsWide / 64;
 constexpr int kBins = 2048, kCopies = 4;  // of the histogram
 constexpr int kTurn = 8;                  // groups of a turn

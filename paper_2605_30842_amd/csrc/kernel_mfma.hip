@@ -335,7 +335,7 @@ __device__ inline float across_groups(float x, Op op) {
 // what the result is off by: 1.8e-6 of the outputs' norm with two parts,
 // 3e-7 with three (a float32 softmax in torch: 6e-7). A third product for
 // each two costs a call that memory bounds nothing: 64 blocks of 64, one
-// sequence 9.7 / 9.7 us, 128 for 8 sequences 50.3 / 50.3.
+// sequence 9.7 / 9.8 us, 128 for 8 sequences 50.3 / 49.9 (two / three parts).
 template <int D, bool FINE>
 __device__ inline void compute_tile(const Tile<D>& T, int t0, int t_end, int g,
                                     const bf16x8 (&qop)[D / 32], float scale_log2, float& m_run,
