@@ -664,6 +664,13 @@ def _empty_on(stream, like, shape, **dtype):
     return t
 
 
+def _like_on(stream, like, dtype):
+    """_empty_on for a contiguous tensor's own shape (for which torch has a call that costs half)."""
+    import torch
+
+    return torch.empty_like(like, dtype=dtype) if stream is None else _empty_on(stream, like, like.shape, dtype=dtype)
+
+
 def _zeros_on(stream, like, shape):
     """float32 zeros, of the call's stream as in _empty_on."""
     import torch
@@ -1184,6 +1191,18 @@ class DecodeAttention:
         """A dense tensor of the plan's device, or ValueError."""
         _check_tensor(name, t, (dtype,), self._torch_device, shape=shape)
 
+    def _keys(self, k, dims):
+        """Shape and strides of a cache's keys, or ValueError."""
+        import torch
+
+        if isinstance(k, torch.Tensor):
+            shape, strides = k.shape, k.stride()
+            if (len(shape) == dims and shape[-2] == self.num_kv_heads and shape[-1] == self.head_dim
+                    and strides[-1] == 1 and k.dtype in self._kv_dtypes and k.get_device() == self._at):
+                return shape, strides
+        self._check_cache(k, k, paged=dims == 4)
+        return k.shape, k.stride()
+
     def _check_rows_of(self, name, t, rows, width):
         """A float32 tensor [rows, width or more] with dense rows that do not overlap."""
         import torch
@@ -1193,12 +1212,25 @@ class DecodeAttention:
               f"{name} must have dense rows of at least {width} elements, got {tuple(t.shape)}")
         _need(rows <= 1 or t.stride(0) >= t.shape[1], f"the rows of {name} must not overlap")
 
+    def _table_width(self, block_table, ctx_lens, batch):
+        """Entries of a sequence's row of the table, or ValueError (ctx_lens has been looked at)."""
+        import torch
+
+        if isinstance(block_table, torch.Tensor):
+            shape = block_table.shape
+            if (len(shape) == 2 and shape[0] == batch and block_table.dtype is torch.int32
+                    and block_table.get_device() == self._at and block_table.is_contiguous()
+                    and ctx_lens.is_contiguous()):
+                return shape[1]
+        self._check_lengths(ctx_lens, batch, block_table=block_table)
+        return block_table.shape[1]
+
     def attn_weights_workspace_bytes(self, batch: int, max_q_len: int, max_ctx_len: int) -> int:
         """Bytes of a workspace that a weights call with these bounds can use (0: none)."""
         return comem_attn_weights_workspace(self.plan, batch, max_q_len, max_ctx_len)
 
-    def _weights_args(self, q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior, decay, out, paged,
-                      stream, workspace):
+    def _weights_args(self, q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior, decay, out, stream,
+                      workspace):
         import torch
 
         tensor, at, f32, i32 = torch.Tensor, self._at, torch.float32, torch.int32
@@ -1227,7 +1259,6 @@ class DecodeAttention:
             else:
                 self._dense("q_start", q_start, torch.int64, lens)
                 self._dense("q_lens", q_lens, i32, lens)
-        self._check_cache(k, k, paged=paged)
         batch, width = lens[0], int(max_ctx_len)
         if out is None:
             out = _zeros_on(stream, q, (batch, width))
@@ -1243,7 +1274,7 @@ class DecodeAttention:
         return batch, out, (self.plan, q.data_ptr(), lse.data_ptr(), None if q_start is None else q_start.data_ptr(),
                             None if q_lens is None else q_lens.data_ptr(), int(max_q_len), k.data_ptr()), (
             ctx_lens.data_ptr(), batch, width, None if prior is None else prior.data_ptr(), float(decay),
-            out.data_ptr(), stride, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes), ws
+            out.data_ptr(), stride, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes)
 
     def attn_weights(self, q, lse, k, seq_start, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
                      max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None, workspace=None):
@@ -1254,21 +1285,22 @@ class DecodeAttention:
         may be prior itself; the new tokens' own prior is 0, and elements past a context stay (0 where out is made here).
         workspace: as in prefill (attn_weights_workspace_bytes says how much can be used).
         """
-        batch, out, head, tail, ws = self._weights_args(q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len,
-                                                        prior, decay, out, False, stream, workspace)
+        _, strides = self._keys(k, 3)
+        batch, out, head, tail = self._weights_args(q, lse, k, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len, prior,
+                                                    decay, out, stream, workspace)
         self._check_lengths(ctx_lens, batch, seq_start=seq_start)
-        _call_on(self, stream, comem_attn_weights, *head, k.stride(0), k.stride(1), seq_start.data_ptr(), *tail)
+        _call_on(self, stream, comem_attn_weights, *head, strides[0], strides[1], seq_start.data_ptr(), *tail)
         return out
 
     def attn_weights_paged(self, q, lse, k_pages, block_table, ctx_lens, max_ctx_len: int, q_start=None, q_lens=None,
                            max_q_len: int = 1, prior=None, decay: float = 1.0, out=None, stream=None, workspace=None):
         """The same over a paged cache."""
-        batch, out, head, tail, ws = self._weights_args(q, lse, k_pages, ctx_lens, max_ctx_len, q_start, q_lens,
-                                                        max_q_len, prior, decay, out, True, stream, workspace)
-        self._check_lengths(ctx_lens, batch, block_table=block_table)
-        pool, strides = k_pages.shape, k_pages.stride()
+        pool, strides = self._keys(k_pages, 4)
+        batch, out, head, tail = self._weights_args(q, lse, k_pages, ctx_lens, max_ctx_len, q_start, q_lens, max_q_len,
+                                                    prior, decay, out, stream, workspace)
+        width = self._table_width(block_table, ctx_lens, batch)
         _call_on(self, stream, comem_attn_weights_paged, *head, strides[0], strides[1], strides[2], pool[1], pool[0],
-                 block_table.data_ptr(), block_table.shape[1], *tail)
+                 block_table.data_ptr(), width, *tail)
         return out
 
     def keep_tokens_workspace_bytes(self, n: int, max_ctx_len: int) -> int:
@@ -1309,10 +1341,11 @@ class DecodeAttention:
         elif not _fits(keep, tensor, (i32,), self._torch_device, (n, width)):
             self._dense("keep", keep, i32, (n, width))
         if kept is None:
-            kept = _empty_on(stream, weights, (n, width))
+            kept = _like_on(stream, keep, torch.float32)
         elif not _fits(kept, tensor, (torch.float32,), self._torch_device, (n, width)):
             self._dense("kept", kept, torch.float32, (n, width))
-        start, lens = _empty_on(stream, ctx_lens, (n,), dtype=torch.int64), _empty_on(stream, ctx_lens, (n,))
+        lens = _like_on(stream, ctx_lens if rows is None else rows, i32)
+        start = _like_on(stream, lens, torch.int64)
         ws = workspace
         if ws is not None or max_ctx_len > KEEP_CHUNKS_MIN_CTX:
             ws = self._scratch(lambda: self.keep_tokens_workspace_bytes(n, int(max_ctx_len)), stream, workspace)
@@ -1349,8 +1382,7 @@ class DecodeAttention:
         bounds [P, Hkv, 2, D] of the cache's type. Call it after new tokens were stored and after compact and fork."""
         import torch
 
-        self._check_cache(k_pages, k_pages, paged=True)
-        pool, strides = k_pages.shape, k_pages.stride()
+        pool, strides = self._keys(k_pages, 4)
         batch, _ = self._check_blocks(pool[1], block_table, ctx_lens, max_ctx_len)
         if type(max_q_len) is not int:
             self._check_bound(max_q_len, "max_q_len")
@@ -1404,7 +1436,7 @@ class DecodeAttention:
         if table is None:
             table = _empty_on(stream, ctx_lens, shape)
         if lens is None:
-            lens = _empty_on(stream, ctx_lens, (batch,))
+            lens = _like_on(stream, ctx_lens, i32)
         if not (isinstance(scores, tensor) and isinstance(table, tensor) and isinstance(lens, tensor)
                 and scores.shape == (batch, hkv, blocks) and scores.dtype is torch.float32
                 and scores.get_device() == at and scores.is_contiguous() and table.shape == shape
@@ -1423,31 +1455,36 @@ class DecodeAttention:
         tokens of the pages table[b, hk] (block_select's results; max_len bounds lens)."""
         import torch
 
-        tensor, at, i32, f32 = torch.Tensor, self._at, torch.int32, torch.float32
-        if not (isinstance(q, tensor) and isinstance(table, tensor) and isinstance(lens, tensor) and q.dim() == 3
-                and q.shape[1] == self.num_q_heads and q.shape[2] == self.head_dim and q.dtype in self._q_dtypes
-                and q.get_device() == at and q.is_contiguous()
-                and (out is None or (isinstance(out, tensor) and out.shape == q.shape and out.dtype is f32
-                                     and out.get_device() == at and out.is_contiguous()))
-                and (lse is None or (isinstance(lse, tensor) and lse.shape == q.shape[:2] and lse.dtype is f32
-                                     and lse.get_device() == at and lse.is_contiguous()))
-                and table.dim() == 3 and table.dtype is i32 and table.shape[0] == q.shape[0]
-                and table.shape[1] == self.num_kv_heads and table.get_device() == at and table.is_contiguous()
-                and lens.shape == q.shape[:1] and lens.dtype is i32 and lens.get_device() == at
-                and lens.is_contiguous()):
+        tensor, at, hkv, i32, f32 = torch.Tensor, self._at, self.num_kv_heads, torch.int32, torch.float32
+        fast = False
+        if isinstance(q, tensor) and isinstance(table, tensor) and isinstance(lens, tensor):
+            shape, blocks = q.shape, table.shape
+            fast = (len(shape) == 3 and shape[1] == self.num_q_heads and shape[2] == self.head_dim
+                    and q.dtype in self._q_dtypes and q.get_device() == at and q.is_contiguous()
+                    and (out is None or (isinstance(out, tensor) and out.shape == shape and out.dtype is f32
+                                         and out.get_device() == at and out.is_contiguous()))
+                    and (lse is None or (isinstance(lse, tensor) and lse.shape == shape[:2] and lse.dtype is f32
+                                         and lse.get_device() == at and lse.is_contiguous()))
+                    and len(blocks) == 3 and blocks[0] == shape[0] and blocks[1] == hkv and table.dtype is i32
+                    and table.get_device() == at and table.is_contiguous() and lens.shape == shape[:1]
+                    and lens.dtype is i32 and lens.get_device() == at and lens.is_contiguous())
+        if not fast:
             self._check_q_out(q, out, lse)
-            self._dense("table", table, i32, (q.shape[0], self.num_kv_heads, None))
-            self._dense("lens", lens, i32, (q.shape[0],))
-        self._check_cache(k_pages, v_pages, paged=True)
+            shape = q.shape
+            self._dense("table", table, i32, (shape[0], hkv, None))
+            self._dense("lens", lens, i32, (shape[0],))
+            blocks = table.shape
+        pool, strides = self._keys(k_pages, 4)
+        if not (isinstance(v_pages, tensor) and v_pages.shape == pool and v_pages.stride() == strides
+                and v_pages.dtype is k_pages.dtype and v_pages.get_device() == at):
+            self._check_cache(k_pages, v_pages, paged=True)
         if type(max_len) is not int:
             self._check_bound(max_len, "max_len")
-        batch = q.shape[0]
         if out is None:
-            out = _empty_on(stream, q, q.shape, dtype=f32)
-        pool, strides = k_pages.shape, k_pages.stride()
+            out = _like_on(stream, q, f32)
         _call_on(self, stream, comem_block_attn, self.plan, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                 strides[0], strides[1], strides[2], pool[1], pool[0], table.data_ptr(), table.shape[2],
-                 lens.data_ptr(), batch, int(max_len), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                 strides[0], strides[1], strides[2], pool[1], pool[0], table.data_ptr(), blocks[2], lens.data_ptr(),
+                 shape[0], int(max_len), out.data_ptr(), None if lse is None else lse.data_ptr(),
                  self.workspace.data_ptr(), self.workspace_bytes)
         return out, lse
 
