@@ -727,7 +727,7 @@ def _in_private_pool(t) -> bool:
 # Shorter contexts hold fewer than two splits' worth of keys: not worth asking for a prefill workspace.
 PREFILL_SPLIT_MIN_CTX = 1024
 # Up to so many tokens a keep call never uses a workspace: not worth asking.
-KEEP_CHUNKS_MIN_CTX = 40960
+KEEP_CHUNKS_MIN_CTX = 49152
 
 
 class DecodeAttention:

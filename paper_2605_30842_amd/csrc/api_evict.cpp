@@ -151,15 +151,15 @@ comem_status launch_weights(const comem_decode_attn_plan& p, comem::WeightsParam
 }
 
 // Rows of a keep call in chunks (comem_keep_tokens_workspace), or 0. us, a
-// quarter kept, one workgroup a row / chunks: one row of 40000 entries 19 / 17,
-// of 65536 27 / 18, of 262144 84 / 24; 32 rows of 131072 49 / 29, of 262144
-// 88 / 64, of 524288 168 / 156; 128 of 65536 36 / 48. Every chunk adds up the
-// counts of all of its row's, so many chunks of many rows lose; up to 40960
-// entries an eager call's host time (three launches 19, one 11) would show.
+// quarter kept, one workgroup a row / chunks: one row of 49152 entries 17.4 /
+// 16.5, of 65536 20 / 16, of 262144 56 / 21; 32 rows of 131072 37 / 28, of
+// 262144 63 / 62; 64 of 65536 25 / 25, of 131072 41 / 49. Every chunk adds up
+// the counts of all of its row's, so many chunks of many rows lose; up to 49152
+// entries an eager call's host time (three launches 18, one 10) would show.
 int64_t keep_chunks(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {
   const int64_t chunks = ceil_div(max_ctx, comem::kChunkEntries);
-  const bool few = 4 * n <= p.num_cus && n * chunks <= 4 * p.num_cus;
-  return max_ctx > 40960 && chunks <= comem::kMostChunks && few ? chunks : 0;
+  const bool few = 8 * n <= p.num_cus && n * chunks <= 4 * p.num_cus;
+  return max_ctx > 49152 && chunks <= comem::kMostChunks && few ? chunks : 0;
 }
 
 size_t keep_bytes(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {

@@ -15,6 +15,7 @@
 // cluster (a sign and an exponent have few values), and counts that meet in one
 // word are added one after another.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "evict.h"
@@ -141,6 +142,8 @@ __device__ inline int upto_lane(int x) {
   return x;
 }
 
+__device__ inline int wave_sum(int x) { return __builtin_amdgcn_readlane(upto_lane(x), 63); }
+
 // 4 bytes from each lane's address to consecutive places in LDS. (The caller
 // waits for vector memory before it reads them.)
 __device__ inline void load_to_lds(const void* from, uint32_t* to) {
@@ -262,18 +265,20 @@ __device__ inline int waves_before(const int* x, int w, int lane) {
 // (4 copies of the histogram, so that lanes with one digit do not all wait for
 // one word), which gives the digit that holds the limit. The second time it
 // counts what lies above that digit and lists the scores that have it, a few
-// percent of the row; the other digits, 11 and 10 bits, follow from the lists
-// (where one overflows, from the row again). The third time it puts what stays.
-// `gridDim.y` workgroups do the first two for a row, with the same results,
-// and share the third.
+// percent of the row, each lane its own; the other digits, 11 and 10 bits,
+// follow from the lists (where one overflows, from the row again). The third
+// time it puts what stays. `gridDim.y` workgroups do the first two for a row,
+// with the same results, and share the third.
 //
-// One compute unit's instructions bound it (24300 entries 14.3 us, 131072 45),
-// so turns without NaN between the entries that always stay compare scores as
-// floats, and only the others, and the lists, make keys.
+// One compute unit's instructions bound it (24300 entries 12.1 us: launch 2.0,
+// first count 2.7, its digit 1.4, the lists 3, the rest 3), so turns without
+// NaN between the entries that always stay compare scores as floats, and only
+// the others, and the lists, make keys. Rows held in LDS between the readings
+// took 13.5: LDS holds fewer lists then, and the loads were hidden.
 constexpr int kThreadsWide = 1024, kWavesWide = kThreadsWide / 64;
 constexpr int kBins = 2048, kCopies = 4;  // of the histogram
 constexpr int kTurn = 8;                  // groups of a turn
-constexpr int kListed = 1920;             // scores of a wave's list
+constexpr int kListed = 30;               // scores of a lane's list
 
 // The least score whose key is k or more (a NaN, which no comparison holds for,
 // where there is no such number).
@@ -343,61 +348,82 @@ struct Row {
     }
   }
 
+  // f(PLAIN) for the kinds of turns apart (one body for both branches at every
+  // entry: 24300 entries 14.0 us instead of 12.1).
+  template <typename F>
+  __device__ static void by_kind(Turn kind, F&& f) {
+    if (kind == Turn::kPlain) {
+      f(std::true_type());
+    } else {
+      f(std::false_type());
+    }
+  }
+
   // Counts a turn's first digits, by the bits as they are; -0 as 0, NaN as one of them.
   template <typename Add>
   __device__ void count(int at, const float (&x)[kTurn], Turn kind, Add&& add) const {
     if (kind == Turn::kForced || kind == Turn::kEmpty) return;
-    const bool plain = kind == Turn::kPlain;
+    by_kind(kind, [&](auto plain) {
 #pragma unroll
-    for (int e = 0; e < kTurn; ++e) {
-      uint32_t u = __float_as_uint(x[e] + 0.f);
-      if (!plain) u = x[e] == x[e] ? u : 0x7fffffffu;
-      if (plain || chosen(at + 64 * e + lane)) add(static_cast<int>(u >> 21));
-    }
+      for (int e = 0; e < kTurn; ++e) {
+        uint32_t u = __float_as_uint(x[e] + 0.f);
+        if constexpr (plain) {
+          add(static_cast<int>(u >> 21));
+        } else {
+          u = x[e] == x[e] ? u : 0x7fffffffu;
+          if (chosen(at + 64 * e + lane)) add(static_cast<int>(u >> 21));
+        }
+      }
+    });
   }
-  // Adds a turn's entries above digit `top` to `above`, and lists those that have it.
+  // Adds the lane's entries of a turn above digit `top` to `above`, and lists
+  // those that have it: store(listed, score, true) for the lane's `listed`-th
+  // one, and with false for the others.
   template <typename Store>
   __device__ void list(int at, const float (&x)[kTurn], Turn kind, uint32_t top, float least, float over, int& above,
                        int& listed, Store&& store) const {
-    if (kind == Turn::kForced) above += 64 * kTurn;
+    if (kind == Turn::kForced) above += kTurn;
     if (kind == Turn::kForced || kind == Turn::kEmpty) return;
-    const bool plain = kind == Turn::kPlain;
+    by_kind(kind, [&](auto plain) {
 #pragma unroll
-    for (int e = 0; e < kTurn; ++e) {
-      uint64_t more, same;
-      if (plain) {
-        more = __builtin_amdgcn_ballot_w64(x[e] >= over);
-        same = __builtin_amdgcn_ballot_w64(x[e] >= least) & ~more;
-      } else {
-        const int i = at + 64 * e + lane;
-        const uint32_t digit = key_of(x[e]) >> 21;
-        more = __builtin_amdgcn_ballot_w64(forced(i) || (chosen(i) && digit > top));
-        same = __builtin_amdgcn_ballot_w64(chosen(i) && digit == top);
+      for (int e = 0; e < kTurn; ++e) {
+        bool more, same;
+        if constexpr (plain) {
+          more = x[e] >= over;
+          same = (x[e] >= least) != more;  // `over` is above `least`
+        } else {
+          const int i = at + 64 * e + lane;
+          const uint32_t digit = key_of(x[e]) >> 21;
+          more = forced(i) || (chosen(i) && digit > top);
+          same = chosen(i) && digit == top;
+        }
+        store(listed, x[e], same);
+        above += more ? 1 : 0;
+        listed += same ? 1 : 0;
       }
-      above += __builtin_popcountll(more);
-      if (same != 0) {
-        if (((same >> lane) & 1) != 0) store(listed + lanes_before(same), x[e]);
-        listed += __builtin_popcountll(same);
-      }
-    }
+    });
   }
   // Puts a turn's entries that stay.
   __device__ void put(int at, const float (&x)[kTurn], Turn kind, const Limit& limit, float least, float tie,
                       Places& places) const {
     if (kind == Turn::kEmpty) return;
-    const bool plain = kind == Turn::kPlain;
+    by_kind(kind, [&](auto plain) {
 #pragma unroll
-    for (int e = 0; e < kTurn; ++e) {
-      const int i = at + 64 * e + lane;
-      bool stays = x[e] >= least, equals = x[e] == tie;
-      if (!plain) {
-        const uint32_t k = key(i, x[e]);
-        stays = k >= limit.least;
-        equals = limit.ties > 0 && k == limit.tie;
+      for (int e = 0; e < kTurn; ++e) {
+        const int i = at + 64 * e + lane;
+        bool stays, equals;
+        if constexpr (plain) {
+          stays = x[e] >= least;
+          equals = x[e] == tie;
+        } else {
+          const uint32_t k = key(i, x[e]);
+          stays = k >= limit.least;
+          equals = limit.ties > 0 && k == limit.tie;
+        }
+        const int to = places.next(stays, equals, limit.ties);
+        if (to >= 0) item.put(to, i, x[e]);
       }
-      const int to = places.next(stays, equals, limit.ties);
-      if (to >= 0) item.put(to, i, x[e]);
-    }
+    });
   }
 };
 
@@ -465,7 +491,7 @@ __device__ inline int taken(s32x4* bin) {
 template <bool BLOCKS>
 __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams p) {
   __shared__ s32x4 hist[kBins];
-  __shared__ float list[kWavesWide][kListed];
+  __shared__ float list[kWavesWide][kListed + 1][64];  // (the last place: those past the end)
   __shared__ Found found;
   __shared__ int wave_above[kWavesWide], wave_equal[kWavesWide];
   __shared__ int too_long;
@@ -510,7 +536,7 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
       });
     } else {
 #pragma unroll 1
-      for (int i = lane; i < listed; i += 64) add_key(key_of(list[w][i]));
+      for (int i = 0; i < listed; ++i) add_key(key_of(list[w][i][lane]));
     }
     lds_barrier();
     int v[2];  // of a thread's two digits, from the top down
@@ -528,9 +554,9 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
           own_above = above;
           own_listed = listed;
         }
-        row.list(at, x, kind, top, least, over, above, listed, [&](int place, float score) {
-          if (place < kListed) list[w][place] = score;
-        });
+        row.list(at, x, kind, top, least, over, above, listed,
+                 // One that has another digit is written over by the next.
+                 [&](int place, float score, bool) { list[w][min(place, kListed)][lane] = score; });
       });
       if (listed > kListed) too_long = 1;
       lds_barrier();
@@ -542,43 +568,40 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
   const Limit limit = search.limit();
   const float least = score_of(limit.least), tie = search.tie();
 
-  // What each run, and this workgroup's part of it, holds of what stays.
-  Places own;
-  int equal = 0;
+  // What each lane of a run, and before this workgroup's part of it, has of what stays.
+  int equal = 0, own_equal = 0;
   if (overflow) {
-    above = 0;
+    above = own_above = 0;
     row.for_turns(run, 0, turns, 0, next, [&](int at, const float (&x)[kTurn], Turn) {
-      if (at == run + 64 * kTurn * part_begin) own = {above, equal};
+      if (at == run + 64 * kTurn * part_begin) {
+        own_above = above;
+        own_equal = equal;
+      }
 #pragma unroll
       for (int e = 0; e < kTurn; ++e) {
         const uint32_t k = row.key(at + 64 * e + lane, x[e]);
-        above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= limit.least));
-        if (limit.ties > 0) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == limit.tie));
+        above += k >= limit.least ? 1 : 0;
+        equal += k == limit.tie ? 1 : 0;
       }
     });
   } else {
-    own.above = own_above;
 #pragma unroll 1
-    for (int i = 0; i < listed; i += 64) {
-      const uint32_t k = i + lane < listed ? key_of(list[w][i + lane]) : 0;
-      const uint64_t mine = own_listed - i >= 64 ? ~uint64_t{0} : own_listed > i ? (uint64_t{1} << (own_listed - i)) - 1 : 0;
-      const uint64_t more = __builtin_amdgcn_ballot_w64(k >= limit.least);
-      above += __builtin_popcountll(more);
-      own.above += __builtin_popcountll(more & mine);
-      if (limit.ties > 0) {
-        const uint64_t same = __builtin_amdgcn_ballot_w64(k == limit.tie);
-        equal += __builtin_popcountll(same);
-        own.equal += __builtin_popcountll(same & mine);
-      }
+    for (int i = 0; i < listed; ++i) {
+      const uint32_t k = key_of(list[w][i][lane]);
+      const int more = k >= limit.least ? 1 : 0, same = k == limit.tie ? 1 : 0, mine = i < own_listed ? 1 : 0;
+      above += more;
+      equal += same;
+      own_above += more & mine;
+      own_equal += same & mine;
     }
   }
+  const int all_above = wave_sum(above), all_equal = wave_sum(equal);
   if (lane == 0) {
-    wave_above[w] = above;
-    wave_equal[w] = equal;
+    wave_above[w] = all_above;
+    wave_equal[w] = all_equal;
   }
   lds_barrier();
-  own.above += waves_before(wave_above, w, lane);
-  if (limit.ties > 0) own.equal += waves_before(wave_equal, w, lane);
+  Places own{wave_sum(own_above) + waves_before(wave_above, w, lane), wave_sum(own_equal) + waves_before(wave_equal, w, lane)};
   if (part_begin != 0) row.ask(run + 64 * kTurn * part_begin, next);
   row.for_turns(run, part_begin, part_end, part_begin, next, [&](int at, const float (&x)[kTurn], Turn kind) {
     row.put(at, x, kind, limit, least, tie, own);
@@ -591,8 +614,8 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
 // adds up those of the row's chunks, finds the digit and lists its chunk's
 // scores that have it; in the third every workgroup goes through the lists for
 // the other digits and for what stays before its chunk, and puts the chunk's.
-// Latency bounds them: 8 rows of 32768-131072, 4.1 MB in and out, 4 + 6 + 7 us,
-// where one workgroup a row takes 42. (A workgroup of 4 waves for a chunk, each
+// Latency bounds them: 8 rows of 32768-131072, 4.1 MB in and out, 17.5 us in
+// all, where one workgroup a row takes 34. (A workgroup of 4 waves for a chunk, each
 // wave with four turns and a list of its own, took 31: too few instructions at
 // once in the lists.)
 static_assert(kChunkEntries == kThreadsWide * kTurn);
@@ -656,10 +679,11 @@ __global__ __launch_bounds__(kThreadsWide) void chunk_list_kernel(const ChoosePa
   const float least = score_of(top << 21), over = top == kBins - 1 ? __builtin_nanf("") : score_of((top + 1) << 21);
   const Turn kind = row.kind(at, x);
   int above = 0, listed = 0;
-  row.list(at, x, kind, top, least, over, above, listed, [](int, float) {});
-  if (lane == 0) {
-    wave_above[w] = above;
-    wave_listed[w] = listed;
+  row.list(at, x, kind, top, least, over, above, listed, [](int, float, bool) {});
+  const int upto = upto_lane(listed), all_above = wave_sum(above);
+  if (lane == 63) {
+    wave_above[w] = all_above;
+    wave_listed[w] = upto;
   }
   lds_barrier();
   if (tid == 0) {
@@ -670,16 +694,18 @@ __global__ __launch_bounds__(kThreadsWide) void chunk_list_kernel(const ChoosePa
     }
   }
   if (w == 0) {
-    const int all_above = waves_before(wave_above, kWavesWide, lane);
-    const int all_listed = waves_before(wave_listed, kWavesWide, lane);
+    const int chunk_above = waves_before(wave_above, kWavesWide, lane);
+    const int chunk_listed = waves_before(wave_listed, kWavesWide, lane);
     if (lane == 0) {
-      space.above[chunk] = all_above;
-      space.listed[chunk] = all_listed;
+      space.above[chunk] = chunk_above;
+      space.listed[chunk] = chunk_listed;
     }
   }
-  listed = waves_before(wave_listed, w, lane);
+  listed = waves_before(wave_listed, w, lane) + upto - listed;
   float* list = space.lists + static_cast<int64_t>(chunk) * kChunkEntries;
-  row.list(at, x, kind, top, least, over, above, listed, [&](int place, float score) { list[place] = score; });
+  row.list(at, x, kind, top, least, over, above, listed, [&](int place, float score, bool has) {
+    if (has) list[place] = score;
+  });
 }
 
 __global__ __launch_bounds__(kThreadsWide) void chunk_put_kernel(const ChooseParams p) {
@@ -769,9 +795,9 @@ __global__ __launch_bounds__(kThreadsWide) void chunk_put_kernel(const ChoosePar
   lds_barrier();
   Places own;
   own.above = waves_before(wave_above, w, lane) +
-              __builtin_amdgcn_readlane(upto_lane(lane < chunk ? above_of[lane] : 0), 63);
+              wave_sum(lane < chunk ? above_of[lane] : 0);
   own.equal = waves_before(wave_equal, w, lane) +
-              __builtin_amdgcn_readlane(upto_lane(lane < chunk ? equal_of[lane] : 0), 63);
+              wave_sum(lane < chunk ? equal_of[lane] : 0);
   row.put(at, x, kind, limit, least, tie, own);
 }
 

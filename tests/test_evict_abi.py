@@ -144,9 +144,9 @@ def test_keep_workspace():
     p, _ = B.comem_decode_attn_init(B.Config(num_q_heads=8, num_kv_heads=8, head_dim=64, dtype=B.BF16, scale=0.1,
                                              max_batch=4, max_ctx_len=1 << 30), B.NO_DEVICE)
     size = lambda *a: B.comem_keep_tokens_workspace(p, *a)  # noqa: E731
-    assert size(0, 100000) == size(5, 40960) == size(5, 0) == size(5, 1 << 30) == 0
-    assert size(65, 50000) == size(33, 500000) == 0
-    assert size(1, 40961) >= 4 * 40961 and size(3, 131072) == 3 * size(1, 131072) and size(1, 131072) % 256 == 0
+    assert size(0, 100000) == size(5, 49152) == size(5, 0) == size(5, 1 << 30) == 0
+    assert size(33, 50000) == size(17, 500000) == 0
+    assert size(1, 49153) >= 4 * 49153 and size(3, 131072) == 3 * size(1, 131072) and size(1, 131072) % 256 == 0
     for a in ((-1, 5), (65536, 5), (1, -1), (1, (1 << 30) + 1)):
         with pytest.raises(B.ComemError) as e:
             size(*a)

@@ -316,7 +316,7 @@ def test_keep_long(n):
     check_keep(w, [n, n // 2], n - 1)
 
 
-@pytest.mark.parametrize("n", [40960, 40961, 49152, 49153, 131073, 524288, 524289])
+@pytest.mark.parametrize("n", [49152, 49153, 57344, 57345, 131073, 524288, 524289])
 def test_keep_with_and_without_a_workspace(n):
     """Long rows in chunks give what one workgroup a row gives: rows that end before, in and at the end of a chunk, one
     that stays whole, one whose bound it passes, one that is forced throughout."""
