@@ -803,7 +803,10 @@ __global__ __launch_bounds__(kThreadsWide) void chunk_put_kernel(const ChoosePar
 
 template <bool BLOCKS>
 ChooseForm form(int64_t most, int64_t items, int cus) {
-  if (most <= kWaveEntries) return {choose_wave_kernel<BLOCKS>, 64, 1};
+  // One wave, or one workgroup while there are compute units enough (us, 64 rows
+  // of 1025 entries 8.7 / 9.8, 1200 9.8 / 9.9, 1536 11.3 / 9.8, 2048 12.7 / 10.0;
+  // 256 of 2048 14.1 / 11.0; 300 of 2049 in workgroups 18.4, 512 of 2048 in waves 14.3).
+  if (most <= 1280 || (most <= kWaveEntries && items > cus)) return {choose_wave_kernel<BLOCKS>, 64, 1};
   const int64_t parts = std::min<int64_t>(8, std::max<int64_t>(1, cus / items));
   return {choose_kernel<BLOCKS>, kThreadsWide, static_cast<int>(parts)};
 }

@@ -306,6 +306,18 @@ def test_keep_sizes(part):
         check_keep(w, lens, budget, bound=bound)
 
 
+@pytest.mark.parametrize("n", [1280, 1281, 2047, 2048, 2049])
+def test_keep_many_rows(n):
+    """More rows than compute units, of lengths around those where the kernel changes, and few of them."""
+    g = torch.Generator().manual_seed(n)
+    w = (torch.randn((300, n), generator=g) * 3).exp()
+    w[7] = w[7].round()
+    lens = torch.randint(0, n + 1, (300,), generator=g).tolist()
+    lens[:9] = [n, n - 1, 0, 1, 255, 256, 257, n, n]
+    check_keep(w, lens, n // 3, first=1, last=2, bound=n)
+    check_keep(w[:9].contiguous(), lens[:9], n // 3, first=1, last=2, bound=n)
+
+
 @pytest.mark.parametrize("n", [32767, 32769, 65536, 65537, 100001, 150000])
 def test_keep_long(n):
     say("keep", n)
