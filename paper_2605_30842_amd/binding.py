@@ -724,6 +724,8 @@ def _in_private_pool(t) -> bool:
     return False
 
 
+INT32 = 1 << 31  # what an argument of 32 bits stays below
+
 # Shorter contexts hold fewer than two splits' worth of keys: not worth asking for a prefill workspace.
 PREFILL_SPLIT_MIN_CTX = 1024
 # Up to so many tokens a keep call never uses a workspace: not worth asking.
@@ -843,13 +845,16 @@ class DecodeAttention:
             _check_tensor(name, t, (k.dtype,), self._torch_device, shape=(batch, self.num_kv_heads, self.head_dim))
 
     @staticmethod
-    def _check_bound(max_ctx_len, name="max_ctx_len"):
-        if type(max_ctx_len) is int:
+    def _check_bound(max_ctx_len, name="max_ctx_len", most=1 << 63):
+        """An integer that the library's argument holds (of `most`, INT32 or 64 bits: ctypes takes a larger one modulo
+        2^32 or 2^64)."""
+        if type(max_ctx_len) is int and 0 <= max_ctx_len < most:
             return
         import numbers
 
         _need(isinstance(max_ctx_len, numbers.Integral) and not isinstance(max_ctx_len, bool),
               f"{name} must be an integer, got {type(max_ctx_len).__name__}")
+        _need(-most <= max_ctx_len < most, f"{name} is out of range, got {max_ctx_len}")
 
     def _outputs(self, q, out, lse):
         if out is None:
@@ -958,7 +963,7 @@ class DecodeAttention:
             if (_fits(ctx_lens, tensor, i32, dev, shape) and _fits(q_lens, tensor, i32, dev, shape)
                     and _fits(q_start, tensor, (torch.int64,), dev, shape)):
                 self._check_q_out(q, out, lse)
-                self._check_bound(max_q_len, "max_q_len")
+                self._check_bound(max_q_len, "max_q_len", INT32)
                 self._check_bound(max_ctx_len)
                 return
         _check_tensor("ctx_lens", ctx_lens, (torch.int32,), self._torch_device, ndim=1)
@@ -966,7 +971,7 @@ class DecodeAttention:
         self._check_q_out(q, out, lse)
         _check_tensor("q_start", q_start, (torch.int64,), self._torch_device, shape=(batch,))
         _check_tensor("q_lens", q_lens, (torch.int32,), self._torch_device, shape=(batch,))
-        self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_q_len, "max_q_len", INT32)
         self._check_bound(max_ctx_len)
 
     def _prefill_outputs(self, q, out, lse, stream=None):
@@ -1130,7 +1135,7 @@ class DecodeAttention:
             rows_stride = strides[0][:1] + strides[1][:1] + strides[2][:1]
         if not fast:
             self._check_rope(q, new_k, new_v, ctx_lens, cos_sin, q_weight, k_weight, q_start, q_lens, positions, q_out)
-        self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_q_len, "max_q_len", INT32)
         self._check_bound(max_ctx_len)
         rows = q.shape[0]
         if q_out is None:
@@ -1203,6 +1208,15 @@ class DecodeAttention:
         self._check_cache(k, k, paged=dims == 4)
         return k.shape, k.stride()
 
+    def _check_budget(self, budget, first, last):
+        """What a selection is asked for; returns the budget, which is a dimension of its results."""
+        if not (type(budget) is type(first) is type(last) is int and 0 <= budget < INT32 and 0 <= first < INT32
+                and 0 <= last < INT32):
+            for name, v in (("budget", budget), ("first", first), ("last", last)):
+                self._check_bound(v, name, INT32)
+            _need(budget >= 0, f"budget must not be negative, got {budget}")
+        return int(budget)
+
     def _check_rows_of(self, name, t, rows, width):
         """A float32 tensor [rows, width or more] with dense rows that do not overlap."""
         import torch
@@ -1246,7 +1260,7 @@ class DecodeAttention:
                          and isinstance(q_start, tensor) and q_start.dtype is torch.int64
                          and q_start.get_device() == at and q_lens.shape == q_start.shape == lens
                          and q_lens.is_contiguous() and q_start.is_contiguous()))
-        self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_q_len, "max_q_len", INT32)
         self._check_bound(max_ctx_len)
         if not fast:
             self._check_q_out(q, None, lse)
@@ -1261,6 +1275,7 @@ class DecodeAttention:
                 self._dense("q_lens", q_lens, i32, lens)
         batch, width = lens[0], int(max_ctx_len)
         if out is None:
+            _need(width >= 0, f"max_ctx_len must not be negative, got {width}")
             out = _zeros_on(stream, q, (batch, width))
         for name, t in (("out", out),) if prior is None else (("out", out), ("prior", prior)):
             if not (isinstance(t, tensor) and t.dtype is f32 and t.get_device() == at and t.is_contiguous()
@@ -1320,10 +1335,8 @@ class DecodeAttention:
         import torch
 
         tensor, at, i32 = torch.Tensor, self._at, torch.int32
-        for name, v in (("max_ctx_len", max_ctx_len), ("budget", budget), ("first", first), ("last", last)):
-            if type(v) is not int:
-                self._check_bound(v, name)
-        width = int(budget)
+        self._check_bound(max_ctx_len)
+        width = self._check_budget(budget, first, last)
         if not (isinstance(weights, tensor) and isinstance(ctx_lens, tensor) and ctx_lens.dtype is i32
                 and ctx_lens.dim() == 1 and ctx_lens.get_device() == at and ctx_lens.is_contiguous()
                 and weights.dtype is torch.float32 and weights.get_device() == at and weights.is_contiguous()
@@ -1364,8 +1377,8 @@ class DecodeAttention:
         import torch
 
         tensor, at, i32 = torch.Tensor, self._at, torch.int32
-        if type(page_size) is not int or type(max_ctx_len) is not int:
-            self._check_bound(page_size, "page_size")
+        if not (type(page_size) is type(max_ctx_len) is int and 0 < page_size < INT32 and 0 <= max_ctx_len < INT32):
+            self._check_bound(page_size, "page_size", INT32)
             self._check_bound(max_ctx_len)
         _need(page_size > 0, f"page_size must be positive, got {page_size}")
         if not (isinstance(ctx_lens, tensor) and isinstance(block_table, tensor) and ctx_lens.dtype is i32
@@ -1384,8 +1397,7 @@ class DecodeAttention:
 
         pool, strides = self._keys(k_pages, 4)
         batch, _ = self._check_blocks(pool[1], block_table, ctx_lens, max_ctx_len)
-        if type(max_q_len) is not int:
-            self._check_bound(max_q_len, "max_q_len")
+        self._check_bound(max_q_len, "max_q_len", INT32)
         shape = (pool[0], pool[2], 2, pool[3])
         if not (isinstance(bounds, torch.Tensor) and bounds.dtype is k_pages.dtype and bounds.get_device() == self._at
                 and bounds.shape == shape and bounds.is_contiguous()):
@@ -1406,6 +1418,7 @@ class DecodeAttention:
         tensor, at, hkv, d = torch.Tensor, self._at, self.num_kv_heads, self.head_dim
         batch, blocks = self._check_blocks(page_size, block_table, ctx_lens, max_ctx_len)
         if scores is None:
+            _need(max_ctx_len >= 0, f"max_ctx_len must not be negative, got {max_ctx_len}")
             scores = _empty_on(stream, ctx_lens, (batch, hkv, blocks), dtype=torch.float32)
         if not (isinstance(q, tensor) and isinstance(bounds, tensor) and isinstance(scores, tensor)
                 and q.shape == (batch, self.num_q_heads, d) and q.dtype in self._q_dtypes and q.get_device() == at
@@ -1429,10 +1442,7 @@ class DecodeAttention:
 
         tensor, at, hkv, i32 = torch.Tensor, self._at, self.num_kv_heads, torch.int32
         batch, blocks = self._check_blocks(page_size, block_table, ctx_lens, max_ctx_len)
-        if not type(budget) is type(first) is type(last) is int:
-            for name, v in (("budget", budget), ("first", first), ("last", last)):
-                self._check_bound(v, name)
-        shape = (batch, hkv, int(budget))
+        shape = (batch, hkv, self._check_budget(budget, first, last))
         if table is None:
             table = _empty_on(stream, ctx_lens, shape)
         if lens is None:
@@ -1478,8 +1488,7 @@ class DecodeAttention:
         if not (isinstance(v_pages, tensor) and v_pages.shape == pool and v_pages.stride() == strides
                 and v_pages.dtype is k_pages.dtype and v_pages.get_device() == at):
             self._check_cache(k_pages, v_pages, paged=True)
-        if type(max_len) is not int:
-            self._check_bound(max_len, "max_len")
+        self._check_bound(max_len, "max_len")
         if out is None:
             out = _like_on(stream, q, f32)
         _call_on(self, stream, comem_block_attn, self.plan, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
