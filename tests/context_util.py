@@ -142,6 +142,11 @@ def weights_of(ctx, q, lse, new, scale, prior=None, decay=1.0):
     return got
 
 
+def near(got, want, off):
+    """Whether every element is within its bound, which a NaN is not."""
+    return bool(((got - want).abs() <= off).all())
+
+
 def chosen(scores, count, first, last):
     """Positions of the `count` entries of a row (1-D) that stay, ascending."""
     x = np.asarray(scores, dtype=np.float32)
