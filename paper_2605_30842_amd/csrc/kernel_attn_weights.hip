@@ -239,7 +239,9 @@ __global__ __launch_bounds__(64 * kWeightsWaves, 2) void attn_weights_kernel(con
           for (int j = 0; j < Ring::kLoads; ++j) q.x[j] = slots[slot].x[Ring::place(j, c, g)];
           pay(q, slots[slot].lse[lane], token_of(group_at(i)));
         }
-        wait_stores_done();  // what was asked for past the last group is in no one's way
+        // What was asked for past the last group is in no one's way, and the last slot has been read before the next
+        // head asks for it anew.
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       } else {
         for (int n = first; n < groups; n += step) {
           const int64_t row = row_of(n);
