@@ -728,7 +728,7 @@ INT32 = 1 << 31  # what an argument of 32 bits stays below
 
 # Shorter contexts hold fewer than two splits' worth of keys: not worth asking for a prefill workspace.
 PREFILL_SPLIT_MIN_CTX = 1024
-# Up to so many tokens a keep call never uses a workspace: not worth asking.
+# Up to so many tokens a keep call never uses a workspace (kKeepChunksMinCtx of the library): not worth asking.
 KEEP_CHUNKS_MIN_CTX = 49152
 
 

@@ -150,6 +150,9 @@ comem_status launch_weights(const comem_decode_attn_plan& p, comem::WeightsParam
   return err == hipSuccess ? COMEM_OK : COMEM_ERR_HIP;
 }
 
+// Longest rows that one workgroup takes: the binding's KEEP_CHUNKS_MIN_CTX, below which it asks for no workspace.
+constexpr int64_t kKeepChunksMinCtx = 49152;
+
 // Rows of a keep call in chunks (comem_keep_tokens_workspace), or 0. us, a
 // quarter kept, one workgroup a row / chunks: one row of 49152 entries 17.4 /
 // 16.5, of 65536 20 / 16, of 262144 56 / 21; 32 rows of 131072 37 / 28, of
@@ -159,7 +162,7 @@ comem_status launch_weights(const comem_decode_attn_plan& p, comem::WeightsParam
 int64_t keep_chunks(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {
   const int64_t chunks = ceil_div(max_ctx, comem::kChunkEntries);
   const bool few = 8 * n <= p.num_cus && n * chunks <= 4 * p.num_cus;
-  return max_ctx > 49152 && chunks <= comem::kMostChunks && few ? chunks : 0;
+  return max_ctx > kKeepChunksMinCtx && chunks <= comem::kMostChunks && few ? chunks : 0;
 }
 
 size_t keep_bytes(const comem_decode_attn_plan& p, int64_t n, int64_t max_ctx) {
