@@ -12,11 +12,21 @@
  *     score[b, hk, n] = scale * max_h sum_d (max(q_hd, 0) hi_d + min(q_hd, 0) lo_d)
  *                    >= scale * q_h . k_t      for the keys t of block n
  *
- * over the G query heads h of KV head hk (FP8 caches: times k_scale). With
+ * over the G query heads h of KV head hk (FP8 caches: times k_scale). Scores are
+ * computed as float32 sums, so the inequality holds up to their rounding: 2 d_h
+ * 2^-23 of the sum of the products' magnitudes, and 2^-22 of the score. With
  * 2 / page_size of the keys' bytes that is what a step reads of the whole
  * context (comem_block_scores). Then each KV head of each sequence attends
  * over the blocks with its largest scores (comem_block_select,
  * comem_block_attn): out and lse as in comem_decode_attn, over their tokens.
+ *
+ * Four launches and the bounds' bytes instead of one and all of the keys' and
+ * values': worth it for long contexts and for batches. A whole step of these
+ * calls and comem_decode_attn_paged, us (graph; 8 KV heads of 128, pages of 64):
+ * one sequence of 32 query heads, 64 blocks, bf16 16384 tokens 20.3 / 16.0, 32768
+ * 21.7 / 25.6 (called eagerly through the torch wrapper 30 / 25), 65536 25.3 /
+ * 43.6, FP8 32768 22.1 / 16.3, 65536 26.0 / 26.3, 131072 28.6 / 45.6; 8 sequences
+ * of 64 heads and 131072 tokens, 128 blocks, bf16 77 / 632, FP8 57 / 339.
  *
  * Ownership, errors, streams and the device-side contract (lengths, block
  * tables) are those of the decode calls (comem_decode_attn.h); pages, strides
@@ -95,8 +105,8 @@ comem_status comem_block_select(const comem_decode_attn_plan* plan, const float*
  *              ceil(max_len / page_size).
  *   lens       device int32 [batch]; max_len the host's bound of them, at most
  *              the plan's max_ctx_len.
- * Other arguments, workspace and results as in comem_decode_attn_paged, but
- * that the weights enter the matrix cores in three bf16 parts instead of two:
+ * Other arguments, workspace (calls that share one do not overlap, decode calls
+ * among them) and results as in comem_decode_attn_paged, but that the weights enter the matrix cores in three bf16 parts instead of two:
  * a weight is off by less than 2^-26 of itself. */
 comem_status comem_block_attn(const comem_decode_attn_plan* plan, const void* q, const void* k_pages,
                               const void* v_pages, int64_t stride_page, int64_t stride_token, int64_t stride_head,

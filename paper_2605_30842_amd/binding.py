@@ -1297,7 +1297,8 @@ class DecodeAttention:
         [rows, Hq]: out[b, t] = decay * prior[b, t] + the sum of its attention weights over heads and new tokens.
 
         Without q_start and q_lens each sequence has one new token, else as in prefill. out (float32 [B, >= max_ctx_len])
-        may be prior itself; the new tokens' own prior is 0, and elements past a context stay (0 where out is made here).
+        may be prior itself; the new tokens' own prior is 0. Elements past a context stay, and so do all of a sequence
+        without new tokens (0 where out is made here: with q_lens that may be 0, let out be prior).
         workspace: as in prefill (attn_weights_workspace_bytes says how much can be used).
         """
         _, strides = self._keys(k, 3)
@@ -1411,8 +1412,8 @@ class DecodeAttention:
         return bounds
 
     def block_scores(self, q, bounds, page_size: int, block_table, ctx_lens, max_ctx_len: int, scores=None, stream=None):
-        """Bounds of the scores that q [B, Hq, D] reaches in each block: [B, Hkv, blocks of max_ctx_len] (elements past a
-        context's blocks are left as they were)."""
+        """Bounds of the scores that q [B, Hq, D] reaches in each block, up to the rounding of float32 sums: [B, Hkv, blocks
+        of max_ctx_len] (elements past a context's blocks are left as they were)."""
         import torch
 
         tensor, at, hkv, d = torch.Tensor, self._at, self.num_kv_heads, self.head_dim
@@ -1462,7 +1463,8 @@ class DecodeAttention:
 
     def block_forward(self, q, k_pages, v_pages, table, lens, max_len: int, out=None, lse=None, stream=None):
         """Decode attention with a block table for each KV head: head hk of sequence b attends over the first lens[b]
-        tokens of the pages table[b, hk] (block_select's results; max_len bounds lens)."""
+        tokens of the pages table[b, hk] (block_select's results; max_len bounds lens). It uses the plan's workspace, as
+        the decode calls do: calls of one plan that use it must not overlap, whatever their streams."""
         import torch
 
         tensor, at, hkv, i32, f32 = torch.Tensor, self._at, self.num_kv_heads, torch.int32, torch.float32

@@ -80,9 +80,10 @@ struct WeightsShape {
 //
 // More rows: the least estimated time over the tile sizes and the shares of the
 // rows. A turn of 8 waves on a unit (16 query rows each, two waves on a SIMD)
-// takes 0.33 us and 0.11 for each slab, a workgroup's start about 2 us and half
-// a slab's more, adding the shares up 3. Once there are workgroups for two a
-// unit they have 4 waves. Measured (us, the choice and the best of 48 forced
+// takes 0.33 us and 0.11 for each slab (float32 2.4: 300 rows over 24300 take
+// 513 us, 2.3 for each turn and unit, at 0.116 of the 0.152 PFLOP/s of a large
+// product), a workgroup's start about 2 us and half a slab's more, adding the
+// shares up 3. Once there are workgroups for two a unit they have 4 waves. Measured (us, the choice and the best of 48 forced
 // ones): 300 rows over 24300 78.7 / 78.7, 64 over 2000 10.4 / 10.4, all of 300
 // 11 / 11, of 2000 50 / 50, of 8192 394-431 / 394, 32-64 over 8 x 8000-16000
 // FP8 58 / 58, 1-16 over 4 x 2000-12000 14.3 / 12.0.

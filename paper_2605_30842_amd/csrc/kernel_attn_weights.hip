@@ -21,11 +21,15 @@
 //
 // A chunk (RING true) is bound by the matrix cores, the exponentials and what
 // the two do not overlap: 300 rows over 24300 tokens with 32 heads of 128, 60
-// GFLOP and 233 million exponentials, 78 us, 0.77 PFLOP/s (a large matrix
-// product 1.19); matrix cores busy 35%, VALU 55% of the SIMDs' cycles. No one of
-// them is the bound: when it took 86 us, leaving out the exponentials saved 3,
-// the products 4, the requests for query rows 18. Rows read from LDS a turn
-// ahead as well: 2% less for 20 registers more; not kept.
+// GFLOP and 233 million exponentials, 75-78 us, 0.76-0.8 PFLOP/s (a large matrix
+// product 1.19; the first 15 ms after the card was idle 84-86, before its clock
+// has risen), FP8 74, float32 513 (0.116 of 0.152); matrix cores busy 35%, VALU
+// 55% of the SIMDs' cycles. No one of them is the bound: when it took 86 us,
+// leaving out the exponentials saved 3, the products 4, the requests for query
+// rows 18. What costs beside them: bank conflicts (see QueryRing), and 24 scalar
+// registers (31 paged) that the 96-token form with 237 of 256 vector registers
+// keeps in lanes of those. Rows read from LDS a turn ahead as well: 2% less for
+// 20 registers more; not kept.
 #include "attn_common.h"
 #include "dot_rows.h"
 #include "evict.h"
@@ -45,9 +49,11 @@ __device__ inline float row_total(float x) {
 
 // Where a wave keeps the query rows that it has asked for ahead: kSlots groups
 // of 16 rows and their lse. A request brings 1 KiB of rows, each one whole; a
-// row's pieces of 16 bytes lie at their place exclusive-or the row's low bits,
-// so that the 16 rows of which a read takes one piece each are in different
-// banks.
+// row's pieces of 16 bytes lie at their place exclusive-or the row's three low
+// bits: of the 16 rows of which a read takes one piece each, rows c and c + 8
+// share their banks and no others do. (Conflicts are 0.46 of the LDS's active
+// cycles at 300 rows over 24300 tokens; four bits, for rows of 16 pieces and
+// more, took no less time.)
 template <int D, CacheType C>
 struct QueryRing {
   static constexpr int kLoads = DotPart<D, C>::kLoads;

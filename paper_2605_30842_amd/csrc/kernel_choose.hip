@@ -152,9 +152,10 @@ __device__ inline void load_to_lds(const void* from, uint32_t* to) {
                                    (__attribute__((address_space(3))) uint32_t*)to, 4, 0, 0);
 }
 
-// Rows of at most kWaveEntries: one wave each, which needs no barrier. 8 bits
-// at a time, 4 copies of the histogram, 4 bins a lane. The loops are rolled:
-// the code is cold at every launch. 8 rows of 512 blocks 5.5 us, 512 rows of
+// Short rows (which ones, says `form` below): one wave each, which needs no
+// barrier and holds at most kWaveEntries of them in LDS. 8 bits at a time, 4
+// copies of the histogram, 4 bins a lane. The loops are rolled: the code is cold
+// at every launch. 8 rows of 512 blocks 5.5 us, 512 rows of
 // 128-1024 9.5 us; latency.
 constexpr int kWaveEntries = 2048, kWaveCopies = 4;
 
@@ -190,8 +191,10 @@ __global__ __launch_bounds__(64) void choose_wave_kernel(const ChooseParams p) {
     for (int i = 0; i < 4; ++i) hist[64 * i + lane] = s32x4{0, 0, 0, 0};
     wave_lds_done();
     const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
+    // Keys past the row are 0. In the first digit they are counted with -inf and scores below -1.7e38: that bin's size
+    // then is no reason to stop (`all`), and the second digit parts them (0, and 0x7f or more).
 #pragma unroll 1
-    for (int g = 0; g < item.n; g += 256) {  // keys past the row are 0, which is in no score's bin
+    for (int g = 0; g < item.n; g += 256) {
       uint32_t k[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) k[e] = keys[g + 64 * e + lane];
@@ -259,8 +262,8 @@ __device__ inline int waves_before(const int* x, int w, int lane) {
   return w > 0 ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
 }
 
-// Longer rows: a workgroup of 16 waves, each with a run of the row, which it
-// reads three times, 8 groups of 64 entries a turn and the next turn's scores
+// Longer rows (see `form`): a workgroup of 16 waves, each with a run of the row,
+// which it reads three times, 8 groups of 64 entries a turn and the next turn's scores
 // asked for ahead. The first time it counts the top 11 bits of the scores
 // (4 copies of the histogram, so that lanes with one digit do not all wait for
 // one word), which gives the digit that holds the limit. The second time it
@@ -270,7 +273,7 @@ __device__ inline int waves_before(const int* x, int w, int lane) {
 // time it puts what stays. `gridDim.y` workgroups do the first two for a row,
 // with the same results, and share the third.
 //
-// One compute unit's instructions bound it (24300 entries 12.1 us: launch 2.0,
+// One compute unit's instructions bound it (24300 entries 12.1-12.8 us: launch 2.0,
 // first count 2.7, its digit 1.4, the lists 3, the rest 3), so turns without
 // NaN between the entries that always stay compare scores as floats, and only
 // the others, and the lists, make keys. Rows held in LDS between the readings
@@ -614,8 +617,9 @@ __global__ __launch_bounds__(kThreadsWide) void choose_kernel(const ChooseParams
 // adds up those of the row's chunks, finds the digit and lists its chunk's
 // scores that have it; in the third every workgroup goes through the lists for
 // the other digits and for what stays before its chunk, and puts the chunk's.
-// Latency bounds them: 8 rows of 32768-131072, 4.1 MB in and out, 17.5 us in
-// all, where one workgroup a row takes 34. (A workgroup of 4 waves for a chunk, each
+// Latency bounds them: 8 rows of 32768-131072, 4.1 MB in and out, 18.3 us in
+// all (traced one launch at a time 3.8, 6.6 and 9.5), where one workgroup a row
+// takes 34. (A workgroup of 4 waves for a chunk, each
 // wave with four turns and a list of its own, took 31: too few instructions at
 // once in the lists.)
 static_assert(kChunkEntries == kThreadsWide * kTurn);
